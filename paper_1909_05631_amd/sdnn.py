@@ -17,6 +17,7 @@ EXPORTED_SYMBOLS = [
     "sdnn_live_counts", "sdnn_final_rows", "sdnn_destroy", "sdnn_last_error", "sdnn_kernel_path",
     "sdnn_set_profiling", "sdnn_layer_times", "sdnn_layer_info", "sdnn_enable_equal_value_kernels",
     "sdnn_infer_static", "sdnn_layer_kernel",
+    "sdnn_readout_workspace_bytes", "sdnn_readout_loss", "sdnn_readout_grad",
 ]
 # kernel families of sdnn_layer_info by a kernel of each (Net.layer_kernels names the kernel itself)
 KERNEL_KINDS = {0: "none", 1: "k_layer_lds", 2: "k_layer_gfm", 3: "k_layer_gfm_u8", 4: "k_layer_gfm_small",
@@ -63,9 +64,14 @@ def load_library():
         L.sdnn_enable_equal_value_kernels.argtypes = [vp, i32]
         L.sdnn_infer_static.argtypes = [vp, vp, i64, vp]
         L.sdnn_layer_kernel.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_char_p)]
+        L.sdnn_readout_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        L.sdnn_readout_workspace_bytes.restype = sz
+        L.sdnn_readout_loss.argtypes = [vp, i64, vp, i64, i32, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+        L.sdnn_readout_grad.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, i64, i64, i64, vp, i64, vp, i64, vp, sz, vp]
         for name in ("sdnn_create", "sdnn_load_layers", "sdnn_infer", "sdnn_categories", "sdnn_live_counts",
                      "sdnn_final_rows", "sdnn_set_profiling", "sdnn_layer_times", "sdnn_layer_info",
-                     "sdnn_enable_equal_value_kernels", "sdnn_infer_static", "sdnn_layer_kernel"):
+                     "sdnn_enable_equal_value_kernels", "sdnn_infer_static", "sdnn_layer_kernel",
+                     "sdnn_readout_loss", "sdnn_readout_grad"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
