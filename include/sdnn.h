@@ -236,6 +236,54 @@ sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t
                               int64_t n_classes, int64_t n_features, void *dx, int64_t lddx, void *dw, int64_t lddw,
                               void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Bytes of workspace for sdnn_orthogonalize; 0 for sizes that it refuses: batch in [0, 65535], rows and cols in
+ * [1, 2^20]. */
+size_t sdnn_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols);
+
+/* Orthogonalise `batch` matrices of rows x cols by Newton-Schulz products: X = g / (||g||_F + eps), then `steps`
+ * times X <- a X + (b A + c A A) X with A = X X^T and coefficients = {a, b, c} (host, 3 values), in the smaller of the
+ * two sizes (for rows > cols the same X is found from X^T X).
+ *   g, out: device, of `dtype`, row strides ldg and ldo, batch strides (values; ignored for one matrix). out may be
+ *   g itself (same strides), and may not overlap it otherwise.
+ * Every product is of factors held in two fp16 parts, with fp32 sums; the result is rounded to `dtype` once. A
+ * matrix of zeros gives zeros (eps > 0); one with an infinity or a NaN gives NaN where those reach.
+ * steps in [0, 32]; eps >= 0; |coefficients| <= 1e6. */
+sdnn_status sdnn_orthogonalize(const void *g, int64_t ldg, int64_t batch_stride_g, void *out, int64_t ldo,
+                               int64_t batch_stride_o, int32_t dtype, int64_t batch, int64_t rows, int64_t cols,
+                               int32_t steps, const float *coefficients, float eps, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
+/* Rows of microscaled 4-bit floats: n_values values are held in sdnn_mx_blocks(n_values) blocks of 32 (whole runs of
+ * 4 blocks; 0 for n_values outside [1, 2^20]). A matrix of n_rows rows is
+ *   codes:  n_rows x 16 * blocks bytes, 16-byte aligned; a byte holds values 2i (low half) and 2i + 1: a sign bit over a
+ *           magnitude code of {0, 0.5, 1, 1.5, 2, 3, 4, 6};
+ *   scales: n_rows x blocks bytes, 4-byte aligned; s stands for 2^(s - 127), 255 for a block of NaN.
+ * Codes past n_values are zero. */
+int64_t sdnn_mx_blocks(int64_t n_values);
+
+/* Quantise x (n_rows x n_values of `dtype`, row stride ldx). A block's scale is 2^(floor(log2 max|x|) - 2), at least
+ * 2^-127; values are rounded to the nearest code, ties to the even one, magnitudes over 6 to 6. A block with
+ * an infinity or a NaN becomes NaN. */
+sdnn_status sdnn_mx_quantize(const void *x, int64_t ldx, int32_t dtype, int64_t n_rows, int64_t n_values, uint8_t *codes,
+                             uint8_t *scales, void *hip_stream);
+
+/* The values that codes and scales stand for, in out (n_rows x n_values of `dtype`, row stride ldo). */
+sdnn_status sdnn_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n_rows, int64_t n_values, void *out,
+                               int64_t ldo, int32_t dtype, void *hip_stream);
+
+/* out = x w^T of quantised rows (x: n_rows, w: n_outputs rows, both of n_values): fp32 sums of exact products, rounded
+ * to `dtype` once. out: n_rows x n_outputs, row stride ldo. */
+sdnn_status sdnn_mx_product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes,
+                            const uint8_t *w_scales, int64_t n_rows, int64_t n_outputs, int64_t n_values, void *out,
+                            int64_t ldo, int32_t dtype, void *hip_stream);
+
+/* The same for rows x of `dtype` (row stride ldx) that are quantised on the way: a readout's answer with its weights held
+ * in 4 bits. The result is that of sdnn_mx_quantize and sdnn_mx_product. */
+size_t sdnn_mx_linear_workspace_bytes(int64_t n_rows, int64_t n_values);
+sdnn_status sdnn_mx_linear(const void *x, int64_t ldx, int32_t dtype, const uint8_t *w_codes, const uint8_t *w_scales,
+                           int64_t n_rows, int64_t n_outputs, int64_t n_values, void *out, int64_t ldo, void *workspace,
+                           size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "error.h"
@@ -18,6 +19,7 @@ using tile::f32x4;
 constexpr int kXcds = 8;
 constexpr int kCus = 256;  // compute units: what a launch has to fill
 constexpr int64_t kMaxRows = 1 << 24, kMaxClasses = 1 << 24, kMaxFeatures = 1 << 20;
+constexpr int kMaxSplits = 64;
 constexpr int64_t kMaxPitch = 1 << 22;  // bytes from row to row that the tiles' 32-bit offsets reach over 256 rows
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -105,9 +107,18 @@ __device__ __forceinline__ int split_exponent(float top) {
 struct Blocks {
   int rows, cols, splits;  // blocks of rows, of columns, parts of k
   int64_t slabs;           // of all of k
+  bool symmetric;          // square blocks on and above the diagonal only
   __device__ __forceinline__ void locate(int id, int total, int &r, int &c, int &split) const {
     const int whole = total / kXcds * kXcds;
     if (id < whole) id = id % kXcds * (total / kXcds) + id / kXcds;
+    if (symmetric) {
+      c = (int)((sqrtf(8.0f * id + 1.0f) - 1.0f) * 0.5f);
+      while (c * (c + 1) / 2 > id) --c;
+      while ((c + 1) * (c + 2) / 2 <= id) ++c;
+      r = id - c * (c + 1) / 2;
+      split = 0;
+      return;
+    }
     const int per = rows * cols;
     split = id / per;
     id -= split * per;
@@ -129,14 +140,16 @@ struct Matrix {
   int64_t pitch;   // bytes
   int64_t rows;    // along: rows; across: rows of k
   int64_t extent;  // bytes in a row: of k (along), of columns (across)
+  int64_t batch;   // bytes from one matrix of a batch (blockIdx.y) to the next
   template <int KIND, int SIZE, bool ACROSS>
   __device__ __forceinline__ tile::Operand at(int block) const {
     const int64_t first = (int64_t)block * SIZE;
+    const char *here = data + blockIdx.y * batch;
     if (ACROSS) {
       const int64_t skip = first * tile::Geometry<KIND>::kBytes;
-      return {data + skip, pitch, rows, extent - skip};
+      return {here + skip, pitch, rows, extent - skip};
     }
-    return {data + first * pitch, pitch, rows - first, extent};
+    return {here + first * pitch, pitch, rows - first, extent};
   }
 };
 
@@ -149,22 +162,87 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
   blocks.range(split, s0, s1);
   B block;
   block.run(a.template at<KIND, BM, ACROSS_A>(r), b.template at<KIND, BN, ACROSS_B>(c), s0, s1, lds);
-  epilogue(block, (int64_t)r * BM + B::row0(), (int64_t)c * BN + B::col0(), split, c);
+  epilogue(block, (int64_t)r * BM + B::row0(), (int64_t)c * BN + B::col0(), split, r != c);
 }
 
 // Launches the blocks of one shape. What the sizes need of it is the caller's rule.
 template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, class Epilogue>
-sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const Epilogue &e, hipStream_t stream, const char *what) {
+sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const Epilogue &e, hipStream_t stream, const char *what, bool symmetric,
+                   int batch) {
   using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B>;
   Blocks blocks;
   blocks.slabs = ceil_div(k, tile::Geometry<KIND>::kPerSlab);
   blocks.splits = splits;
   const int64_t r = ceil_div(rows, BM), c = ceil_div(cols, BN);
-  if (r * c * splits * B::kThreads > 0xffffffffll || a.pitch > kMaxPitch || b.pitch > kMaxPitch) return fail(SDNN_EINVAL, "%s: %lld x %lld outputs are too many for one launch", what, (long long)rows, (long long)cols);
+  const int64_t n = symmetric ? c * (c + 1) / 2 : r * c * splits;
+  blocks.symmetric = symmetric;
+  if (n * B::kThreads > 0xffffffffll || a.pitch > kMaxPitch || b.pitch > kMaxPitch) return fail(SDNN_EINVAL, "%s: %lld x %lld outputs are too many for one launch", what, (long long)rows, (long long)cols);
   blocks.rows = (int)r;
   blocks.cols = (int)c;
-  hipLaunchKernelGGL((k_product<B, KIND, BM, BN, ACROSS_A, ACROSS_B, Epilogue>), dim3((unsigned)(r * c * splits)), dim3(B::kThreads), 0, stream, a, b, blocks, e);
+  hipLaunchKernelGGL((k_product<B, KIND, BM, BN, ACROSS_A, ACROSS_B, Epilogue>), dim3((unsigned)n, (unsigned)batch), dim3(B::kThreads), 0, stream, a, b, blocks, e);
   return launched(what);
+}
+
+// The shapes of a block: outputs, waves, how many a CU holds, microseconds that one takes for a slab when the CU is
+// full of them (its share) and when it is alone.
+enum Shape { kWide, kMiddle, kSmall, kFlat, kTall, kShapes };
+struct ShapeCost {
+  int bm, bn, held;
+  double full, alone;
+};
+constexpr ShapeCost kCost[kShapes] = {
+    {256, 256, 1, 1.9, 1.9}, {128, 128, 2, 0.52, 0.7}, {64, 64, 4, 0.2, 0.5}, {32, 128, 4, 0.2, 0.5}, {128, 32, 4, 0.2, 0.5}};
+
+struct Plan {
+  Shape shape;
+  int splits;
+};
+
+// The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs, and for
+// a split sum its slabs' traffic (at 4 TB/s) and one launch more.
+inline Plan plan(int64_t rows, int64_t cols, int64_t slabs, int most_splits, int64_t batch = 1, bool symmetric = false) {
+  Plan best = {kWide, 1};
+  double least = 1e30;
+  for (int s = 0; s < kShapes; ++s) {
+    const ShapeCost &c = kCost[s];
+    if (symmetric && c.bm != c.bn) continue;
+    const double across = (double)ceil_div(cols, c.bn), blocks = symmetric ? across * (across + 1) / 2 : (double)ceil_div(rows, c.bm) * across;
+    for (int split = 1; split <= most_splits && (split == 1 || split * 2 <= slabs); split *= 2) {
+      const double n = blocks * split * batch, rounds = std::ceil(n / (kCus * c.held));
+      const double held = std::min<double>(c.held, std::ceil(n / kCus));
+      double t = rounds * (double)ceil_div(slabs, split) * std::max(c.alone, held * c.full) + 3.0;
+      if (split > 1) t += 4.0 + 2e-6 * rows * cols * split * batch;
+      if (t < least) {
+        least = t;
+        best = {(Shape)s, split};
+      }
+    }
+  }
+  return best;
+}
+
+template <int KIND, bool AA, bool AB, class E>
+sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
+  switch (p.shape) {
+    case kWide: return launch<KIND, 256, 256, 2, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kMiddle: return launch<KIND, 128, 128, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSmall: return launch<KIND, 64, 64, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kFlat: return launch<KIND, 32, 128, 1, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    default: return launch<KIND, 128, 32, 4, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+  }
+}
+
+inline sdnn_status check_matrix(const char *name, const void *p, int64_t ld, int64_t cols, int32_t dtype) {
+  if (!p) return fail(SDNN_EINVAL, "%s is null", name);
+  if ((uintptr_t)p % dtype_bytes(dtype)) return fail(SDNN_EINVAL, "%s is not aligned to its values", name);
+  if (ld < cols || ld > (1ll << 40)) return fail(SDNN_EINVAL, "the row stride of %s, %lld, is outside [%lld, 2^40]", name, (long long)ld, (long long)cols);
+  return SDNN_OK;
+}
+
+inline sdnn_status check_workspace(const void *p, size_t bytes, size_t need) {
+  if (bytes < need) return fail(SDNN_ERANGE, "workspace of %zu bytes, %zu needed", bytes, need);
+  if (need && (!p || ((uintptr_t)p & 255))) return fail(SDNN_EINVAL, "workspace is null or not 256-byte aligned");
+  return SDNN_OK;
 }
 
 }  // namespace dense

@@ -17,8 +17,6 @@
 // between the products.
 #include "dense.h"
 
-#include <cmath>
-
 using namespace dense;
 using tile::Block;
 using tile::KIND_BF16;
@@ -28,7 +26,6 @@ namespace {
 
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
-constexpr int kMaxSplits = 64;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kGradExponent = 15;  // fp16 parts of exp(l - lse) - [v = y] hold it times 2^15
 
@@ -158,7 +155,7 @@ struct LossParts {
   int64_t count;   // parts of a row
   float *picked;   // the label's logit
   template <class B>
-  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, int) const {
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
     constexpr int kWide = 16 * B::kTN;
 #pragma unroll
@@ -229,7 +226,7 @@ struct WriteGrad {
   char *g;
   int64_t pitch;  // bytes
   template <class B>
-  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, int) const {
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
     const int e = whole_exponent<KIND>(scale);
     const float mean = weights ? 0.0f : scalars->mean;
@@ -286,7 +283,7 @@ struct Store {
   bool vec;
   OutScale scale;
   template <class B>
-  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, int) const {
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
@@ -312,7 +309,7 @@ struct Accumulate {
   int64_t ld, rows, cols;
   bool add;
   template <class B>
-  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int split, int) const {
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int split, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
     float *slab = slabs + split * rows * ld;
 #pragma unroll
@@ -349,53 +346,6 @@ __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int split
 // ------------------------------------------------------------------------------------------------
 // Host
 
-// The shapes of a block: outputs, waves, how many a CU holds, microseconds that one takes for a slab when the CU is
-// full of them (its share) and when it is alone.
-enum Shape { kWide, kMiddle, kSmall, kFlat, kTall, kShapes };
-struct ShapeCost {
-  int bm, bn, held;
-  double full, alone;
-};
-constexpr ShapeCost kCost[kShapes] = {
-    {256, 256, 1, 1.9, 1.9}, {128, 128, 2, 0.52, 0.7}, {64, 64, 4, 0.2, 0.5}, {32, 128, 4, 0.2, 0.5}, {128, 32, 4, 0.2, 0.5}};
-
-struct Plan {
-  Shape shape;
-  int splits;
-};
-
-// The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs, and for
-// a split sum its slabs' traffic (at 4 TB/s) and one launch more.
-Plan plan(int64_t rows, int64_t cols, int64_t slabs, bool may_split) {
-  Plan best = {kWide, 1};
-  double least = 1e30;
-  for (int s = 0; s < kShapes; ++s) {
-    const ShapeCost &c = kCost[s];
-    const double blocks = (double)ceil_div(rows, c.bm) * (double)ceil_div(cols, c.bn);
-    for (int split = 1; split <= (may_split ? kMaxSplits : 1) && (split == 1 || split * 2 <= slabs); split *= 2) {
-      const double n = blocks * split, rounds = std::ceil(n / (kCus * c.held));
-      const double held = std::min<double>(c.held, std::ceil(n / kCus));
-      double t = rounds * (double)ceil_div(slabs, split) * std::max(c.alone, held * c.full) + 3.0;
-      if (split > 1) t += 4.0 + 8e-6 * rows * cols * split / 4.0;
-      if (t < least) {
-        least = t;
-        best = {(Shape)s, split};
-      }
-    }
-  }
-  return best;
-}
-
-template <int KIND, bool AA, bool AB, class E>
-sdnn_status run_shape(Shape s, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const E &e, hipStream_t stream, const char *what) {
-  switch (s) {
-    case kWide: return launch<KIND, 256, 256, 2, 4, AA, AB>(a, b, rows, cols, k, splits, e, stream, what);
-    case kMiddle: return launch<KIND, 128, 128, 2, 2, AA, AB>(a, b, rows, cols, k, splits, e, stream, what);
-    case kSmall: return launch<KIND, 64, 64, 2, 2, AA, AB>(a, b, rows, cols, k, splits, e, stream, what);
-    case kFlat: return launch<KIND, 32, 128, 1, 4, AA, AB>(a, b, rows, cols, k, splits, e, stream, what);
-    default: return launch<KIND, 128, 32, 4, 1, AA, AB>(a, b, rows, cols, k, splits, e, stream, what);
-  }
-}
 constexpr int kWaveCols[kShapes] = {64, 64, 32, 32, 32};  // columns of a wave: the parts of a row of logits
 
 // Sizes of one call.
@@ -413,10 +363,10 @@ struct Sizes {
     return std::min(p, classes);
   }
   int64_t g_pitch() const { return ceil_div(piece(), per_slab()) * 128; }
-  Plan loss() const { return plan(rows, classes, feature_slabs(), false); }
-  Plan logits(int64_t n) const { return plan(rows, n, feature_slabs(), false); }
-  Plan dx() const { return plan(rows, features, ceil_div(piece(), per_slab()), true); }
-  Plan dw(int64_t n) const { return plan(n, features, ceil_div(rows, per_slab()), true); }
+  Plan loss() const { return plan(rows, classes, feature_slabs(), 1); }
+  Plan logits(int64_t n) const { return plan(rows, n, feature_slabs(), 1); }
+  Plan dx() const { return plan(rows, features, ceil_div(piece(), per_slab()), kMaxSplits); }
+  Plan dw(int64_t n) const { return plan(n, features, ceil_div(rows, per_slab()), kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
 };
 
@@ -467,15 +417,15 @@ unsigned row_grid(int64_t rows) { return (unsigned)std::max<int64_t>(1, std::min
 template <int KIND>
 Matrix operand(const void *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, const uint32_t *top, int *exponents, const float *weights, char *space, hipStream_t stream) {
   if constexpr (KIND == KIND_BF16) {
-    if (!labels && usable_in_place(data, ld, s.features)) return {(const char *)data, ld * 2, rows, s.features * 2};
+    if (!labels && usable_in_place(data, ld, s.features)) return {(const char *)data, ld * 2, rows, s.features * 2, 0};
     const bool vec = ((uintptr_t)data & 15) == 0 && ld % 8 == 0;
     if (rows)
       hipLaunchKernelGGL(k_copy_rows, dim3(row_grid(rows)), dim3(256), 0, stream, (const __bf16 *)data, ld, rows, s.features, s.pitch_values(), labels, s.classes, vec, (__bf16 *)space);
-    return {space, s.pitch_values() * 2, rows, s.pitch_values() * 2};
+    return {space, s.pitch_values() * 2, rows, s.pitch_values() * 2, 0};
   } else {
     if (rows)
       hipLaunchKernelGGL(k_split_rows, dim3(row_grid(rows)), dim3(256), 0, stream, (const float *)data, ld, rows, s.features, s.groups(), labels, s.classes, weights, top, exponents, space);
-    return {space, s.groups() * 128, rows, s.groups() * 128};
+    return {space, s.groups() * 128, rows, s.groups() * 128, 0};
   }
 }
 
@@ -488,7 +438,7 @@ sdnn_status loss_of(const Sizes &s, const void *x, int64_t ldx, const void *w, i
   sdnn_status st = launched("rows");
   if (st != SDNN_OK) return st;
   const LossParts<KIND> e{{sp.ex, sp.ew, nullptr, nullptr}, labels, s.rows, s.classes, sp.parts, sp.count, sp.picked};
-  st = run_shape<KIND, false, false>(s.loss().shape, a, b, s.rows, s.classes, s.features, 1, e, stream, "loss");
+  st = run_shape<KIND, false, false>(s.loss(), a, b, s.rows, s.classes, s.features, e, stream, "loss");
   if (st != SDNN_OK) return st;
   hipLaunchKernelGGL(k_loss, dim3((unsigned)ceil_div(s.rows, 4)), dim3(256), 0, stream, sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse);
   return launched("loss");
@@ -497,9 +447,9 @@ sdnn_status loss_of(const Sizes &s, const void *x, int64_t ldx, const void *w, i
 // C = A B^T over k, into `to` directly or through fp32 slabs.
 template <int KIND, bool AA, class T>
 sdnn_status product(const Plan &p, const Matrix &a, const Matrix &b, int64_t k, float *slabs, int64_t ld_slab, bool through, bool add, bool last, const Store<T> &to, hipStream_t stream, const char *what) {
-  if (!through) return run_shape<KIND, AA, true>(p.shape, a, b, to.rows, to.cols, k, 1, to, stream, what);
+  if (!through) return run_shape<KIND, AA, true>(p, a, b, to.rows, to.cols, k, to, stream, what);
   const Accumulate e{slabs, ld_slab, to.rows, to.cols, add};
-  sdnn_status st = run_shape<KIND, AA, true>(p.shape, a, b, to.rows, to.cols, k, p.splits, e, stream, what);
+  sdnn_status st = run_shape<KIND, AA, true>(p, a, b, to.rows, to.cols, k, e, stream, what);
   if (st != SDNN_OK || !last) return st;
   const int64_t work = ceil_div(to.rows * (ld_slab / 4), 256);
   hipLaunchKernelGGL((k_sum_slabs<T>), dim3((unsigned)std::min<int64_t>(work, 8192)), dim3(256), 0, stream, slabs, p.splits, ld_slab, to);
@@ -557,18 +507,18 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     wp.data += v0 * b.pitch;
     wp.rows = n;
     const WriteGrad<KIND> e{{nullptr, nullptr, top_x, top_w}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
-    st = run_shape<KIND, false, false>(s.logits(n).shape, a, wp, s.rows, n, s.features, 1, e, stream, "gradient");
+    st = run_shape<KIND, false, false>(s.logits(n), a, wp, s.rows, n, s.features, e, stream, "gradient");
     if (st != SDNN_OK) return st;
     const int64_t wide = KIND == KIND_SPLIT ? ceil_div(n, 32) * 128 : ceil_div(n, 8) * 16;  // bytes of a row of G
     if (dx) {
       const Store<T> to{dx, lddx, s.rows, s.features, vector_rows(dx, lddx), {row_weights, mean, top_w}};
-      st = product<KIND, false>(px, Matrix{sp.g, s.g_pitch(), s.rows, wide}, wp, n, sp.dx, s.ld_slab(), through_x, v0 > 0, last, to, stream, "gradient of the rows");
+      st = product<KIND, false>(px, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, wp, n, sp.dx, s.ld_slab(), through_x, v0 > 0, last, to, stream, "gradient of the rows");
       if (st != SDNN_OK) return st;
     }
     if (dw) {
       const Plan pw = s.dw(n);
       const Store<T> to{dw + v0 * lddw, lddw, n, s.features, vector_rows(dw + v0 * lddw, lddw), {nullptr, mean, top_g}};
-      st = product<KIND, true>(pw, Matrix{sp.g, s.g_pitch(), s.rows, wide}, ag, s.rows, sp.dw, s.ld_slab(), pw.splits > 1, false, true, to, stream, "gradient of the weights");
+      st = product<KIND, true>(pw, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, ag, s.rows, sp.dw, s.ld_slab(), pw.splits > 1, false, true, to, stream, "gradient of the weights");
     }
   }
   return st;
@@ -579,19 +529,6 @@ sdnn_status check_sizes(int64_t n_rows, int64_t n_classes, int64_t n_features, i
   if (n_classes < 1 || n_classes > kMaxClasses) return fail(SDNN_EINVAL, "n_classes %lld is outside [1, %lld]", (long long)n_classes, (long long)kMaxClasses);
   if (n_features < 1 || n_features > kMaxFeatures) return fail(SDNN_EINVAL, "n_features %lld is outside [1, %lld]", (long long)n_features, (long long)kMaxFeatures);
   if (!good_dtype(dtype)) return fail(SDNN_EINVAL, "dtype %d is neither SDNN_FP32 nor SDNN_BF16", dtype);
-  return SDNN_OK;
-}
-
-sdnn_status check_matrix(const char *name, const void *p, int64_t ld, int64_t cols, int32_t dtype) {
-  if (!p) return fail(SDNN_EINVAL, "%s is null", name);
-  if ((uintptr_t)p % dtype_bytes(dtype)) return fail(SDNN_EINVAL, "%s is not aligned to its values", name);
-  if (ld < cols || ld > (1ll << 40)) return fail(SDNN_EINVAL, "the row stride of %s, %lld, is outside [%lld, 2^40]", name, (long long)ld, (long long)cols);
-  return SDNN_OK;
-}
-
-sdnn_status check_workspace(const void *p, size_t bytes, size_t need) {
-  if (bytes < need) return fail(SDNN_ERANGE, "workspace of %zu bytes, %zu needed", bytes, need);
-  if (need && (!p || ((uintptr_t)p & 255))) return fail(SDNN_EINVAL, "workspace is null or not 256-byte aligned");
   return SDNN_OK;
 }
 
