@@ -106,7 +106,7 @@ __device__ __forceinline__ int split_exponent(float top) {
 // which share their operands in its L2.
 struct Blocks {
   int rows, cols, splits;  // blocks of rows, of columns, parts of k
-  int64_t slabs;           // of all of k
+  int slabs, per;          // slabs of all of k, of a part
   bool symmetric;          // square blocks on and above the diagonal only
   __device__ __forceinline__ void locate(int id, int total, int &r, int &c, int &split) const {
     const int whole = total / kXcds * kXcds;
@@ -119,18 +119,17 @@ struct Blocks {
       split = 0;
       return;
     }
-    const int per = rows * cols;
-    split = id / per;
-    id -= split * per;
+    const int area = rows * cols;
+    split = id / area;
+    id -= split * area;
     const int tall = 8 * cols, g = id / tall, in = id - g * tall;
     const int h = rows - g * 8 < 8 ? rows - g * 8 : 8;
     c = in / h;
     r = g * 8 + in - c * h;
   }
-  __device__ __forceinline__ void range(int split, int64_t &s0, int64_t &s1) const {
-    const int64_t per = (slabs + splits - 1) / splits;
-    s0 = split * per < slabs ? split * per : slabs;
-    s1 = s0 + per < slabs ? s0 + per : slabs;
+  __device__ __forceinline__ void range(int split, int &s0, int &s1) const {
+    s0 = tile::uniform(min(split * per, slabs));
+    s1 = tile::uniform(min(s0 + per, slabs));
   }
 };
 
@@ -141,15 +140,16 @@ struct Matrix {
   int64_t rows;    // along: rows; across: rows of k
   int64_t extent;  // bytes in a row: of k (along), of columns (across)
   int64_t batch;   // bytes from one matrix of a batch (blockIdx.y) to the next
+  const uint8_t *scales = nullptr;  // KIND_MX: pitch / 16 bytes a row
   template <int KIND, int SIZE, bool ACROSS>
   __device__ __forceinline__ tile::Operand at(int block) const {
     const int64_t first = (int64_t)block * SIZE;
     const char *here = data + blockIdx.y * batch;
     if (ACROSS) {
       const int64_t skip = first * tile::Geometry<KIND>::kBytes;
-      return {here + skip, pitch, rows, extent - skip};
+      return {here + skip, (int)pitch, (int)rows, (int)(extent - skip)};
     }
-    return {here + first * pitch, pitch, rows - first, extent};
+    return {here + first * pitch, (int)pitch, (int)(rows - first), (int)extent, scales ? (const char *)scales + first * (pitch / 16) : nullptr};
   }
 };
 
@@ -158,7 +158,9 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
   __shared__ __attribute__((aligned(1024))) char lds[B::kLds];
   int r, c, split;
   blocks.locate(blockIdx.x, gridDim.x, r, c, split);
-  int64_t s0, s1;
+  r = tile::uniform(r);
+  c = tile::uniform(c);
+  int s0, s1;
   blocks.range(split, s0, s1);
   B block;
   block.run(a.template at<KIND, BM, ACROSS_A>(r), b.template at<KIND, BN, ACROSS_B>(c), s0, s1, lds);
@@ -166,12 +168,13 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
 }
 
 // Launches the blocks of one shape. What the sizes need of it is the caller's rule.
-template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, class Epilogue>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES, bool ACROSS_A, bool ACROSS_B, class Epilogue>
 sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const Epilogue &e, hipStream_t stream, const char *what, bool symmetric,
                    int batch) {
-  using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B>;
+  using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES>;
   Blocks blocks;
-  blocks.slabs = ceil_div(k, tile::Geometry<KIND>::kPerSlab);
+  blocks.slabs = (int)ceil_div(k, tile::Geometry<KIND>::kPerSlab);
+  blocks.per = (int)ceil_div(blocks.slabs, splits);
   blocks.splits = splits;
   const int64_t r = ceil_div(rows, BM), c = ceil_div(cols, BN);
   const int64_t n = symmetric ? c * (c + 1) / 2 : r * c * splits;
@@ -183,29 +186,30 @@ sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols,
   return launched(what);
 }
 
-// The shapes of a block: outputs, waves, how many a CU holds, microseconds that one takes for a slab when the CU is
-// full of them (its share) and when it is alone.
-enum Shape { kWide, kMiddle, kSmall, kFlat, kTall, kShapes };
+// The shapes of a block: outputs, how many a CU holds, microseconds that one takes for a slab when the CU is full of
+// them (its share) and when it is alone.
+enum Shape { kWide, kMiddle, kSquare, kSmall, kFlat, kTall, kShapes };
 struct ShapeCost {
   int bm, bn, held;
   double full, alone;
 };
-constexpr ShapeCost kCost[kShapes] = {
-    {256, 256, 1, 1.9, 1.9}, {128, 128, 2, 0.52, 0.7}, {64, 64, 4, 0.2, 0.5}, {32, 128, 4, 0.2, 0.5}, {128, 32, 4, 0.2, 0.5}};
+constexpr ShapeCost kCost[kShapes] = {{256, 256, 1, 1.6, 1.6},  {192, 192, 1, 0.95, 0.95}, {128, 128, 2, 0.52, 0.6},
+                                      {64, 64, 2, 0.2, 0.25}, {32, 128, 2, 0.2, 0.25},   {128, 32, 2, 0.2, 0.25}};
 
 struct Plan {
   Shape shape;
   int splits;
 };
+enum Form { kAnyForm, kAlong };  // kAlong: both operands are (rows of 192 columns make no whole loads)
 
 // The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs, and for
 // a split sum its slabs' traffic (at 4 TB/s) and one launch more.
-inline Plan plan(int64_t rows, int64_t cols, int64_t slabs, int most_splits, int64_t batch = 1, bool symmetric = false) {
+inline Plan plan(int64_t rows, int64_t cols, int64_t slabs, int most_splits, Form form = kAnyForm, int64_t batch = 1, bool symmetric = false) {
   Plan best = {kWide, 1};
   double least = 1e30;
   for (int s = 0; s < kShapes; ++s) {
     const ShapeCost &c = kCost[s];
-    if (symmetric && c.bm != c.bn) continue;
+    if ((symmetric && c.bm != c.bn) || (s == kMiddle && form != kAlong)) continue;
     const double across = (double)ceil_div(cols, c.bn), blocks = symmetric ? across * (across + 1) / 2 : (double)ceil_div(rows, c.bm) * across;
     for (int split = 1; split <= most_splits && (split == 1 || split * 2 <= slabs); split *= 2) {
       const double n = blocks * split * batch, rounds = std::ceil(n / (kCus * c.held));
@@ -224,11 +228,13 @@ inline Plan plan(int64_t rows, int64_t cols, int64_t slabs, int most_splits, int
 template <int KIND, bool AA, bool AB, class E>
 sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
   switch (p.shape) {
-    case kWide: return launch<KIND, 256, 256, 2, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kMiddle: return launch<KIND, 128, 128, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSmall: return launch<KIND, 64, 64, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kFlat: return launch<KIND, 32, 128, 1, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    default: return launch<KIND, 128, 32, 4, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kWide: return launch<KIND, 256, 256, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kMiddle:
+      if constexpr (!AA && !AB) return launch<KIND, 192, 192, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kFlat: return launch<KIND, 32, 128, 1, 4, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    default: return launch<KIND, 128, 32, 4, 1, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
   }
 }
 

@@ -11,8 +11,6 @@
 #include "dense.h"
 
 using namespace dense;
-using tile::i32x4;
-using tile::i32x8;
 using tile::KIND_MX;
 
 namespace {
@@ -105,140 +103,34 @@ __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *codes, const 
   }
 }
 
-// Rows of codes with their scales as an operand.
-struct MxMatrix {
-  const char *codes;
-  const uint8_t *scales;
-  int64_t rows, blocks;
-};
-
-__device__ __forceinline__ f32x4 mfma_mx(i32x4 a, i32x4 b, f32x4 c, int q, int sa, int sb) {
-  const i32x8 wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-  // format 4: 4-bit floats (they fill half of the operand); byte q of the scale registers
-  return q == 0 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, 0, sa, 0, sb) : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, 1, sa, 1, sb);
-}
-
-// The product of one block: tile::Block's loop with the scales, which go from global memory to registers a slab ahead
-// (two bytes a lane and subtile: the scales of its two blocks).
-template <int BM, int BN, int WM, int WN>
-struct MxBlock {
-  using Base = tile::Block<KIND_MX, BM, BN, WM, WN, false, false>;
-  static constexpr int kThreads = Base::kThreads, kTM = Base::kTM, kTN = Base::kTN, kLds = Base::kLds;
-  f32x4 acc[kTM][kTN];
-
-  template <int SUBTILES>
-  __device__ __forceinline__ static void scales_of(const MxMatrix &m, int64_t first, int64_t s, int (&out)[SUBTILES]) {
-    const int lane = threadIdx.x & 63, i = lane & 15, j = lane >> 4;
-    const int64_t block = s * 8 + 2 * j;
+template <class T>
+struct Store {
+  T *out;
+  int64_t ld, rows, cols;
+  bool vec;
+  template <class B>
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
+    const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
 #pragma unroll
-    for (int t = 0; t < SUBTILES; ++t) {
-      const int64_t r = first + 16 * t + i;
-      out[t] = r < m.rows && block < m.blocks ? *(const uint16_t *)(m.scales + r * m.blocks + block) : 0;
-    }
-  }
-
-  __device__ __forceinline__ void run(const MxMatrix &a, const MxMatrix &b, int64_t row, int64_t col, char *lds) {
-    const int64_t pitch = a.blocks * 16, slabs = (a.blocks + 7) / 8;
-    const tile::Operand oa{a.codes + row * pitch, pitch, a.rows - row, pitch}, ob{b.codes + col * pitch, pitch, b.rows - col, pitch};
-    typename Base::LoadA la;
-    typename Base::LoadB lb;
-    la.init(oa);
-    lb.init(ob);
-    tile::Reader<KIND_MX, BM, false> ra;
-    tile::Reader<KIND_MX, BN, false> rb;
-    ra.init(Base::row0());
-    rb.init(Base::col0());
-    int sa[kTM], sb[kTN], na[kTM], nb[kTN];
+    for (int i = 0; i < B::kTM; ++i) {
+      const int64_t r = row0 + 16 * i + i16;
+      if (r >= rows) continue;
 #pragma unroll
-    for (int i = 0; i < kTM; ++i)
-#pragma unroll
-      for (int j = 0; j < kTN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    la.load(oa, 0, lds);
-    lb.load(ob, 0, lds + BM * tile::kSlab);
-    scales_of<kTM>(a, row + Base::row0(), 0, na);
-    scales_of<kTN>(b, col + Base::col0(), 0, nb);
-    for (int64_t s = 0; s < slabs; ++s) {
-      char *now = lds + (s & 1) * Base::kStage, *next = lds + ((s + 1) & 1) * Base::kStage;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      i32x4 fa[kTM][2], fb[kTN][2];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-#pragma unroll
-        for (int j = 0; j < kTN; ++j) fb[j][q] = rb.read(now + BM * tile::kSlab, j, q);
-#pragma unroll
-        for (int i = 0; i < kTM; ++i) fa[i][q] = ra.read(now, i, q);
+      for (int j = 0; j < B::kTN; ++j) {
+        const int64_t c = col0 + 16 * j + 4 * j4;
+        if (c >= cols) continue;
+        store4(out + r * ld + c, block.acc[i][j], (int)(cols - c < 4 ? cols - c : 4), vec);
       }
-#pragma unroll
-      for (int i = 0; i < kTM; ++i) sa[i] = na[i];
-#pragma unroll
-      for (int j = 0; j < kTN; ++j) sb[j] = nb[j];
-      if (s + 1 < slabs) {
-        la.load(oa, s + 1, next);
-        lb.load(ob, s + 1, next + BM * tile::kSlab);
-        scales_of<kTM>(a, row + Base::row0(), s + 1, na);
-        scales_of<kTN>(b, col + Base::col0(), s + 1, nb);
-      }
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < kTM; ++i)
-#pragma unroll
-          for (int j = 0; j < kTN; ++j) acc[i][j] = mfma_mx(fb[j][q], fa[i][q], acc[i][j], q, sb[j], sa[i]);
     }
-#pragma unroll
-    for (int i = 0; i < kTM; ++i)
-#pragma unroll
-      for (int j = 0; j < kTN; ++j) asm volatile("" : "+v"(acc[i][j]));  // stays ahead of the stores' branches
   }
 };
-
-template <int BM, int BN, int WM, int WN, class T>
-__global__ __launch_bounds__(64 * WM *WN) void k_mx_product(MxMatrix a, MxMatrix b, Blocks blocks, T *out, int64_t ld, bool vec) {
-  using B = MxBlock<BM, BN, WM, WN>;
-  __shared__ __attribute__((aligned(1024))) char lds[B::kLds];
-  int r, c, split;
-  blocks.locate(blockIdx.x, gridDim.x, r, c, split);
-  const int64_t row = (int64_t)r * BM, col = (int64_t)c * BN;
-  B block;
-  block.run(a, b, row, col, lds);
-  const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
-#pragma unroll
-  for (int i = 0; i < B::kTM; ++i) {
-    const int64_t m = row + B::Base::row0() + 16 * i + i16;
-    if (m >= a.rows) continue;
-#pragma unroll
-    for (int j = 0; j < B::kTN; ++j) {
-      const int64_t n = col + B::Base::col0() + 16 * j + 4 * j4;
-      if (n >= b.rows) continue;
-      store4(out + m * ld + n, block.acc[i][j], (int)(b.rows - n < 4 ? b.rows - n : 4), vec);
-    }
-  }
-}
-
-template <int BM, int BN, int WM, int WN, class T>
-sdnn_status launch_product(const MxMatrix &a, const MxMatrix &b, T *out, int64_t ld, hipStream_t stream) {
-  Blocks blocks{};
-  const int64_t r = ceil_div(a.rows, BM), c = ceil_div(b.rows, BN);
-  if (r * c * 64 * WM * WN > 0xffffffffll) return fail(SDNN_EINVAL, "%lld x %lld outputs are too many for one launch", (long long)a.rows, (long long)b.rows);
-  blocks.rows = (int)r;
-  blocks.cols = (int)c;
-  blocks.splits = 1;
-  const bool vec = (uintptr_t)out % (4 * sizeof(T)) == 0 && ld % 4 == 0;
-  hipLaunchKernelGGL((k_mx_product<BM, BN, WM, WN, T>), dim3((unsigned)(r * c)), dim3(64 * WM * WN), 0, stream, a, b, blocks, out, ld, vec);
-  return launched("product");
-}
 
 template <class T>
-sdnn_status product(const MxMatrix &a, const MxMatrix &b, T *out, int64_t ld, hipStream_t stream) {
-  const Plan p = plan(a.rows, b.rows, ceil_div(a.blocks, 8), 1);
-  switch (p.shape) {
-    case kWide: return launch_product<256, 256, 2, 4>(a, b, out, ld, stream);
-    case kMiddle: return launch_product<128, 128, 2, 2>(a, b, out, ld, stream);
-    case kSmall: return launch_product<64, 64, 2, 2>(a, b, out, ld, stream);
-    case kFlat: return launch_product<32, 128, 1, 4>(a, b, out, ld, stream);
-    default: return launch_product<128, 32, 4, 1>(a, b, out, ld, stream);
-  }
+sdnn_status product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales, int64_t rows, int64_t outputs, int64_t n, T *out, int64_t ld, hipStream_t stream) {
+  const int64_t pitch = blocks_of(n) * 16;
+  const Matrix a{(const char *)x_codes, pitch, rows, pitch, 0, x_scales}, b{(const char *)w_codes, pitch, outputs, pitch, 0, w_scales};
+  const Store<T> e{out, ld, rows, outputs, (uintptr_t)out % (4 * sizeof(T)) == 0 && ld % 4 == 0};
+  return run_shape<KIND_MX, false, false>(plan(rows, outputs, ceil_div(n, 256), 1), a, b, rows, outputs, n, e, stream, "product");
 }
 
 unsigned grid_of(int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), kCus * 32)); }
@@ -309,9 +201,8 @@ sdnn_status sdnn_mx_product(const uint8_t *x_codes, const uint8_t *x_scales, con
   if ((st = check_mx("w", w_codes, w_scales)) != SDNN_OK) return st;
   if ((st = check_matrix("out", out, ldo, n_outputs, dtype)) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const int64_t blocks = blocks_of(n_values);
-  const MxMatrix a{(const char *)x_codes, x_scales, n_rows, blocks}, b{(const char *)w_codes, w_scales, n_outputs, blocks};
-  return dtype == SDNN_BF16 ? product(a, b, (__bf16 *)out, ldo, stream) : product(a, b, (float *)out, ldo, stream);
+  return dtype == SDNN_BF16 ? product(x_codes, x_scales, w_codes, w_scales, n_rows, n_outputs, n_values, (__bf16 *)out, ldo, stream)
+                            : product(x_codes, x_scales, w_codes, w_scales, n_rows, n_outputs, n_values, (float *)out, ldo, stream);
 }
 
 size_t sdnn_mx_linear_workspace_bytes(int64_t n_rows, int64_t n_values) {

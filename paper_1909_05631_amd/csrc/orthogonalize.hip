@@ -20,7 +20,7 @@ using tile::KIND_SPLIT;
 namespace {
 
 constexpr int kMaxSteps = 32;
-constexpr int kNormBlocks = 128;  // partial sums of squares per matrix
+constexpr int kNormBlocks = 1024;  // partial sums of squares per matrix
 
 // log2 of a step's bounds of the singular values of X, and what the norm makes of the second.
 struct Bound {
@@ -49,29 +49,42 @@ struct Source {
   int64_t ld, batch, rows, cols;
 };
 
+// The sum over a workgroup of 256, in one order.
+__device__ __forceinline__ double sum_of_workgroup(double s, double (&part)[4]) {
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  return part[0] + part[1] + part[2] + part[3];
+}
+
 // Sums of squares in fp64, one per workgroup.
 template <class T>
 __global__ __launch_bounds__(256) void k_squares(Source<T> g, double *parts) {
   __shared__ double part[4];
   const T *m = g.data + blockIdx.y * g.batch;
   double s = 0.0;
-  for (int64_t r = blockIdx.x; r < g.rows; r += gridDim.x)
+  for (int64_t r = blockIdx.x; r < g.rows; r += gridDim.x) {
+#pragma unroll 4
     for (int64_t c = threadIdx.x; c < g.cols; c += 256) {
       const double v = load_as_float(m + r * g.ld + c);
-      s += v * v;
+      s = fma(v, v, s);
     }
-  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) parts[blockIdx.y * kNormBlocks + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
+  }
+  s = sum_of_workgroup(s, part);
+  if (threadIdx.x == 0) parts[blockIdx.y * kNormBlocks + blockIdx.x] = s;
+}
+
+__device__ __forceinline__ double sum_of_parts(const double *parts, int count, double (&part)[4]) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < count; i += 256) s += parts[blockIdx.y * kNormBlocks + i];
+  return sum_of_workgroup(s, part);
 }
 
 // The start: X_0 in two parts, and the norm's part of the bounds.
 template <class T>
 __global__ __launch_bounds__(256) void k_start(Source<T> g, const double *parts, int count, double eps, Bound bound, Info *info, char *x, int64_t pitch) {
-  double s = 0.0;
-  for (int i = 0; i < count; ++i) s += parts[blockIdx.y * kNormBlocks + i];
-  const double norm = sqrt(s), inverse = 1.0 / (norm + eps);
+  __shared__ double part[4];
+  const double norm = sqrt(sum_of_parts(parts, count, part)), inverse = 1.0 / (norm + eps);
   const float log2_f = (float)log2(norm * inverse);
   if (blockIdx.x == 0 && threadIdx.x == 0) info[blockIdx.y].log2_f = log2_f;
   const int e = x_exponent(fminf(bound.u, log2_f + bound.l));
@@ -188,9 +201,8 @@ struct Update {
 // No step: the start itself.
 template <class T>
 __global__ __launch_bounds__(256) void k_scale(Source<T> g, const double *parts, int count, double eps, T *out, int64_t ld, int64_t batch) {
-  double s = 0.0;
-  for (int i = 0; i < count; ++i) s += parts[blockIdx.y * kNormBlocks + i];
-  const double inverse = 1.0 / (sqrt(s) + eps);
+  __shared__ double part[4];
+  const double inverse = 1.0 / (sqrt(sum_of_parts(parts, count, part)) + eps);
   for (int64_t r = blockIdx.x; r < g.rows; r += gridDim.x)
     for (int64_t c = threadIdx.x; c < g.cols; c += 256)
       out[blockIdx.y * batch + r * ld + c] = (T)(float)(load_as_float(g.data + blockIdx.y * g.batch + r * g.ld + c) * inverse);
@@ -240,7 +252,7 @@ sdnn_status orthogonalize(const T *g, int64_t ldg, int64_t batch_g, T *out, int6
   Carver carver{(char *)workspace};
   const Space sp(carver, batch, rows, cols);
   const Source<T> src{g, ldg, batch_g, rows, cols};
-  const unsigned norm_blocks = (unsigned)std::min<int64_t>(rows, kNormBlocks), row_blocks = (unsigned)std::min<int64_t>(rows, 8192);
+  const unsigned norm_blocks = (unsigned)std::min<int64_t>(rows, kNormBlocks), row_blocks = (unsigned)std::min<int64_t>(rows, 2048);
   hipLaunchKernelGGL((k_squares<T>), dim3(norm_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts);
   if (steps == 0) {
     hipLaunchKernelGGL((k_scale<T>), dim3(row_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts, (int)norm_blocks, (double)eps, out, ldo, batch_o);
@@ -259,9 +271,9 @@ sdnn_status orthogonalize(const T *g, int64_t ldg, int64_t batch_g, T *out, int6
   hipLaunchKernelGGL((k_start<T>), dim3(row_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts, (int)norm_blocks, (double)eps, bounds[0], sp.info, sp.x[0], pitch);
   sdnn_status st = launched("orthogonalize");
   const bool tall = rows > cols;
-  const Plan gram = plan(m, m, ceil_div(std::max(rows, cols), 32), 1, batch, true);
-  const Plan power = plan(m, m, ceil_div(m, 32), 1, batch, true);
-  const Plan update = plan(rows, cols, ceil_div(m, 32), 1, batch);
+  const Plan gram = plan(m, m, ceil_div(std::max(rows, cols), 32), 1, tall ? kAnyForm : kAlong, batch, true);
+  const Plan power = plan(m, m, ceil_div(m, 32), 1, kAlong, batch, true);
+  const Plan update = plan(rows, cols, ceil_div(m, 32), 1, tall ? kAlong : kAnyForm, batch);
   for (int k = 0; k < steps && st == SDNN_OK; ++k) {
     const char *x = sp.x[k & 1];
     char *next = k + 1 < steps ? sp.x[(k + 1) & 1] : nullptr;

@@ -27,6 +27,7 @@ namespace {
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kTopBlocks = 512;
 constexpr int kGradExponent = 15;  // fp16 parts of exp(l - lse) - [v = y] hold it times 2^15
 
 // exp, by the hardware's exponential of base 2 (one rounding of the argument, which is at most 0 in the sums: the
@@ -39,11 +40,11 @@ __device__ __forceinline__ bool counted(const int64_t *labels, int64_t t, int64_
 
 // What the kernels of one call hand on in device memory.
 struct Scalars {
-  uint32_t top[3];  // bits of the largest finite magnitude of x (counted rows), of w, of x times its rows' weights
-  float mean;       // 1 / (number of counted rows), at most 1
+  float top[3][kTopBlocks];  // largest finite magnitudes of x (counted rows), of w, of x times its rows' weights, by workgroup
+  float mean;                // 1 / (number of counted rows), at most 1
 };
 
-// One workgroup: the number of counted rows; clears the maxima.
+// One workgroup: the number of counted rows.
 __global__ __launch_bounds__(1024) void k_count(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) {
   __shared__ int part[16];
   int n = 0;
@@ -55,7 +56,6 @@ __global__ __launch_bounds__(1024) void k_count(const int64_t *labels, int64_t r
     n = 0;
     for (int i = 0; i < 16; ++i) n += part[i];
     out->mean = 1.0f / (float)(n > 1 ? n : 1);
-    out->top[0] = out->top[1] = out->top[2] = 0;
   }
 }
 
@@ -64,25 +64,44 @@ __device__ __forceinline__ float finite_magnitude(float v) {
   return a < __builtin_inff() ? a : 0.0f;  // false for NaN too
 }
 
-// Largest finite magnitude of a matrix, of its rows times their weights if there are any (a maximum: its order does
-// not matter). Rows without a label are skipped.
-__global__ __launch_bounds__(256) void k_top(const float *x, int64_t ld, int64_t rows, int64_t cols, const int64_t *labels, int64_t classes, const float *weights, uint32_t *top) {
+__device__ __forceinline__ float max_of_workgroup(float m, float (&part)[4]) {
+  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+  __syncthreads();
+  return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+
+// Largest finite magnitudes of a matrix, of its rows times their weights if there are any: one per workgroup. Rows without a label are skipped.
+__global__ __launch_bounds__(256) void k_top(const float *x, int64_t ld, int64_t rows, int64_t cols, const int64_t *labels, int64_t classes, const float *weights, float *top) {
+  __shared__ float part[4];
   float m = 0.0f;
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     if (labels && !counted(labels, r, classes)) continue;
     const float w = weights ? weights[r] : 1.0f;
+#pragma unroll 4
     for (int64_t c = threadIdx.x; c < cols; c += 256) m = fmaxf(m, finite_magnitude(x[r * ld + c] * w));
   }
+  m = max_of_workgroup(m, part);
+  if (threadIdx.x == 0) top[blockIdx.x] = m;
+}
+
+// What k_top found, by one wave (all of its lanes get it).
+__device__ __forceinline__ float top_of(const float *top) {
+  float m = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kTopBlocks / 64; ++i) m = fmaxf(m, top[i * 64 + (threadIdx.x & 63)]);
   for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if ((threadIdx.x & 63) == 0 && m > 0.0f) atomicMax(top, __float_as_uint(m));
+  return m;
 }
 
 // fp32 rows in the split form, 32 * groups values each, zeros past `cols`. A row's exponent: from its own largest
 // magnitude (exponents != nullptr, where it is written), or from the whole matrix's (top). weights: the values are
 // multiplied by their row's weight first. Rows without a label become zeros.
 __global__ __launch_bounds__(256) void k_split_rows(const float *x, int64_t ld, int64_t rows, int64_t cols, int64_t groups, const int64_t *labels, int64_t classes, const float *weights,
-                                                    const uint32_t *top, int *exponents, char *out) {
+                                                    const float *top, int *exponents, char *out) {
   __shared__ float part[4];
+  const int whole = exponents ? 0 : split_exponent(top_of(top));
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const float *row = x + r * ld;
     const bool live = !labels || counted(labels, r, classes);
@@ -92,14 +111,10 @@ __global__ __launch_bounds__(256) void k_split_rows(const float *x, int64_t ld, 
       float m = 0.0f;
       if (live)
         for (int64_t c = threadIdx.x; c < cols; c += 256) m = fmaxf(m, finite_magnitude(row[c]));
-      for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-      __syncthreads();
-      e = split_exponent(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
+      e = split_exponent(max_of_workgroup(m, part));
       if (threadIdx.x == 0) exponents[r] = e;
     } else {
-      e = split_exponent(__uint_as_float(*top));
+      e = whole;
     }
     char *to = out + r * groups * 128;
     for (int64_t k = threadIdx.x * 4; k < groups * 32; k += 1024) {
@@ -137,12 +152,12 @@ __global__ __launch_bounds__(256) void k_copy_rows(const __bf16 *x, int64_t ld, 
 // What turns a block's sums into logits: the operands' powers of two.
 struct LogitScale {
   const int *row, *col;            // exponents by row and column (split, loss)
-  const uint32_t *top_x, *top_w;   // or of the whole matrices (split, gradient)
+  const float *top_x, *top_w;      // or of the whole matrices (split, gradient)
 };
 template <int KIND>
 __device__ __forceinline__ int whole_exponent(const LogitScale &s) {
   if (KIND == KIND_BF16 || s.row) return 0;
-  return split_exponent(__uint_as_float(*s.top_x)) + split_exponent(__uint_as_float(*s.top_w));
+  return split_exponent(top_of(s.top_x)) + split_exponent(top_of(s.top_w));
 }
 
 // Loss: per row and the wave's columns, the largest logit and the sum of exponentials against it.
@@ -260,21 +275,24 @@ struct WriteGrad {
   }
 };
 
-// What a product's sums are multiplied by: row weights, the mean, the split operands' powers of two.
+// What a product's sums are multiplied by: the mean and the split operands' powers of two (found once a wave), and
+// the row's weight. A sum of zero stays zero whatever the weight: rows without a label.
 struct OutScale {
   const float *rows;
   const float *mean;
-  const uint32_t *top;  // of the operand that was split (nullptr: none)
-  __device__ __forceinline__ float of(int64_t row, float v) const {
-    if (top) v = ldexpf(v, -kGradExponent - split_exponent(__uint_as_float(*top)));
-    if (mean) v *= *mean;
+  const float *top;  // of the operand that was split (nullptr: none)
+  struct Found {
+    float mean;
+    int e;
+  };
+  __device__ __forceinline__ Found find() const { return {mean ? *mean : 1.0f, top ? -kGradExponent - split_exponent(top_of(top)) : 0}; }
+  __device__ __forceinline__ float weight(int64_t row) const { return rows ? rows[row] : 1.0f; }
+  __device__ __forceinline__ f32x4 apply(Found f, float weight, f32x4 v) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = v[k] == 0.0f ? 0.0f : ldexpf(v[k], f.e) * f.mean * weight;
     return v;
   }
 };
-
-// dx's rows: weights apply only where the row has a label (its sums are zero otherwise).
-__device__ __forceinline__ float row_weight(const OutScale &s, int64_t row) { return s.rows ? s.rows[row] : 1.0f; }
-__device__ __forceinline__ float scaled(const OutScale &s, float w, float v, int64_t row) { return v == 0.0f ? 0.0f : s.of(row, v) * w; }
 
 template <class T>
 struct Store {
@@ -285,19 +303,17 @@ struct Store {
   template <class B>
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
+    const OutScale::Found found = scale.find();
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t r = row0 + 16 * i + i16;
       if (r >= rows) continue;
-      const float w = row_weight(scale, r);
+      const float w = scale.weight(r);
 #pragma unroll
       for (int j = 0; j < B::kTN; ++j) {
         const int64_t c = col0 + 16 * j + 4 * j4;
         if (c >= cols) continue;
-        f32x4 v = block.acc[i][j];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = scaled(scale, w, v[k], r);
-        store4(out + r * ld + c, v, (int)(cols - c < 4 ? cols - c : 4), vec);
+        store4(out + r * ld + c, scale.apply(found, w, block.acc[i][j]), (int)(cols - c < 4 ? cols - c : 4), vec);
       }
     }
   }
@@ -331,22 +347,20 @@ struct Accumulate {
 template <class T>
 __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int splits, int64_t ld_slab, Store<T> to) {
   const int64_t per = ld_slab / 4;
+  const OutScale::Found found = to.scale.find();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < to.rows * per; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / per, c = (i - r * per) * 4;
     if (c >= to.cols) continue;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(slabs + (s * to.rows + r) * ld_slab + c);
-    const float w = row_weight(to.scale, r);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = scaled(to.scale, w, v[k], r);
-    store4(to.out + r * to.ld + c, v, (int)(to.cols - c < 4 ? to.cols - c : 4), to.vec);
+    store4(to.out + r * to.ld + c, to.scale.apply(found, to.scale.weight(r), v), (int)(to.cols - c < 4 ? to.cols - c : 4), to.vec);
   }
 }
 
 // ------------------------------------------------------------------------------------------------
 // Host
 
-constexpr int kWaveCols[kShapes] = {64, 64, 32, 32, 32};  // columns of a wave: the parts of a row of logits
+constexpr int kWaveCols[kShapes] = {64, 48, 64, 32, 32, 32};  // columns of a wave: the parts of a row of logits
 
 // Sizes of one call.
 struct Sizes {
@@ -363,8 +377,8 @@ struct Sizes {
     return std::min(p, classes);
   }
   int64_t g_pitch() const { return ceil_div(piece(), per_slab()) * 128; }
-  Plan loss() const { return plan(rows, classes, feature_slabs(), 1); }
-  Plan logits(int64_t n) const { return plan(rows, n, feature_slabs(), 1); }
+  Plan loss() const { return plan(rows, classes, feature_slabs(), 1, kAlong); }
+  Plan logits(int64_t n) const { return plan(rows, n, feature_slabs(), 1, kAlong); }
   Plan dx() const { return plan(rows, features, ceil_div(piece(), per_slab()), kMaxSplits); }
   Plan dw(int64_t n) const { return plan(n, features, ceil_div(rows, per_slab()), kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
@@ -411,11 +425,11 @@ struct GradSpace {
   }
 };
 
-unsigned row_grid(int64_t rows) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(rows, 8192)); }
+unsigned row_grid(int64_t rows) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(rows, 2048)); }
 
 // A matrix as an operand: in place, or copied into `space` first.
 template <int KIND>
-Matrix operand(const void *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, const uint32_t *top, int *exponents, const float *weights, char *space, hipStream_t stream) {
+Matrix operand(const void *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, const float *top, int *exponents, const float *weights, char *space, hipStream_t stream) {
   if constexpr (KIND == KIND_BF16) {
     if (!labels && usable_in_place(data, ld, s.features)) return {(const char *)data, ld * 2, rows, s.features * 2, 0};
     const bool vec = ((uintptr_t)data & 15) == 0 && ld % 8 == 0;
@@ -477,20 +491,20 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     return launched("gradient");
   }
   hipLaunchKernelGGL(k_count, dim3(1), dim3(1024), 0, stream, labels, s.rows, s.classes, sp.scalars);
-  uint32_t *top_x = nullptr, *top_w = nullptr;
+  float *top_x = nullptr, *top_w = nullptr;
   if constexpr (KIND == KIND_SPLIT) {
-    top_x = &sp.scalars->top[0];
-    top_w = &sp.scalars->top[1];
-    hipLaunchKernelGGL(k_top, dim3(std::min(row_grid(s.rows), 1024u)), dim3(256), 0, stream, x, ldx, s.rows, s.features, labels, s.classes, (const float *)nullptr, top_x);
-    hipLaunchKernelGGL(k_top, dim3(std::min(row_grid(s.classes), 1024u)), dim3(256), 0, stream, w, ldw, s.classes, s.features, (const int64_t *)nullptr, s.classes, (const float *)nullptr, top_w);
+    top_x = sp.scalars->top[0];
+    top_w = sp.scalars->top[1];
+    hipLaunchKernelGGL(k_top, dim3(kTopBlocks), dim3(256), 0, stream, x, ldx, s.rows, s.features, labels, s.classes, (const float *)nullptr, top_x);
+    hipLaunchKernelGGL(k_top, dim3(kTopBlocks), dim3(256), 0, stream, w, ldw, s.classes, s.features, (const int64_t *)nullptr, s.classes, (const float *)nullptr, top_w);
   }
   const Matrix a = operand<KIND>(x, ldx, s.rows, s, labels, top_x, nullptr, nullptr, sp.x, stream);
   const Matrix b = operand<KIND>(w, ldw, s.classes, s, nullptr, top_w, nullptr, nullptr, sp.w, stream);
   Matrix ag = a;  // dw's other operand: the rows, in fp32 times their weights (in bf16 G holds the weights)
-  const uint32_t *top_g = top_x;
+  const float *top_g = top_x;
   if (KIND == KIND_SPLIT && weights && dw) {
-    uint32_t *top = &sp.scalars->top[2];
-    hipLaunchKernelGGL(k_top, dim3(std::min(row_grid(s.rows), 1024u)), dim3(256), 0, stream, (const float *)x, ldx, s.rows, s.features, labels, s.classes, weights, top);
+    float *top = sp.scalars->top[2];
+    hipLaunchKernelGGL(k_top, dim3(kTopBlocks), dim3(256), 0, stream, (const float *)x, ldx, s.rows, s.features, labels, s.classes, weights, top);
     ag = operand<KIND>(x, ldx, s.rows, s, labels, top, nullptr, weights, sp.xg, stream);
     top_g = top;
   }

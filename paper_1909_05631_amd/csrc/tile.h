@@ -34,7 +34,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kSlab = 128;             // bytes of k per row and slab
 constexpr uint32_t kOut = 0x7fffff00;  // an offset past every operand: reads zeros
@@ -42,12 +42,12 @@ constexpr uint32_t kOut = 0x7fffff00;  // an offset past every operand: reads ze
 // One operand of a block. along: `base` is the block's first row, `rows` its rows inside the operand,
 // `extent` the bytes of k. across: `base` is the block's first column, `rows` the rows of k, `extent` the
 // bytes of columns inside the operand. `pitch`: bytes from row to row; 16-byte aligned, as is base.
-// (rows of a slab) * pitch stays under 2^31 (checked on the host).
+// 256 pitches stay under 2^31 (checked on the host).
+// KIND_MX: `scales` is the first row's scale bytes, pitch / 16 of them a row.
 struct Operand {
   const char *base;
-  int64_t pitch;
-  int64_t rows;
-  int64_t extent;
+  int pitch, rows, extent;
+  const char *scales = nullptr;
 };
 
 // Values per slab, bytes per value of an across operand.
@@ -56,6 +56,30 @@ struct Geometry {
   static constexpr int kPerSlab = KIND == KIND_BF16 ? 64 : KIND == KIND_SPLIT ? 32 : 256;
   static constexpr int kBytes = KIND == KIND_BF16 ? 2 : 4;
 };
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// 16 bytes a lane from a buffer to LDS at `lds` + 16 * lane. Written out so that the compiler does not wait for it at
+// the next LDS read: Block counts these loads itself. It has no output register; its data goes to LDS alone.
+__device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, int base, int lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(base) : "memory");
+}
+
+// The same of 4 bytes a lane.
+__device__ __forceinline__ void load_word_to_lds(i32x4 buffer, uint32_t offset, int base, int lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(base) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "the counter's width");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Every wave's LDS reads are done and its counted loads have arrived: from here on the others see them.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 
 // Moves slab `s` of one operand to LDS. ROWS: the block's rows (along) or columns (across) of this operand.
 template <int KIND, int ROWS, bool ACROSS, int THREADS>
@@ -66,9 +90,8 @@ struct Loader {
   static constexpr int kRowBytes = ACROSS ? ROWS * Geometry<KIND>::kBytes : kSlab;  // a row in LDS
   static constexpr int kRowsPerRound = kRound / kRowBytes;
   static constexpr int kSlabRows = kBytes / kRowBytes;
-  static_assert(kBytes % kRound == 0 || kRounds == 1, "whole rounds");
-  static_assert(kRowBytes <= kRound || ACROSS, "a round holds whole rows");
-  static_assert(!ACROSS || (kRound % kRowBytes == 0 && kRowsPerRound % 4 == 0) || kRounds == 1, "the permutation repeats every round");
+  static_assert(kBytes % kRound == 0, "whole rounds");
+  static_assert(kRound % kRowBytes == 0 && kRowsPerRound % (ACROSS ? 4 : 8) == 0, "the permutation repeats every round");
 
   static constexpr int kTurn = (kRowBytes / 16 - 1) & 6;  // chunk bits that an across row's number permutes
 
@@ -81,35 +104,65 @@ struct Loader {
     row = t / (kRowBytes / 16);
     const int c = t % (kRowBytes / 16);
     chunk = ACROSS ? c ^ ((row << 1) & kTurn) : c ^ (row & 7);
-    offset = (uint32_t)(row * op.pitch) + chunk * 16;
+    offset = row * op.pitch + chunk * 16;
     if (ACROSS && chunk * 16 >= op.extent) offset = kOut;
   }
 
-  __device__ __forceinline__ void load(const Operand &op, int64_t s, char *lds) const {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const char *origin;
-    uint32_t size, off = offset;
+  // A slab's loads, issued one at a time. Past the operand's k they read zeros: every slab has kRounds of them, which the
+  // waits count on.
+  struct Slab {
+    i32x4 buffer;
+    uint32_t off;
+    int step, lds;
+    __device__ __forceinline__ void issue(int i) const { load_to_lds(buffer, off, i * step, lds + i * kRound); }
+  };
+  __device__ __forceinline__ Slab slab(const Operand &op, int s, int lds) const {
+    uint32_t off = offset;
+    int wide, rows;
+    uint64_t origin = (uint64_t)op.base;
     if (ACROSS) {
-      const int64_t left = op.rows - s * kSlabRows;
-      const int n = left < kSlabRows ? (int)left : kSlabRows;
-      const int wide = op.extent < kRowBytes ? (int)op.extent : kRowBytes;
-      origin = op.base + s * kSlabRows * op.pitch;
-      size = n > 0 ? (uint32_t)((n - 1) * op.pitch) + wide : 0;
+      wide = min(op.extent, kRowBytes);
+      rows = min(op.rows - s * kSlabRows, kSlabRows);
+      origin += (uint64_t)(uint32_t)s * (uint32_t)(kSlabRows * op.pitch);
     } else {
-      const int64_t left = op.extent - s * kSlab;
-      const int wide = left < kSlab ? (int)left : kSlab;
-      const int n = op.rows < ROWS ? (int)op.rows : ROWS;
-      origin = op.base + s * kSlab;
-      size = n > 0 && wide > 0 ? (uint32_t)((n - 1) * op.pitch) + wide : 0;
+      wide = min(op.extent - s * kSlab, kSlab);
+      rows = wide > 0 ? min(op.rows, ROWS) : 0;
+      origin += (uint64_t)(uint32_t)s * kSlab;
       if (chunk * 16 >= wide) off = kOut;
     }
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)origin, 0, size, 0x00027000);
-    const int step = (int)(kRowsPerRound * op.pitch);
+    const int size = max(rows, 0) * op.pitch - op.pitch + wide;
+    return {{uniform((int)origin), uniform((int)(origin >> 32)), uniform(rows > 0 ? size : 0), 0x00027000}, off, kRowsPerRound * op.pitch, lds};
+  }
+  __device__ __forceinline__ void load(const Operand &op, int s, int lds) const {
+    const Slab part = slab(op, s, lds);
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
-      if (kBytes < kRound && wave * 1024 >= kBytes) break;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(lds + i * kRound + wave * 1024), 16, off, i * step, 0, 0);
-    }
+    for (int i = 0; i < kRounds; ++i) part.issue(i);
+  }
+};
+
+// The same for the scale bytes of KIND_MX: 8 a row and slab. Lanes past the rows read zeros into padding.
+template <int ROWS, int THREADS>
+struct ScaleLoader {
+  static constexpr int kRound = THREADS * 4;
+  static constexpr int kRounds = (ROWS * 8 + kRound - 1) / kRound;
+  static constexpr int kBytes = kRounds * kRound;
+  static constexpr int kRowsPerRound = kRound / 8;
+  uint32_t offset;
+  int half;  // of the slab's 8 bytes
+
+  __device__ __forceinline__ void init(const Operand &op) {
+    const int row = threadIdx.x >> 1;
+    half = threadIdx.x & 1;
+    offset = row < ROWS ? row * (op.pitch / 16) + half * 4 : kOut;
+  }
+  __device__ __forceinline__ void load(const Operand &op, int s, int lds) const {
+    const int wide = min(op.extent / 16 - s * 8, 8), pitch = op.pitch / 16, rows = wide > 0 ? min(op.rows, ROWS) : 0;
+    const uint64_t origin = (uint64_t)op.scales + (uint64_t)(uint32_t)s * 8;
+    const i32x4 r = {uniform((int)origin), uniform((int)(origin >> 32)), uniform(rows > 0 ? (rows - 1) * pitch + wide : 0), 0x00027000};
+    const uint32_t off = half * 4 < wide ? offset : kOut;
+    // a wave's 256 bytes follow the wave before it, as its 1024 bytes of values do
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) load_word_to_lds(r, off, i * kRowsPerRound * pitch, lds + i * kRound);
   }
 };
 
@@ -175,6 +228,13 @@ struct Reader {
   }
 };
 
+// 4-bit floats (format 4, which fill half of the operand's registers), scale byte Q of the lanes' words.
+template <int Q>
+__device__ __forceinline__ f32x4 mfma_mx(i32x4 a, i32x4 b, f32x4 c, int scale_a, int scale_b) {
+  const i32x8 wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, Q, scale_a, Q, scale_b);
+}
+
 template <int KIND>
 __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
   if constexpr (KIND == KIND_BF16)
@@ -185,27 +245,91 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 
 // The product of one block. WM x WN waves share it, each BM / WM x BN / WN outputs in subtiles of 16 x 16.
 // acc[i][j]: rows 16 i + lane % 16 of the wave's part, columns 16 j + 4 (lane / 16) + 0..3.
-template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B>
+//
+// STAGES buffers in LDS. A slab is multiplied in passes: its two halves (bf16, 4-bit), or high*high, high*low, low*high
+// (KIND_SPLIT). A pass goes down the subtiles of A, and each one's registers take the next pass's fragment as soon as
+// its products are issued, so that LDS reads run between products and one set of A fragments is enough. A little
+// into a slab's last pass, when its last fragments have been read, the waves meet, and the slab's buffer takes
+// slab s + STAGES: its loads have a slab's time.
+//
+// 256 x 256 by 8 waves of 128 x 64: two waves a SIMD cover each other's waits, and 208 of 256 registers hold sums and
+// fragments. Measured on 8192^3: bf16 1300 TFLOP/s at 66% of the cycles in matrix instructions (the card lowers its
+// clock to 1.9 GHz under them; at 1570 for the library's kernel in the same run), KIND_SPLIT 1430, 477 of fp32.
+// Four waves of 128 x 128 read less LDS and measured 1010, raised wave priorities during the products 7% less.
+template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, int STAGES>
 struct Block {
   static constexpr int kThreads = 64 * WM * WN;
   static constexpr int kTM = BM / WM / 16, kTN = BN / WN / 16;
-  static constexpr int kStage = (BM + BN) * kSlab;
-  static constexpr int kLds = 2 * kStage;
   using LoadA = Loader<KIND, BM, ACROSS_A, kThreads>;
   using LoadB = Loader<KIND, BN, ACROSS_B, kThreads>;
+  using ScaleA = ScaleLoader<BM, kThreads>;
+  using ScaleB = ScaleLoader<BN, kThreads>;
+  static constexpr bool kMx = KIND == KIND_MX;
+  static constexpr int kValues = (BM + BN) * kSlab;
+  static constexpr int kStage = kValues + (kMx ? ScaleA::kBytes + ScaleB::kBytes : 0);
+  static constexpr int kLds = STAGES * kStage;
+  static_assert(kLds <= 160 * 1024, "LDS of a CU");
+  static constexpr int kLoads = LoadA::kRounds + LoadB::kRounds + (kMx ? ScaleA::kRounds + ScaleB::kRounds : 0);  // of a wave and slab
 
   f32x4 acc[kTM][kTN];
 
-  __device__ __forceinline__ static int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+  __device__ __forceinline__ static int wave() { return uniform(threadIdx.x >> 6); }
   __device__ __forceinline__ static int row0() { return (wave() / WN) * (BM / WM); }
   __device__ __forceinline__ static int col0() { return (wave() % WN) * (BN / WN); }
 
+  template <class R>
+  __device__ __forceinline__ static void read(const R &r, const char *lds, int q, i32x4 (&f)[kTN]) {
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) f[j] = r.read(lds, j, q);
+  }
+  // A subtile's scale bytes: the two of a lane's blocks.
+  __device__ __forceinline__ static int read_scale(const char *lds, int first, int i) {
+    const int lane = threadIdx.x & 63;
+    return *(const uint16_t *)(lds + (first + 16 * i + (lane & 15)) * 8 + 2 * (lane >> 4));
+  }
+  template <int Q>
+  __device__ __forceinline__ void multiply(int i, i32x4 a, const i32x4 (&b)[kTN], int scale, const int (&scales)[kTN]) {
+#pragma unroll
+    for (int j = 0; j < kTN; ++j)
+      if constexpr (kMx)
+        acc[i][j] = mfma_mx<Q>(b[j], a, acc[i][j], scales[j], scale);
+      else
+        acc[i][j] = mfma<KIND>(b[j], a, acc[i][j]);
+  }
+  // Nothing of the operand past slab s1.
+  __device__ __forceinline__ static void clip(Operand &op, bool across, int slab_rows, int s1) {
+    int &k = across ? op.rows : op.extent;
+    const int64_t end = (int64_t)s1 * (across ? slab_rows : kSlab);
+    if (end < k) k = (int)end;
+    op.pitch = uniform(op.pitch);
+    op.rows = uniform(op.rows);
+    op.extent = uniform(op.extent);
+  }
+
+  // The order that the scheduler is to keep: products and LDS reads as they are written.
+  template <int SUBTILES>
+  __device__ __forceinline__ static void products() {
+    if constexpr (SUBTILES > 0) __builtin_amdgcn_sched_group_barrier(0x008, SUBTILES * kTN, 0);
+  }
+  template <int READS>
+  __device__ __forceinline__ static void reads() {
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+
   // Slabs [s0, s1) of the operands.
-  __device__ __forceinline__ void run(const Operand &a, const Operand &b, int64_t s0, int64_t s1, char *lds) {
+  __device__ __forceinline__ void run(Operand a, Operand b, int s0, int s1, char *lds) {
+    clip(a, ACROSS_A, LoadA::kSlabRows, s1);
+    clip(b, ACROSS_B, LoadB::kSlabRows, s1);
     LoadA la;
     LoadB lb;
+    ScaleA lsa;
+    ScaleB lsb;
     la.init(a);
     lb.init(b);
+    if constexpr (kMx) {
+      lsa.init(a);
+      lsb.init(b);
+    }
     Reader<KIND, BM, ACROSS_A> ra;
     Reader<KIND, BN, ACROSS_B> rb;
     ra.init(row0());
@@ -214,63 +338,113 @@ struct Block {
     for (int i = 0; i < kTM; ++i)
 #pragma unroll
       for (int j = 0; j < kTN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (s0 < s1) {
-      la.load(a, s0, lds);
-      lb.load(b, s0, lds + BM * kSlab);
-    }
-    for (int64_t s = s0; s < s1; ++s) {
-      char *now = lds + ((s - s0) & 1) * kStage, *next = lds + ((s - s0 + 1) & 1) * kStage;
-      // slab s has arrived, and every wave is done with the buffer that slab s + 1 goes to
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      step(ra, rb, now);
-      if (s + 1 < s1) {
-        la.load(a, s + 1, next);
-        lb.load(b, s + 1, next + BM * kSlab);
+    if (s0 >= s1) return;
+    const int base = uniform((int)(uintptr_t)(lds_char *)lds), mine = base + wave() * 1024;
+    const auto load_scales = [&](int s, int to) {
+      if constexpr (kMx) {
+        const int at = base + to + kValues + wave() * 256;
+        lsa.load(a, s, at);
+        lsb.load(b, s, at + ScaleA::kBytes);
       }
-      multiply();
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) {
+      load_scales(s0 + i, i * kStage);
+      la.load(a, s0 + i, mine + i * kStage);
+      lb.load(b, s0 + i, mine + i * kStage + BM * kSlab);
     }
+    wait_loads<(STAGES - 1) * kLoads>();
+    meet();
+    constexpr int kEach = kMx ? 2 : ACROSS_A ? 2 : 1;                      // LDS reads with a subtile of A
+    constexpr int kAll = kTN * (kMx ? 2 : ACROSS_B ? 2 : 1);               // with all of B
+    i32x4 fa[kTM], fb[kTN], gb[kTN];
+    int sa[kTM], sb[kTN];
+    read(rb, lds + BM * kSlab, 0, fb);
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) fa[i] = ra.read(lds, i, 0);
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) sa[i] = kMx ? read_scale(lds + kValues, row0(), i) : 0;
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) sb[j] = kMx ? read_scale(lds + kValues + ScaleA::kBytes, col0(), j) : 0;
+    int at = 0;
+    for (int s = s0; s < s1; ++s) {
+      const int used = at * kStage;
+      const char *now = lds + used;
+      at = at + 1 == STAGES ? 0 : at + 1;
+      const char *then = lds + at * kStage;
+      read(rb, now + BM * kSlab, 1, gb);
+      reads<kTN * (ACROSS_B ? 2 : 1)>();
+      if constexpr (KIND == KIND_SPLIT) {
+#pragma unroll
+        for (int i = 0; i < kTM; ++i) multiply<0>(i, fa[i], fb, 0, sb);
+        products<kTM>();
+      }
+#pragma unroll
+      for (int i = 0; i < kTM; ++i) {
+        multiply<0>(i, fa[i], KIND == KIND_SPLIT ? gb : fb, sa[i], sb);
+        fa[i] = ra.read(now, i, 1);
+        products<1>();
+        reads<ACROSS_A ? 2 : 1>();
+      }
+      constexpr int kDelay = kTM < 4 ? kTM / 2 : 2;
+#pragma unroll
+      for (int i = 0; i < kDelay; ++i) multiply<1>(i, fa[i], KIND == KIND_SPLIT ? fb : gb, sa[i], sb);
+      products<kDelay>();
+#pragma unroll
+      for (int i = 0; i < kDelay; ++i)
+#pragma unroll
+        for (int j = 0; j < kTN; ++j) asm volatile("" : "+v"(acc[i][j]));  // ahead of the meeting
+      // slab s + 1 has arrived; all fragments of slab s are in registers
+      wait_loads<(STAGES - 2) * kLoads>();
+      meet();
+      load_scales(s + STAGES, used);
+      const auto next_a = la.slab(a, s + STAGES, mine + used);
+      const auto next_b = lb.slab(b, s + STAGES, mine + used + BM * kSlab);
+      constexpr int kValueLoads = LoadA::kRounds + LoadB::kRounds;
+      int issued = 0;
+      const auto issue = [&](int until) {
+#pragma unroll
+        for (int i = 0; i < kValueLoads; ++i)
+          if (i >= issued && i < until) {
+            if (i < LoadA::kRounds)
+              next_a.issue(i);
+            else
+              next_b.issue(i - LoadA::kRounds);
+          }
+        issued = until;
+      };
+      if (kTM < 8) issue(kValueLoads);  // a small block has no time to spread them over
+      i32x4 hb[kTN];
+      int hs[kTN];
+      read(rb, then + BM * kSlab, 0, hb);
+#pragma unroll
+      for (int j = 0; j < kTN; ++j) hs[j] = kMx ? read_scale(then + kValues + ScaleA::kBytes, col0(), j) : 0;
+#pragma unroll
+      for (int i = 0; i < kDelay; ++i) {
+        fa[i] = ra.read(then, i, 0);
+        if (kMx) sa[i] = read_scale(then + kValues, row0(), i);
+      }
+      reads<kAll + kDelay * kEach>();
+#pragma unroll
+      for (int i = kDelay; i < kTM; ++i) {
+        multiply<1>(i, fa[i], KIND == KIND_SPLIT ? fb : gb, sa[i], sb);
+        fa[i] = ra.read(then, i, 0);
+        if (kMx) sa[i] = read_scale(then + kValues, row0(), i);
+        issue(kValueLoads * (i - kDelay + 1) / (kTM - kDelay));
+        products<1>();
+        reads<kEach>();
+      }
+#pragma unroll
+      for (int j = 0; j < kTN; ++j) {
+        fb[j] = hb[j];
+        sb[j] = hs[j];
+      }
+    }
+    wait_loads<0>();
 #pragma unroll
     for (int i = 0; i < kTM; ++i)
 #pragma unroll
       for (int j = 0; j < kTN; ++j) asm volatile("" : "+v"(acc[i][j]));  // stays ahead of the epilogue's branches
-  }
-
-  i32x4 fa[kTM][2], fb[kTN][2];
-
-  template <class RA, class RB>
-  __device__ __forceinline__ void step(const RA &ra, const RB &rb, const char *now) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-#pragma unroll
-      for (int j = 0; j < kTN; ++j) fb[j][q] = rb.read(now + BM * kSlab, j, q);
-#pragma unroll
-      for (int i = 0; i < kTM; ++i) fa[i][q] = ra.read(now, i, q);
-    }
-  }
-
-  __device__ __forceinline__ void multiply() {
-    if constexpr (KIND == KIND_SPLIT) {
-#pragma unroll
-      for (int i = 0; i < kTM; ++i)
-#pragma unroll
-        for (int j = 0; j < kTN; ++j) acc[i][j] = mfma<KIND>(fb[j][0], fa[i][0], acc[i][j]);
-#pragma unroll
-      for (int i = 0; i < kTM; ++i)
-#pragma unroll
-        for (int j = 0; j < kTN; ++j) acc[i][j] = mfma<KIND>(fb[j][1], fa[i][0], acc[i][j]);
-#pragma unroll
-      for (int i = 0; i < kTM; ++i)
-#pragma unroll
-        for (int j = 0; j < kTN; ++j) acc[i][j] = mfma<KIND>(fb[j][0], fa[i][1], acc[i][j]);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < kTM; ++i)
-#pragma unroll
-          for (int j = 0; j < kTN; ++j) acc[i][j] = mfma<KIND>(fb[j][q], fa[i][q], acc[i][j]);
-    }
   }
 };
 
