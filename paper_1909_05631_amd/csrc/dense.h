@@ -23,7 +23,7 @@ constexpr int kMaxSplits = 64;
 constexpr int64_t kMaxPitch = 1 << 22;  // bytes from row to row that the tiles' 32-bit offsets reach over 256 rows
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline int64_t ceil_div(int64_t x, int64_t a) { return (x + a - 1) / a; }
+__host__ __device__ inline int64_t ceil_div(int64_t x, int64_t a) { return (x + a - 1) / a; }
 
 inline bool good_dtype(int32_t d) { return d == SDNN_FP32 || d == SDNN_BF16; }
 inline int dtype_bytes(int32_t d) { return d == SDNN_BF16 ? 2 : 4; }
@@ -164,14 +164,14 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
   blocks.range(split, s0, s1);
   B block;
   block.run(a.template at<KIND, BM, ACROSS_A>(r), b.template at<KIND, BN, ACROSS_B>(c), s0, s1, lds);
-  epilogue(block, (int64_t)r * BM + B::row0(), (int64_t)c * BN + B::col0(), split, r != c);
+  if (B::holds()) epilogue(block, (int64_t)r * BM + B::row0(), (int64_t)c * BN + B::col0(), split, r != c);
 }
 
 // Launches the blocks of one shape. What the sizes need of it is the caller's rule.
-template <int KIND, int BM, int BN, int WM, int WN, int STAGES, bool ACROSS_A, bool ACROSS_B, class Epilogue>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES, int GROUPS, bool ACROSS_A, bool ACROSS_B, class Epilogue>
 sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const Epilogue &e, hipStream_t stream, const char *what, bool symmetric,
                    int batch) {
-  using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES>;
+  using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES, GROUPS>;
   Blocks blocks;
   blocks.slabs = (int)ceil_div(k, tile::Geometry<KIND>::kPerSlab);
   blocks.per = (int)ceil_div(blocks.slabs, splits);
@@ -186,15 +186,15 @@ sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols,
   return launched(what);
 }
 
-// The shapes of a block: outputs, how many a CU holds, microseconds that one takes for a slab when the CU is full of
-// them (its share) and when it is alone.
-enum Shape { kWide, kMiddle, kSquare, kSmall, kFlat, kTall, kShapes };
+// The shapes of a block: outputs, how many a CU holds, microseconds of bf16 that one takes for a slab when the CU is full
+// of them (its share) and when it is alone there (kPaired and the last three have two slabs in work at once).
+enum Shape { kWide, kBroad, kMiddle, kSquare, kPaired, kStream, kSmall, kFlat, kTall, kShapes };
 struct ShapeCost {
   int bm, bn, held;
   double full, alone;
 };
-constexpr ShapeCost kCost[kShapes] = {{256, 256, 1, 1.6, 1.6},  {192, 192, 1, 0.95, 0.95}, {128, 128, 2, 0.52, 0.6},
-                                      {64, 64, 2, 0.2, 0.25}, {32, 128, 2, 0.2, 0.25},   {128, 32, 2, 0.2, 0.25}};
+constexpr ShapeCost kCost[kShapes] = {{256, 256, 1, 1.56, 1.56}, {256, 192, 1, 1.25, 1.25}, {192, 192, 1, 1.0, 1.0}, {128, 128, 2, 0.51, 0.65}, {128, 128, 1, 0.55, 0.55},
+                                      {64, 64, 4, 0.15, 0.25},   {64, 64, 1, 0.18, 0.18},    {32, 128, 1, 0.18, 0.18}, {128, 32, 1, 0.18, 0.18}};
 
 struct Plan {
   Shape shape;
@@ -202,20 +202,23 @@ struct Plan {
 };
 enum Form { kAnyForm, kAlong };  // kAlong: both operands are (rows of 192 columns make no whole loads)
 
-// The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs, and for
-// a split sum its slabs' traffic (at 4 TB/s) and one launch more.
-inline Plan plan(int64_t rows, int64_t cols, int64_t slabs, int most_splits, Form form = kAnyForm, int64_t batch = 1, bool symmetric = false) {
+// The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs (1.4 as long for
+// three products a slab), and for a split sum its slabs' traffic (at 4 TB/s) and one launch more.
+inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_splits, Form form = kAnyForm, int64_t batch = 1, bool symmetric = false) {
+  const int64_t slabs = ceil_div(k, kind == tile::KIND_BF16 ? 64 : kind == tile::KIND_SPLIT ? 32 : 256);
+  const double longer = kind == tile::KIND_SPLIT ? 1.4 : 1.0;
   Plan best = {kWide, 1};
   double least = 1e30;
   for (int s = 0; s < kShapes; ++s) {
     const ShapeCost &c = kCost[s];
-    if ((symmetric && c.bm != c.bn) || (s == kMiddle && form != kAlong)) continue;
+    if ((symmetric && c.bm != c.bn) || ((s == kMiddle || s == kBroad) && form != kAlong)) continue;
     const double across = (double)ceil_div(cols, c.bn), blocks = symmetric ? across * (across + 1) / 2 : (double)ceil_div(rows, c.bm) * across;
-    for (int split = 1; split <= most_splits && (split == 1 || split * 2 <= slabs); split *= 2) {
+    for (int split = 1; split <= most_splits && (split == 1 || split * 2 <= slabs); ++split) {
       const double n = blocks * split * batch, rounds = std::ceil(n / (kCus * c.held));
       const double held = std::min<double>(c.held, std::ceil(n / kCus));
-      double t = rounds * (double)ceil_div(slabs, split) * std::max(c.alone, held * c.full) + 3.0;
-      if (split > 1) t += 4.0 + 2e-6 * rows * cols * split * batch;
+      // (a round's first loads and last stores overlap with other blocks' work where a CU holds several)
+      double t = rounds * (longer * (double)ceil_div(slabs, split) * std::max(c.alone, held * c.full) + 5.0 / std::sqrt(held));
+      if (split > 1) t += 5.0 + 2e-6 * rows * cols * split * batch;
       if (t < least) {
         least = t;
         best = {(Shape)s, split};
@@ -227,14 +230,19 @@ inline Plan plan(int64_t rows, int64_t cols, int64_t slabs, int most_splits, For
 
 template <int KIND, bool AA, bool AB, class E>
 sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
+  constexpr int kGroups = KIND == tile::KIND_MX ? 1 : 2;  // (its scales need LDS too: two blocks a CU instead)
   switch (p.shape) {
-    case kWide: return launch<KIND, 256, 256, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kBroad:
+      if constexpr (!AA && !AB) return launch<KIND, 256, 192, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kMiddle:
-      if constexpr (!AA && !AB) return launch<KIND, 192, 192, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kFlat: return launch<KIND, 32, 128, 1, 4, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    default: return launch<KIND, 128, 32, 4, 1, 4, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      if constexpr (!AA && !AB) return launch<KIND, 192, 192, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kPaired: return launch<KIND, 128, 128, 2, 2, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kStream: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kGroups, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    default: return launch<KIND, 128, 32, 4, 1, 3, kGroups, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
   }
 }
 

@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kNanScale = 255;
 
-inline int64_t blocks_of(int64_t n) { return 4 * ceil_div(n, 128); }
+__host__ __device__ inline int64_t blocks_of(int64_t n) { return 4 * ceil_div(n, 128); }
 
 // Magnitude code of a >= 0: the grid's middles, ties to the even code.
 __device__ __forceinline__ uint32_t code_of(float a) {
@@ -66,15 +66,17 @@ __device__ __forceinline__ void load8(const T *row, int64_t k, int64_t n, bool v
 // Eight values a lane, four lanes a block. Bound by memory: 4 (or 2) bytes read and 17/32 written a value.
 template <class T>
 __global__ __launch_bounds__(256) void k_quantize(const T *x, int64_t ld, int64_t rows, int64_t n, int64_t blocks, bool vec, uint8_t *codes, uint8_t *scales) {
-  const int64_t per = blocks * 4, total = rows * per;  // a multiple of 16: a block's lanes stay together
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per, c = i - r * per;
-    float v[8];
-    load8(x + r * ld, c * 8, n, vec, v);
-    uint32_t scale;
-    const uint32_t word = quantize8(v, scale);
-    *(uint32_t *)(codes + i * 4) = word;
-    if ((c & 3) == 0) scales[i >> 2] = (uint8_t)scale;
+  const int per = (int)blocks * 4;  // a multiple of 16: a block's lanes stay together
+  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+    const T *row = x + r * ld;
+    uint8_t *to = codes + r * blocks * 16, *scale_to = scales + r * blocks;
+    for (int c = blockIdx.x * 256 + threadIdx.x; c < per; c += gridDim.x * 256) {
+      float v[8];
+      load8(row, c * 8, n, vec, v);
+      uint32_t scale;
+      *(uint32_t *)(to + c * 4) = quantize8(v, scale);
+      if ((c & 3) == 0) scale_to[c >> 2] = (uint8_t)scale;
+    }
   }
 }
 
@@ -88,18 +90,19 @@ __device__ __forceinline__ float value_of(uint32_t code, uint32_t scale) {
 
 template <class T>
 __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t n, int64_t blocks, T *out, int64_t ld, bool vec) {
-  const int64_t per = blocks * 4, total = rows * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per, k = (i - r * per) * 8;
-    if (k >= n) continue;
-    const uint32_t word = *(const uint32_t *)(codes + i * 4), scale = scales[i >> 2];
-    f32x4 v[2];
+  const int per = (int)ceil_div(n, 8);
+  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+    const uint8_t *from = codes + r * blocks * 16, *scale_of = scales + r * blocks;
+    for (int c = blockIdx.x * 256 + threadIdx.x; c < per; c += gridDim.x * 256) {
+      const uint32_t word = *(const uint32_t *)(from + c * 4), scale = scale_of[c >> 2];
+      f32x4 v[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j >> 2][j & 3] = value_of(word >> (4 * j) & 15, scale);
-    T *to = out + r * ld + k;
-    const int left = n - k < 8 ? (int)(n - k) : 8;
-    store4(to, v[0], left < 4 ? left : 4, vec);
-    if (left > 4) store4(to + 4, v[1], left - 4, vec);
+      for (int j = 0; j < 8; ++j) v[j >> 2][j & 3] = value_of(word >> (4 * j) & 15, scale);
+      T *to = out + r * ld + c * 8;
+      const int left = min((int)n - c * 8, 8);
+      store4(to, v[0], left < 4 ? left : 4, vec);
+      if (left > 4) store4(to + 4, v[1], left - 4, vec);
+    }
   }
 }
 
@@ -130,16 +133,20 @@ sdnn_status product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8
   const int64_t pitch = blocks_of(n) * 16;
   const Matrix a{(const char *)x_codes, pitch, rows, pitch, 0, x_scales}, b{(const char *)w_codes, pitch, outputs, pitch, 0, w_scales};
   const Store<T> e{out, ld, rows, outputs, (uintptr_t)out % (4 * sizeof(T)) == 0 && ld % 4 == 0};
-  return run_shape<KIND_MX, false, false>(plan(rows, outputs, ceil_div(n, 256), 1), a, b, rows, outputs, n, e, stream, "product");
+  return run_shape<KIND_MX, false, false>(plan(KIND_MX, rows, outputs, n, 1, kAlong), a, b, rows, outputs, n, e, stream, "product");
 }
 
-unsigned grid_of(int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, 256), kCus * 32)); }
+// Workgroups along a row of `items` lanes, and down the rows: 16 to 32 a CU where there is work for them.
+dim3 grid_of(int64_t rows, int64_t items) {
+  const int64_t x = ceil_div(items, 256);
+  return dim3((unsigned)x, (unsigned)std::max<int64_t>(1, std::min<int64_t>({rows, 65535, ceil_div(kCus * 32, x)})));
+}
 
 template <class T>
 sdnn_status quantize(const T *x, int64_t ld, int64_t rows, int64_t n, uint8_t *codes, uint8_t *scales, hipStream_t stream) {
   const int64_t blocks = blocks_of(n);
   const bool vec = (uintptr_t)x % 16 == 0 && ld * sizeof(T) % 16 == 0;
-  hipLaunchKernelGGL((k_quantize<T>), dim3(grid_of(rows * blocks * 4)), dim3(256), 0, stream, x, ld, rows, n, blocks, vec, codes, scales);
+  hipLaunchKernelGGL((k_quantize<T>), grid_of(rows, blocks * 4), dim3(256), 0, stream, x, ld, rows, n, blocks, vec, codes, scales);
   return launched("quantize");
 }
 
@@ -183,7 +190,7 @@ sdnn_status sdnn_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int6
   if ((st = check_mx("the input", codes, scales)) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
   const int64_t blocks = blocks_of(n_values);
-  const dim3 grid(grid_of(n_rows * blocks * 4));
+  const dim3 grid = grid_of(n_rows, ceil_div(n_values, 8));
   const bool vec = (uintptr_t)out % (4 * dtype_bytes(dtype)) == 0 && ldo % 4 == 0;
   if (dtype == SDNN_BF16)
     hipLaunchKernelGGL((k_dequantize<__bf16>), grid, dim3(256), 0, stream, codes, scales, n_rows, n_values, blocks, (__bf16 *)out, ldo, vec);

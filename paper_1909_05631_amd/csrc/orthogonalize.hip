@@ -271,9 +271,9 @@ sdnn_status orthogonalize(const T *g, int64_t ldg, int64_t batch_g, T *out, int6
   hipLaunchKernelGGL((k_start<T>), dim3(row_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts, (int)norm_blocks, (double)eps, bounds[0], sp.info, sp.x[0], pitch);
   sdnn_status st = launched("orthogonalize");
   const bool tall = rows > cols;
-  const Plan gram = plan(m, m, ceil_div(std::max(rows, cols), 32), 1, tall ? kAnyForm : kAlong, batch, true);
-  const Plan power = plan(m, m, ceil_div(m, 32), 1, kAlong, batch, true);
-  const Plan update = plan(rows, cols, ceil_div(m, 32), 1, tall ? kAlong : kAnyForm, batch);
+  const Plan gram = plan(KIND_SPLIT, m, m, std::max(rows, cols), 1, tall ? kAnyForm : kAlong, batch, true);
+  const Plan power = plan(KIND_SPLIT, m, m, m, 1, kAlong, batch, true);
+  const Plan update = plan(KIND_SPLIT, rows, cols, m, 1, tall ? kAlong : kAnyForm, batch);
   for (int k = 0; k < steps && st == SDNN_OK; ++k) {
     const char *x = sp.x[k & 1];
     char *next = k + 1 < steps ? sp.x[(k + 1) & 1] : nullptr;

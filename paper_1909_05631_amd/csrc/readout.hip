@@ -15,7 +15,11 @@
 // G w (over the piece's classes) and dw = G^T x (over the rows), both through the transposing LDS reads, so neither
 // w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G: it stays in the Infinity Cache
 // between the products.
+//
+// Few rows or few classes (at most 16, few.h) have no use for tiles: one kernel with fp32 arithmetic streams the
+// other matrix past them, once.
 #include "dense.h"
+#include "few.h"
 
 using namespace dense;
 using tile::Block;
@@ -44,21 +48,6 @@ struct Scalars {
   float mean;                // 1 / (number of counted rows), at most 1
 };
 
-// One workgroup: the number of counted rows.
-__global__ __launch_bounds__(1024) void k_count(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) {
-  __shared__ int part[16];
-  int n = 0;
-  for (int64_t t = threadIdx.x; t < rows; t += 1024) n += counted(labels, t, classes);
-  for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    n = 0;
-    for (int i = 0; i < 16; ++i) n += part[i];
-    out->mean = 1.0f / (float)(n > 1 ? n : 1);
-  }
-}
-
 __device__ __forceinline__ float finite_magnitude(float v) {
   const float a = fabsf(v);
   return a < __builtin_inff() ? a : 0.0f;  // false for NaN too
@@ -72,21 +61,58 @@ __device__ __forceinline__ float max_of_workgroup(float m, float (&part)[4]) {
   return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
-// Largest finite magnitudes of a matrix, of its rows times their weights if there are any: one per workgroup. Rows without a label are skipped.
-__global__ __launch_bounds__(256) void k_top(const float *x, int64_t ld, int64_t rows, int64_t cols, const int64_t *labels, int64_t classes, const float *weights, float *top) {
-  __shared__ float part[4];
-  float m = 0.0f;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    if (labels && !counted(labels, r, classes)) continue;
-    const float w = weights ? weights[r] : 1.0f;
-#pragma unroll 4
-    for (int64_t c = threadIdx.x; c < cols; c += 256) m = fmaxf(m, finite_magnitude(x[r * ld + c] * w));
+// The number of counted rows, by a workgroup of 256.
+__device__ __forceinline__ void count_rows(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) {
+  __shared__ int part[4];
+  int n = 0;
+#pragma unroll 8
+  for (int64_t t = threadIdx.x; t < rows; t += 256) n += counted(labels, t, classes);
+  for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    n = part[0] + part[1] + part[2] + part[3];
+    out->mean = 1.0f / (float)(n > 1 ? n : 1);
   }
-  m = max_of_workgroup(m, part);
-  if (threadIdx.x == 0) top[blockIdx.x] = m;
+}
+__global__ __launch_bounds__(256) void k_count(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) { count_rows(labels, rows, classes, out); }
+
+__device__ __forceinline__ float top4(f32x4 v, float w) {
+  return fmaxf(fmaxf(finite_magnitude(v[0] * w), finite_magnitude(v[1] * w)), fmaxf(finite_magnitude(v[2] * w), finite_magnitude(v[3] * w)));
 }
 
-// What k_top found, by one wave (all of its lanes get it).
+// A matrix's rows for the kernels that go over x and w in one launch. Rows without a label (labels != nullptr) are
+// skipped or become zeros; the others are multiplied by their weights, if there are any.
+struct Rows {
+  const float *data;
+  int64_t ld, rows;
+  const int64_t *labels;
+  const float *weights;
+  float *top;      // the largest finite magnitudes, one per workgroup
+  int *exponents;  // of each row (nullptr: one of the whole matrix, from top)
+  char *out;       // the split form
+  bool vec;        // rows are 16-byte aligned
+};
+
+// Largest finite magnitudes of x, w and the weighted x (kTopBlocks workgroups each), and the number of counted rows (the
+// first workgroup). Bound by memory.
+__global__ __launch_bounds__(256) void k_survey(Rows x, Rows w, Rows xg, int64_t cols, const int64_t *labels, int64_t classes, Scalars *scalars) {
+  __shared__ float part[4];
+  if (blockIdx.x == 0) return count_rows(labels, x.rows, classes, scalars);
+  const int which = (blockIdx.x - 1) / kTopBlocks, block = (blockIdx.x - 1) % kTopBlocks;
+  const Rows &m = which == 0 ? x : which == 1 ? w : xg;
+  float top = 0.0f;
+  for (int64_t r = block; r < m.rows; r += kTopBlocks) {
+    if (m.labels && !counted(m.labels, r, classes)) continue;
+    const float weight = m.weights ? m.weights[r] : 1.0f;
+#pragma unroll 2
+    for (int64_t c = threadIdx.x * 4; c < cols; c += 1024) top = fmaxf(top, top4(few::load4(m.data + r * m.ld, (int)c, (int)cols, m.vec), weight));
+  }
+  top = max_of_workgroup(top, part);
+  if (threadIdx.x == 0) m.top[block] = top;
+}
+
+// What k_survey found, by one wave (all of its lanes get it).
 __device__ __forceinline__ float top_of(const float *top) {
   float m = 0.0f;
 #pragma unroll
@@ -95,42 +121,46 @@ __device__ __forceinline__ float top_of(const float *top) {
   return m;
 }
 
-// fp32 rows in the split form, 32 * groups values each, zeros past `cols`. A row's exponent: from its own largest
-// magnitude (exponents != nullptr, where it is written), or from the whole matrix's (top). weights: the values are
-// multiplied by their row's weight first. Rows without a label become zeros.
-__global__ __launch_bounds__(256) void k_split_rows(const float *x, int64_t ld, int64_t rows, int64_t cols, int64_t groups, const int64_t *labels, int64_t classes, const float *weights,
-                                                    const float *top, int *exponents, char *out) {
+// fp32 rows in the split form, 32 * groups values each, zeros past `cols`: `first` workgroups on x, `second` on w, the
+// rest on the weighted x.
+__global__ __launch_bounds__(256) void k_split_rows(Rows x, Rows w, Rows xg, int first, int second, int64_t cols, int64_t groups, int64_t classes) {
   __shared__ float part[4];
-  const int whole = exponents ? 0 : split_exponent(top_of(top));
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const float *row = x + r * ld;
-    const bool live = !labels || counted(labels, r, classes);
-    const float w = weights && live ? weights[r] : 1.0f;
-    int e;
-    if (exponents) {
-      float m = 0.0f;
+  const int b = blockIdx.x, which = b < first ? 0 : b < first + second ? 1 : 2;
+  const Rows &m = which == 0 ? x : which == 1 ? w : xg;
+  const int block = which == 0 ? b : which == 1 ? b - first : b - first - second;
+  const int step = which == 0 ? first : which == 1 ? second : (int)gridDim.x - first - second;
+  const int whole = m.exponents ? 0 : split_exponent(top_of(m.top));
+  for (int64_t r = block; r < m.rows; r += step) {
+    const float *row = m.data + r * m.ld;
+    const bool live = !m.labels || counted(m.labels, r, classes);
+    const float weight = m.weights && live ? m.weights[r] : 1.0f;
+    int e = whole;
+    if (m.exponents) {
+      float top = 0.0f;
       if (live)
-        for (int64_t c = threadIdx.x; c < cols; c += 256) m = fmaxf(m, finite_magnitude(row[c]));
-      e = split_exponent(max_of_workgroup(m, part));
-      if (threadIdx.x == 0) exponents[r] = e;
-    } else {
-      e = whole;
+        for (int64_t k = threadIdx.x * 4; k < cols; k += 1024) top = fmaxf(top, top4(few::load4(row, (int)k, (int)cols, m.vec), weight));
+      e = split_exponent(max_of_workgroup(top, part));
+      if (threadIdx.x == 0) m.exponents[r] = e;
     }
-    char *to = out + r * groups * 128;
+    char *to = m.out + r * groups * 128;
+#pragma unroll 2
     for (int64_t k = threadIdx.x * 4; k < groups * 32; k += 1024) {
       f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (live)
+      if (live) v = few::load4(row, (int)k, (int)cols, m.vec);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (k + i < cols) v[i] = ldexpf(row[k + i] * w, e);
+      for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i] * weight, e);
       store_split4(to, k, v);
     }
   }
 }
 
-// bf16 rows on 16-byte aligned rows of `pitch` values, zeros past `cols` and in rows without a label.
-__global__ __launch_bounds__(256) void k_copy_rows(const __bf16 *x, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, const int64_t *labels, int64_t classes, bool vec, __bf16 *out) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+// bf16 rows on 16-byte aligned rows of `pitch` values, zeros past `cols` and in rows without a label. With `scalars`, the
+// last workgroup counts the rows that have one.
+__global__ __launch_bounds__(256) void k_copy_rows(const __bf16 *x, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, const int64_t *labels, int64_t classes, bool vec, __bf16 *out,
+                                                   Scalars *scalars) {
+  if (scalars && blockIdx.x == gridDim.x - 1) return count_rows(labels, rows, classes, scalars);
+  const int step = (int)gridDim.x - (scalars ? 1 : 0);
+  for (int64_t r = blockIdx.x; r < rows; r += step) {
     const bool live = !labels || counted(labels, r, classes);
     for (int64_t k = threadIdx.x * 8; k < pitch; k += 2048) {
       typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -204,30 +234,51 @@ struct LossParts {
   }
 };
 
-// One wave per row: joins the parts. A NaN logit makes NaN of its row's sum (the maximum passes it over).
+// Joins the parts of a row: one wave a row, or a workgroup where there are many. A NaN logit makes NaN of its row's
+// sum (the maximum passes it over).
+struct Softmax {
+  float top, sum;
+  __device__ __forceinline__ void join(float t, float s) {
+    const float n = fmaxf(top, t);
+    sum = (top == -__builtin_inff() ? sum : sum * exp_of(top - n)) + (t == -__builtin_inff() ? s : s * exp_of(t - n));
+    top = n;
+  }
+};
+template <int WAVES>
 __global__ __launch_bounds__(256) void k_loss(const float2 *parts, int64_t count, const float *picked, const int64_t *labels, int64_t rows, int64_t classes, float *loss, float *lse) {
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (t >= rows) return;
-  float m = -__builtin_inff(), sum = 0.0f;
-  for (int64_t p = lane; p < count; p += 64) {
-    const float2 a = parts[t * count + p];
-    const float n = fmaxf(m, a.x);
-    const float keep = m == -__builtin_inff() ? 0.0f : exp_of(m - n);
-    sum = sum * keep + (a.x == -__builtin_inff() ? a.y : a.y * exp_of(a.x - n));
-    m = n;
+  __shared__ float2 shared[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t t = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (WAVES == 1 && t >= rows) return;
+  Softmax a{-__builtin_inff(), 0.0f};
+#pragma unroll 4
+  for (int64_t p = threadIdx.x & (64 * WAVES - 1); p < count; p += 64 * WAVES) {
+    const float2 b = parts[t * count + p];
+    a.join(b.x, b.y);
   }
   for (int d = 32; d; d >>= 1) {
-    const float om = __shfl_xor(m, d), os = __shfl_xor(sum, d);
-    const float n = fmaxf(m, om);
-    sum = (m == -__builtin_inff() ? sum : sum * exp_of(m - n)) + (om == -__builtin_inff() ? os : os * exp_of(om - n));
-    m = n;
+    const float top = __shfl_xor(a.top, d), sum = __shfl_xor(a.sum, d);
+    a.join(top, sum);
   }
-  if (lane == 0) {
-    const float s = m + logf(sum);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) shared[wave] = float2{a.top, a.sum};
+    __syncthreads();
+    a = {shared[0].x, shared[0].y};
+    for (int w = 1; w < 4; ++w) a.join(shared[w].x, shared[w].y);
+  }
+  if (lane == 0 && (WAVES == 1 || wave == 0)) {
+    const float s = a.top + logf(a.sum);
     if (lse) lse[t] = s;
     loss[t] = counted(labels, t, classes) ? s - picked[t] : 0.0f;
   }
+}
+
+sdnn_status join_parts(const float2 *parts, int64_t count, const float *picked, const int64_t *labels, int64_t rows, int64_t classes, float *loss, float *lse, hipStream_t stream) {
+  if (count > 256 && rows < 8 * kCus)
+    hipLaunchKernelGGL((k_loss<4>), dim3((unsigned)rows), dim3(256), 0, stream, parts, count, picked, labels, rows, classes, loss, lse);
+  else
+    hipLaunchKernelGGL((k_loss<1>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, stream, parts, count, picked, labels, rows, classes, loss, lse);
+  return launched("loss");
 }
 
 // Gradient: the piece's G. bf16: with the row's weight; split: without it, times 2^15.
@@ -343,24 +394,47 @@ struct Accumulate {
   }
 };
 
-// The slabs' sum, in their order, rounded to the output's type.
-template <class T>
+// The slabs' sum, rounded to the output's type: 256 / GROUPS items a workgroup, each group taking every GROUPS-th slab.
+template <class T, int GROUPS>
 __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int splits, int64_t ld_slab, Store<T> to) {
-  const int64_t per = ld_slab / 4;
+  constexpr int kItems = 256 / GROUPS;
+  __shared__ f32x4 shared[GROUPS][kItems];
+  const int64_t per = ld_slab / 4, total = to.rows * per;
   const OutScale::Found found = to.scale.find();
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < to.rows * per; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per, c = (i - r * per) * 4;
-    if (c >= to.cols) continue;
+  const int group = threadIdx.x / kItems, item = threadIdx.x % kItems;
+  for (int64_t i0 = (int64_t)blockIdx.x * kItems; i0 < total; i0 += (int64_t)gridDim.x * kItems) {
+    const int64_t i = i0 + item, r = i / per, c = (i - r * per) * 4;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(slabs + (s * to.rows + r) * ld_slab + c);
-    store4(to.out + r * to.ld + c, to.scale.apply(found, to.scale.weight(r), v), (int)(to.cols - c < 4 ? to.cols - c : 4), to.vec);
+    if (i < total)
+#pragma unroll 8
+      for (int s = group; s < splits; s += GROUPS) v += *(const f32x4 *)(slabs + (s * to.rows + r) * ld_slab + c);
+    if constexpr (GROUPS > 1) {
+      __syncthreads();
+      shared[group][item] = v;
+      __syncthreads();
+      if (group == 0)
+        for (int g = 1; g < GROUPS; ++g) v += shared[g][item];
+    }
+    if (group == 0 && i < total && c < to.cols) store4(to.out + r * to.ld + c, to.scale.apply(found, to.scale.weight(r), v), (int)(to.cols - c < 4 ? to.cols - c : 4), to.vec);
   }
+}
+
+template <class T>
+sdnn_status sum_slabs(const float *slabs, int splits, int64_t ld_slab, const Store<T> &to, hipStream_t stream, const char *what) {
+  const int64_t items = to.rows * (ld_slab / 4);
+  if (splits >= 32)
+    hipLaunchKernelGGL((k_sum_slabs<T, 16>), dim3((unsigned)std::min<int64_t>(ceil_div(items, 16), 8192)), dim3(256), 0, stream, slabs, splits, ld_slab, to);
+  else if (splits >= 8)
+    hipLaunchKernelGGL((k_sum_slabs<T, 4>), dim3((unsigned)std::min<int64_t>(ceil_div(items, 64), 8192)), dim3(256), 0, stream, slabs, splits, ld_slab, to);
+  else
+    hipLaunchKernelGGL((k_sum_slabs<T, 1>), dim3((unsigned)std::min<int64_t>(ceil_div(items, 256), 8192)), dim3(256), 0, stream, slabs, splits, ld_slab, to);
+  return launched(what);
 }
 
 // ------------------------------------------------------------------------------------------------
 // Host
 
-constexpr int kWaveCols[kShapes] = {64, 48, 64, 32, 32, 32};  // columns of a wave: the parts of a row of logits
+constexpr int kWaveCols[kShapes] = {64, 48, 48, 64, 64, 32, 32, 32, 32};  // columns of a wave: the parts of a row of logits
 
 // Sizes of one call.
 struct Sizes {
@@ -370,18 +444,21 @@ struct Sizes {
   int64_t groups() const { return ceil_div(features, 32); }
   int64_t pitch_values() const { return ceil_div(features, 8) * 8; }  // bf16 rows that had to be copied
   size_t packed(int64_t n) const { return dtype == SDNN_BF16 ? (size_t)(n * pitch_values() * 2) : (size_t)(n * groups() * 128); }
-  int64_t feature_slabs() const { return ceil_div(features, per_slab()); }
+  int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : KIND_SPLIT; }
   // Classes of a piece: 2^26 values of G, whole blocks of 256 classes.
   int64_t piece() const {
     const int64_t p = std::max<int64_t>(256, std::min(kPieceClasses, kPieceValues / std::max<int64_t>(rows, 1)) / 256 * 256);
     return std::min(p, classes);
   }
   int64_t g_pitch() const { return ceil_div(piece(), per_slab()) * 128; }
-  Plan loss() const { return plan(rows, classes, feature_slabs(), 1, kAlong); }
-  Plan logits(int64_t n) const { return plan(rows, n, feature_slabs(), 1, kAlong); }
-  Plan dx() const { return plan(rows, features, ceil_div(piece(), per_slab()), kMaxSplits); }
-  Plan dw(int64_t n) const { return plan(n, features, ceil_div(rows, per_slab()), kMaxSplits); }
+  Plan loss() const { return plan(kind(), rows, classes, features, 1, kAlong); }
+  Plan logits(int64_t n) const { return plan(kind(), rows, n, features, 1, kAlong); }
+  Plan dx() const { return plan(kind(), rows, features, piece(), kMaxSplits); }
+  Plan dw(int64_t n) const { return plan(kind(), n, features, rows, kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
+  // Few rows are held rather than few classes.
+  bool rows_held() const { return few::fit_of(rows, features) != few::kNone && (rows <= classes || few::fit_of(classes, features) == few::kNone); }
+  few::Fit few() const { return few::fit_of(rows_held() ? rows : classes, features); }
 };
 
 bool usable_in_place(const void *p, int64_t ld, int64_t cols) {
@@ -395,11 +472,12 @@ struct LossSpace {
   float *picked;
   int64_t count;
   LossSpace(Carver &c, const Sizes &s) {
-    x = c.take<char>(s.packed(s.rows));
-    w = c.take<char>(s.packed(s.classes));
+    const bool packed = s.few() == few::kNone;
+    x = c.take<char>(packed ? s.packed(s.rows) : 0);
+    w = c.take<char>(packed ? s.packed(s.classes) : 0);
     ex = c.take<int>(s.rows);
     ew = c.take<int>(s.classes);
-    count = ceil_div(s.classes, kWaveCols[s.loss().shape]);
+    count = !packed ? (s.rows_held() ? (int64_t)few::grid_of(s.few(), s.classes, false) * few::batch_of(s.few()) : 0) : ceil_div(s.classes, kWaveCols[s.loss().shape]);
     parts = c.take<float2>(s.rows * count);
     picked = c.take<float>(s.rows);
   }
@@ -408,9 +486,14 @@ struct LossSpace {
 struct GradSpace {
   char *x, *w, *xg, *g;
   Scalars *scalars;
-  float *dx, *dw;
+  float *dx, *dw, *few;
   GradSpace(Carver &c, const Sizes &s) {
     scalars = c.take<Scalars>(1);
+    if (s.few() != ::few::kNone) {
+      const bool held = s.rows_held();
+      few = c.take<float>((size_t)(::few::grid_of(s.few(), held ? s.classes : s.rows, true) * (held ? s.rows : s.classes) * s.ld_slab()));
+      return;
+    }
     x = c.take<char>(s.packed(s.rows));
     w = c.take<char>(s.packed(s.classes));
     xg = c.take<char>(s.dtype == SDNN_FP32 ? s.packed(s.rows) : 0);
@@ -427,35 +510,78 @@ struct GradSpace {
 
 unsigned row_grid(int64_t rows) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(rows, 2048)); }
 
-// A matrix as an operand: in place, or copied into `space` first.
-template <int KIND>
-Matrix operand(const void *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, const float *top, int *exponents, const float *weights, char *space, hipStream_t stream) {
-  if constexpr (KIND == KIND_BF16) {
-    if (!labels && usable_in_place(data, ld, s.features)) return {(const char *)data, ld * 2, rows, s.features * 2, 0};
-    const bool vec = ((uintptr_t)data & 15) == 0 && ld % 8 == 0;
-    if (rows)
-      hipLaunchKernelGGL(k_copy_rows, dim3(row_grid(rows)), dim3(256), 0, stream, (const __bf16 *)data, ld, rows, s.features, s.pitch_values(), labels, s.classes, vec, (__bf16 *)space);
-    return {space, s.pitch_values() * 2, rows, s.pitch_values() * 2, 0};
-  } else {
-    if (rows)
-      hipLaunchKernelGGL(k_split_rows, dim3(row_grid(rows)), dim3(256), 0, stream, (const float *)data, ld, rows, s.features, s.groups(), labels, s.classes, weights, top, exponents, space);
-    return {space, s.groups() * 128, rows, s.groups() * 128, 0};
-  }
+bool aligned16(const void *p, int64_t ld, int bytes) { return ((uintptr_t)p & 15) == 0 && ld * bytes % 16 == 0; }
+
+// bf16 rows as an operand: in place, or copied into `space` (always with labels; then the counted rows are counted too).
+Matrix bf16_rows(const __bf16 *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, Scalars *scalars, char *space, hipStream_t stream) {
+  if (!labels && usable_in_place(data, ld, s.features)) return {(const char *)data, ld * 2, rows, s.features * 2, 0};
+  hipLaunchKernelGGL(k_copy_rows, dim3(row_grid(rows) + (scalars ? 1 : 0)), dim3(256), 0, stream, data, ld, rows, s.features, s.pitch_values(), labels, s.classes, aligned16(data, ld, 2), (__bf16 *)space,
+                     scalars);
+  return {space, s.pitch_values() * 2, rows, s.pitch_values() * 2, 0};
 }
 
-template <int KIND>
-sdnn_status loss_of(const Sizes &s, const void *x, int64_t ldx, const void *w, int64_t ldw, const int64_t *labels, float *loss, float *lse, void *workspace, hipStream_t stream) {
+Matrix split_matrix(const Rows &r, const Sizes &s) { return {r.out, s.groups() * 128, r.rows, s.groups() * 128, 0}; }
+
+// x, w and, with xg.rows, the weighted x in the split form.
+void split_rows(const Rows &x, const Rows &w, const Rows &xg, const Sizes &s, hipStream_t stream) {
+  const unsigned a = row_grid(x.rows), b = row_grid(w.rows), c = xg.rows ? row_grid(xg.rows) : 0;
+  hipLaunchKernelGGL(k_split_rows, dim3(a + b + c), dim3(256), 0, stream, x, w, xg, (int)a, (int)b, s.features, s.groups(), s.classes);
+}
+
+template <class T>
+bool vector_rows(const T *p, int64_t ld) {
+  return (uintptr_t)p % (4 * sizeof(T)) == 0 && ld % 4 == 0;
+}
+
+template <class T>
+few::Few<T> few_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t ldw, const int64_t *labels) {
+  const bool rows = s.rows_held();
+  few::Few<T> p{};
+  p.held = rows ? x : w;
+  p.stream = rows ? w : x;
+  p.ld_held = rows ? ldx : ldw;
+  p.ld_stream = rows ? ldw : ldx;
+  p.held_rows = (int)(rows ? s.rows : s.classes);
+  p.stream_rows = rows ? s.classes : s.rows;
+  p.features = (int)s.features;
+  p.vec_held = vector_rows(p.held, p.ld_held);
+  p.vec_stream = vector_rows(p.stream, p.ld_stream);
+  p.labels = labels;
+  p.classes = s.classes;
+  return p;
+}
+
+template <int KIND, class T>
+sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t ldw, const int64_t *labels, float *loss, float *lse, void *workspace, hipStream_t stream) {
   Carver carver{(char *)workspace};
   const LossSpace sp(carver, s);
-  const Matrix a = operand<KIND>(x, ldx, s.rows, s, nullptr, nullptr, sp.ex, nullptr, sp.x, stream);
-  const Matrix b = operand<KIND>(w, ldw, s.classes, s, nullptr, nullptr, sp.ew, nullptr, sp.w, stream);
+  if (s.few() != few::kNone) {
+    few::Few<T> p = few_of(s, x, ldx, w, ldw, labels);
+    p.loss = loss;
+    p.lse = lse;
+    p.parts = sp.parts;
+    p.picked = sp.picked;
+    if (!s.rows_held()) return few::launch<false, false>(s.few(), p, stream, "loss");
+    const sdnn_status st = few::launch<true, false>(s.few(), p, stream, "loss");
+    return st != SDNN_OK ? st : join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
+  }
+  Matrix a, b;
+  if constexpr (KIND == KIND_BF16) {
+    a = bf16_rows(x, ldx, s.rows, s, nullptr, nullptr, sp.x, stream);
+    b = bf16_rows(w, ldw, s.classes, s, nullptr, nullptr, sp.w, stream);
+  } else {
+    const Rows rx{x, ldx, s.rows, nullptr, nullptr, nullptr, sp.ex, sp.x, aligned16(x, ldx, 4)};
+    const Rows rw{w, ldw, s.classes, nullptr, nullptr, nullptr, sp.ew, sp.w, aligned16(w, ldw, 4)};
+    split_rows(rx, rw, Rows{}, s, stream);
+    a = split_matrix(rx, s);
+    b = split_matrix(rw, s);
+  }
   sdnn_status st = launched("rows");
   if (st != SDNN_OK) return st;
   const LossParts<KIND> e{{sp.ex, sp.ew, nullptr, nullptr}, labels, s.rows, s.classes, sp.parts, sp.count, sp.picked};
   st = run_shape<KIND, false, false>(s.loss(), a, b, s.rows, s.classes, s.features, e, stream, "loss");
   if (st != SDNN_OK) return st;
-  hipLaunchKernelGGL(k_loss, dim3((unsigned)ceil_div(s.rows, 4)), dim3(256), 0, stream, sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse);
-  return launched("loss");
+  return join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
 }
 
 // C = A B^T over k, into `to` directly or through fp32 slabs.
@@ -465,14 +591,7 @@ sdnn_status product(const Plan &p, const Matrix &a, const Matrix &b, int64_t k, 
   const Accumulate e{slabs, ld_slab, to.rows, to.cols, add};
   sdnn_status st = run_shape<KIND, AA, true>(p, a, b, to.rows, to.cols, k, e, stream, what);
   if (st != SDNN_OK || !last) return st;
-  const int64_t work = ceil_div(to.rows * (ld_slab / 4), 256);
-  hipLaunchKernelGGL((k_sum_slabs<T>), dim3((unsigned)std::min<int64_t>(work, 8192)), dim3(256), 0, stream, slabs, p.splits, ld_slab, to);
-  return launched(what);
-}
-
-template <class T>
-bool vector_rows(const T *p, int64_t ld) {
-  return (uintptr_t)p % (4 * sizeof(T)) == 0 && ld % 4 == 0;
+  return sum_slabs(slabs, p.splits, ld_slab, to, stream, what);
 }
 
 template <class T>
@@ -490,23 +609,47 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     if (dw) hipLaunchKernelGGL((k_zero_rows<T>), dim3(row_grid(s.classes)), dim3(256), 0, stream, dw, lddw, s.classes, s.features);
     return launched("gradient");
   }
-  hipLaunchKernelGGL(k_count, dim3(1), dim3(1024), 0, stream, labels, s.rows, s.classes, sp.scalars);
-  float *top_x = nullptr, *top_w = nullptr;
-  if constexpr (KIND == KIND_SPLIT) {
+  if (s.few() != few::kNone) {
+    const bool held = s.rows_held();
+    few::Few<T> p = few_of(s, x, ldx, w, ldw, labels);
+    T *d_held = held ? dx : dw;
+    const int64_t ld_d_held = held ? lddx : lddw;
+    p.known_lse = lse;
+    p.weights = weights;
+    p.mean = &sp.scalars->mean;
+    p.d_stream = held ? dw : dx;
+    p.ld_d = held ? lddw : lddx;
+    p.vec_d = vector_rows(p.d_stream, p.ld_d);
+    p.slabs = d_held ? sp.few : nullptr;
+    p.ld_slab = s.ld_slab();
+    if (!held && !weights) hipLaunchKernelGGL(k_count, dim3(1), dim3(256), 0, stream, labels, s.rows, s.classes, sp.scalars);
+    const sdnn_status st = held ? few::launch<true, true>(s.few(), p, stream, "gradient") : few::launch<false, true>(s.few(), p, stream, "gradient");
+    if (st != SDNN_OK || !d_held) return st;
+    const Store<T> to{d_held, ld_d_held, p.held_rows, s.features, vector_rows(d_held, ld_d_held), {nullptr, nullptr, nullptr}};
+    return sum_slabs(sp.few, (int)few::grid_of(s.few(), p.stream_rows, true), s.ld_slab(), to, stream, "gradient");
+  }
+  Matrix a, b, ag;  // ag: dw's other operand: the rows, in fp32 times their weights (in bf16 G holds the weights)
+  float *top_x = nullptr, *top_w = nullptr, *top_g = nullptr;
+  if constexpr (KIND == KIND_BF16) {
+    ag = a = bf16_rows(x, ldx, s.rows, s, labels, sp.scalars, sp.x, stream);
+    b = bf16_rows(w, ldw, s.classes, s, nullptr, nullptr, sp.w, stream);
+  } else {
+    const bool weighted = weights && dw;
     top_x = sp.scalars->top[0];
     top_w = sp.scalars->top[1];
-    hipLaunchKernelGGL(k_top, dim3(kTopBlocks), dim3(256), 0, stream, x, ldx, s.rows, s.features, labels, s.classes, (const float *)nullptr, top_x);
-    hipLaunchKernelGGL(k_top, dim3(kTopBlocks), dim3(256), 0, stream, w, ldw, s.classes, s.features, (const int64_t *)nullptr, s.classes, (const float *)nullptr, top_w);
-  }
-  const Matrix a = operand<KIND>(x, ldx, s.rows, s, labels, top_x, nullptr, nullptr, sp.x, stream);
-  const Matrix b = operand<KIND>(w, ldw, s.classes, s, nullptr, top_w, nullptr, nullptr, sp.w, stream);
-  Matrix ag = a;  // dw's other operand: the rows, in fp32 times their weights (in bf16 G holds the weights)
-  const float *top_g = top_x;
-  if (KIND == KIND_SPLIT && weights && dw) {
-    float *top = sp.scalars->top[2];
-    hipLaunchKernelGGL(k_top, dim3(kTopBlocks), dim3(256), 0, stream, (const float *)x, ldx, s.rows, s.features, labels, s.classes, weights, top);
-    ag = operand<KIND>(x, ldx, s.rows, s, labels, top, nullptr, weights, sp.xg, stream);
-    top_g = top;
+    top_g = weighted ? sp.scalars->top[2] : top_x;
+    const Rows rx{x, ldx, s.rows, labels, nullptr, top_x, nullptr, sp.x, aligned16(x, ldx, 4)};
+    const Rows rw{w, ldw, s.classes, nullptr, nullptr, top_w, nullptr, sp.w, aligned16(w, ldw, 4)};
+    Rows rg = rx;
+    rg.rows = weighted ? s.rows : 0;
+    rg.weights = weights;
+    rg.top = top_g;
+    rg.out = sp.xg;
+    hipLaunchKernelGGL(k_survey, dim3(1 + kTopBlocks * (weighted ? 3 : 2)), dim3(256), 0, stream, rx, rw, rg, s.features, labels, s.classes, sp.scalars);
+    split_rows(rx, rw, rg, s, stream);
+    a = split_matrix(rx, s);
+    b = split_matrix(rw, s);
+    ag = weighted ? split_matrix(rg, s) : a;
   }
   sdnn_status st = launched("gradient");
   const float *mean = KIND == KIND_SPLIT && !weights ? &sp.scalars->mean : nullptr;
@@ -570,7 +713,8 @@ sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t
   const Sizes s{n_rows, n_classes, n_features, dtype};
   if ((st = check_workspace(workspace, workspace_bytes, sdnn_readout_workspace_bytes(n_rows, n_classes, n_features, dtype, 0))) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  return dtype == SDNN_BF16 ? loss_of<KIND_BF16>(s, x, ldx, w, ldw, labels, loss, lse, workspace, stream) : loss_of<KIND_SPLIT>(s, x, ldx, w, ldw, labels, loss, lse, workspace, stream);
+  return dtype == SDNN_BF16 ? loss_of<KIND_BF16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, loss, lse, workspace, stream)
+                            : loss_of<KIND_SPLIT>(s, (const float *)x, ldx, (const float *)w, ldw, labels, loss, lse, workspace, stream);
 }
 
 sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t dtype, const int64_t *labels, const float *lse, const float *row_grad, int64_t n_rows,

@@ -84,13 +84,14 @@ __device__ __forceinline__ void meet() {
 // Moves slab `s` of one operand to LDS. ROWS: the block's rows (along) or columns (across) of this operand.
 template <int KIND, int ROWS, bool ACROSS, int THREADS>
 struct Loader {
-  static constexpr int kBytes = ROWS * kSlab;
+  static constexpr int kData = ROWS * kSlab;
   static constexpr int kRound = THREADS * 16;  // bytes that the workgroup moves at once
-  static constexpr int kRounds = (kBytes + kRound - 1) / kRound;
+  static constexpr int kRounds = (kData + kRound - 1) / kRound;
+  static constexpr int kBytes = kRounds * kRound;  // in LDS: lanes past a short slab read zeros into padding
   static constexpr int kRowBytes = ACROSS ? ROWS * Geometry<KIND>::kBytes : kSlab;  // a row in LDS
   static constexpr int kRowsPerRound = kRound / kRowBytes;
-  static constexpr int kSlabRows = kBytes / kRowBytes;
-  static_assert(kBytes % kRound == 0, "whole rounds");
+  static constexpr int kSlabRows = kData / kRowBytes;
+  static_assert(kData % kRound == 0 || kRounds == 1, "whole rounds");
   static_assert(kRound % kRowBytes == 0 && kRowsPerRound % (ACROSS ? 4 : 8) == 0, "the permutation repeats every round");
 
   static constexpr int kTurn = (kRowBytes / 16 - 1) & 6;  // chunk bits that an across row's number permutes
@@ -105,7 +106,7 @@ struct Loader {
     const int c = t % (kRowBytes / 16);
     chunk = ACROSS ? c ^ ((row << 1) & kTurn) : c ^ (row & 7);
     offset = row * op.pitch + chunk * 16;
-    if (ACROSS && chunk * 16 >= op.extent) offset = kOut;
+    if ((ACROSS && chunk * 16 >= op.extent) || row * kRowBytes >= kData) offset = kOut;
   }
 
   // A slab's loads, issued one at a time. Past the operand's k they read zeros: every slab has kRounds of them, which the
@@ -256,25 +257,31 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 // fragments. Measured on 8192^3: bf16 1300 TFLOP/s at 66% of the cycles in matrix instructions (the card lowers its
 // clock to 1.9 GHz under them; at 1570 for the library's kernel in the same run), KIND_SPLIT 1430, 477 of fp32.
 // Four waves of 128 x 128 read less LDS and measured 1010, raised wave priorities during the products 7% less.
-template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, int STAGES>
+//
+// GROUPS of WM x WN waves may share the block's outputs, each taking every GROUPS-th slab of the same stage, with their
+// sums joined through LDS at the end: a launch of few blocks runs through k in fewer meetings.
+template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, int STAGES, int GROUPS = 1>
 struct Block {
-  static constexpr int kThreads = 64 * WM * WN;
+  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves * GROUPS;
   static constexpr int kTM = BM / WM / 16, kTN = BN / WN / 16;
   using LoadA = Loader<KIND, BM, ACROSS_A, kThreads>;
   using LoadB = Loader<KIND, BN, ACROSS_B, kThreads>;
   using ScaleA = ScaleLoader<BM, kThreads>;
   using ScaleB = ScaleLoader<BN, kThreads>;
   static constexpr bool kMx = KIND == KIND_MX;
-  static constexpr int kValues = (BM + BN) * kSlab;
-  static constexpr int kStage = kValues + (kMx ? ScaleA::kBytes + ScaleB::kBytes : 0);
+  static constexpr int kValuesA = LoadA::kBytes, kValues = kValuesA + LoadB::kBytes;
+  static constexpr int kPart = kValues + (kMx ? ScaleA::kBytes + ScaleB::kBytes : 0);  // a group's slab
+  static constexpr int kStage = GROUPS * kPart;
   static constexpr int kLds = STAGES * kStage;
   static_assert(kLds <= 160 * 1024, "LDS of a CU");
-  static constexpr int kLoads = LoadA::kRounds + LoadB::kRounds + (kMx ? ScaleA::kRounds + ScaleB::kRounds : 0);  // of a wave and slab
+  static constexpr int kLoads = GROUPS * (LoadA::kRounds + LoadB::kRounds + (kMx ? ScaleA::kRounds + ScaleB::kRounds : 0));  // of a wave and stage
+  static_assert(GROUPS == 1 || kStage * STAGES >= (GROUPS - 1) * BM * BN * 4, "the sums' room");
 
   f32x4 acc[kTM][kTN];
 
   __device__ __forceinline__ static int wave() { return uniform(threadIdx.x >> 6); }
-  __device__ __forceinline__ static int row0() { return (wave() / WN) * (BM / WM); }
+  __device__ __forceinline__ static int group() { return wave() / kWaves; }
+  __device__ __forceinline__ static int row0() { return (wave() % kWaves / WN) * (BM / WM); }
   __device__ __forceinline__ static int col0() { return (wave() % WN) * (BN / WN); }
 
   template <class R>
@@ -347,19 +354,24 @@ struct Block {
         lsb.load(b, s, at + ScaleA::kBytes);
       }
     };
+    const auto load = [&](int s, int to) {
 #pragma unroll
-    for (int i = 0; i < STAGES; ++i) {
-      load_scales(s0 + i, i * kStage);
-      la.load(a, s0 + i, mine + i * kStage);
-      lb.load(b, s0 + i, mine + i * kStage + BM * kSlab);
-    }
+      for (int g = 0; g < GROUPS; ++g) {
+        load_scales(s + g, to + g * kPart);
+        la.load(a, s + g, mine + to + g * kPart);
+        lb.load(b, s + g, mine + to + g * kPart + kValuesA);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) load(s0 + i * GROUPS, i * kStage);
+    lds += group() * kPart;
     wait_loads<(STAGES - 1) * kLoads>();
     meet();
     constexpr int kEach = kMx ? 2 : ACROSS_A ? 2 : 1;                      // LDS reads with a subtile of A
     constexpr int kAll = kTN * (kMx ? 2 : ACROSS_B ? 2 : 1);               // with all of B
     i32x4 fa[kTM], fb[kTN], gb[kTN];
     int sa[kTM], sb[kTN];
-    read(rb, lds + BM * kSlab, 0, fb);
+    read(rb, lds + kValuesA, 0, fb);
 #pragma unroll
     for (int i = 0; i < kTM; ++i) fa[i] = ra.read(lds, i, 0);
 #pragma unroll
@@ -367,12 +379,12 @@ struct Block {
 #pragma unroll
     for (int j = 0; j < kTN; ++j) sb[j] = kMx ? read_scale(lds + kValues + ScaleA::kBytes, col0(), j) : 0;
     int at = 0;
-    for (int s = s0; s < s1; ++s) {
+    for (int s = s0; s < s1; s += GROUPS) {
       const int used = at * kStage;
       const char *now = lds + used;
       at = at + 1 == STAGES ? 0 : at + 1;
       const char *then = lds + at * kStage;
-      read(rb, now + BM * kSlab, 1, gb);
+      read(rb, now + kValuesA, 1, gb);
       reads<kTN * (ACROSS_B ? 2 : 1)>();
       if constexpr (KIND == KIND_SPLIT) {
 #pragma unroll
@@ -397,9 +409,13 @@ struct Block {
       // slab s + 1 has arrived; all fragments of slab s are in registers
       wait_loads<(STAGES - 2) * kLoads>();
       meet();
-      load_scales(s + STAGES, used);
+      constexpr bool kSpread = kTM >= 8 && GROUPS == 1;  // a small block has no time to spread its loads over
+      if constexpr (kSpread)
+        load_scales(s + STAGES, used);
+      else
+        load(s + STAGES * GROUPS, used);
       const auto next_a = la.slab(a, s + STAGES, mine + used);
-      const auto next_b = lb.slab(b, s + STAGES, mine + used + BM * kSlab);
+      const auto next_b = lb.slab(b, s + STAGES, mine + used + kValuesA);
       constexpr int kValueLoads = LoadA::kRounds + LoadB::kRounds;
       int issued = 0;
       const auto issue = [&](int until) {
@@ -413,10 +429,9 @@ struct Block {
           }
         issued = until;
       };
-      if (kTM < 8) issue(kValueLoads);  // a small block has no time to spread them over
       i32x4 hb[kTN];
       int hs[kTN];
-      read(rb, then + BM * kSlab, 0, hb);
+      read(rb, then + kValuesA, 0, hb);
 #pragma unroll
       for (int j = 0; j < kTN; ++j) hs[j] = kMx ? read_scale(then + kValues + ScaleA::kBytes, col0(), j) : 0;
 #pragma unroll
@@ -430,7 +445,7 @@ struct Block {
         multiply<1>(i, fa[i], KIND == KIND_SPLIT ? fb : gb, sa[i], sb);
         fa[i] = ra.read(then, i, 0);
         if (kMx) sa[i] = read_scale(then + kValues, row0(), i);
-        issue(kValueLoads * (i - kDelay + 1) / (kTM - kDelay));
+        if constexpr (kSpread) issue(kValueLoads * (i - kDelay + 1) / (kTM - kDelay));
         products<1>();
         reads<kEach>();
       }
@@ -445,7 +460,24 @@ struct Block {
     for (int i = 0; i < kTM; ++i)
 #pragma unroll
       for (int j = 0; j < kTN; ++j) asm volatile("" : "+v"(acc[i][j]));  // stays ahead of the epilogue's branches
+    if constexpr (GROUPS > 1) {
+      f32x4 *room = (f32x4 *)(lds - group() * kPart) + (wave() % kWaves) * (kTM * kTN * 64) + (threadIdx.x & 63);
+      __syncthreads();
+      if (group() > 0) {
+#pragma unroll
+        for (int i = 0; i < kTM * kTN; ++i) room[((group() - 1) * kWaves * kTM * kTN + i) * 64] = acc[i / kTN][i % kTN];
+      }
+      __syncthreads();
+      if (group() == 0) {
+#pragma unroll
+        for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+          for (int i = 0; i < kTM * kTN; ++i) acc[i / kTN][i % kTN] += room[(g * kWaves * kTM * kTN + i) * 64];
+      }
+    }
   }
+  // The waves that hold the block's sums after run().
+  __device__ __forceinline__ static bool holds() { return GROUPS == 1 || group() == 0; }
 };
 
 }  // namespace tile

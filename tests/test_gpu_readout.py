@@ -122,6 +122,26 @@ def test_loss_and_gradient(rows, classes, features, dtype):
     c.check(g)
 
 
+# few rows, few classes (both sides of what they take), features past one, four and sixteen steps of a workgroup's columns
+FEW = [(1, 300, 1024), (1, 301, 1025), (1, 70, 4097), (1, 33, 16384), (1, 33, 16385), (2, 1000, 1000), (3, 50, 1030), (4, 40, 4096), (4, 40, 4097), (5, 77, 1024), (16, 513, 1023),
+       (16, 30, 1025), (17, 30, 100), (500, 16, 1024), (301, 2, 4000), (77, 1, 9001), (40, 1, 64), (1300, 3, 65), (9, 9, 9), (2, 3000, 5000)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,classes,features", FEW)
+def test_few_rows_and_few_classes(rows, classes, features, dtype):
+    log(f"readout few {rows} x {classes} x {features} {dtype}")
+    c = Case(rows, classes, features, dtype, seed=classes, pad=rows % 3, offset=rows % 2)
+    if rows > 3:
+        c.y[1], c.y[3] = -1, classes
+        c.x[1] = float("nan")
+    c.run()
+    c.check()
+    g = c.torch.randn(rows, generator=c.torch.Generator("cuda").manual_seed(1), device="cuda")
+    c.run(g)
+    c.check(g)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (8, 0), (3, 5), (24, 8)])
 def test_strides_and_alignment(pad, offset, dtype):
