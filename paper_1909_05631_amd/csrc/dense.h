@@ -193,8 +193,8 @@ struct ShapeCost {
   int bm, bn, held;
   double full, alone;
 };
-constexpr ShapeCost kCost[kShapes] = {{256, 256, 1, 1.56, 1.56}, {256, 192, 1, 1.25, 1.25}, {192, 192, 1, 1.0, 1.0}, {128, 128, 2, 0.51, 0.65}, {128, 128, 1, 0.55, 0.55},
-                                      {64, 64, 4, 0.15, 0.25},   {64, 64, 1, 0.18, 0.18},    {32, 128, 1, 0.18, 0.18}, {128, 32, 1, 0.18, 0.18}};
+constexpr ShapeCost kCost[kShapes] = {{256, 256, 1, 1.65, 1.65}, {256, 192, 1, 1.35, 1.35}, {192, 192, 1, 1.0, 1.0}, {128, 128, 2, 0.5, 0.65}, {128, 128, 1, 0.55, 0.55},
+                                      {64, 64, 4, 0.19, 0.25},   {64, 64, 1, 0.19, 0.19},   {32, 128, 1, 0.19, 0.19}, {128, 32, 1, 0.19, 0.19}};
 
 struct Plan {
   Shape shape;
@@ -230,7 +230,7 @@ inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_split
 
 template <int KIND, bool AA, bool AB, class E>
 sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
-  constexpr int kGroups = KIND == tile::KIND_MX ? 1 : 2;  // (its scales need LDS too: two blocks a CU instead)
+  constexpr int kPair = KIND == tile::KIND_MX ? 1 : 2;  // (its scales need LDS too: two blocks a CU instead)
   switch (p.shape) {
     case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kBroad:
@@ -240,9 +240,9 @@ sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t r
     case kSquare: return launch<KIND, 128, 128, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kPaired: return launch<KIND, 128, 128, 2, 2, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kStream: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kGroups, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    default: return launch<KIND, 128, 32, 4, 1, 3, kGroups, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    default: return launch<KIND, 128, 32, 4, 1, 3, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
   }
 }
 

@@ -1,5 +1,5 @@
 // The readout of few rows or of few classes, in fp32 arithmetic without matrix tiles: the few (the "held" rows of x or of
-// w, at most 16) stay in registers, spread over a workgroup's columns, while the rows of the other matrix
+// w, at most 4) stay in registers, spread over a workgroup's columns, while the rows of the other matrix
 // stream past, each read once:
 //
 //   l_hs = held_h . stream_s           per lane over its columns, then across the workgroup
@@ -15,6 +15,8 @@
 
 #include "dense.h"
 
+#include <type_traits>
+
 namespace few {
 
 using namespace dense;
@@ -27,7 +29,7 @@ struct Few {
   int64_t ld_held, ld_stream;
   int held_rows, features;
   int64_t stream_rows;
-  bool vec_held, vec_stream;
+  bool vec_held, vec_stream;  // rows aligned for four values, features a multiple of four
   const int64_t *labels;
   int64_t classes;
   // loss
@@ -56,6 +58,34 @@ __device__ __forceinline__ f32x4 load4(const T *row, int col, int n, bool vec) {
   }
   return v;
 }
+
+// A row as a buffer: reads past its end, and all reads of a row that is left out, are zeros without a branch, so
+// that a thread's loads are all on their way at once.
+template <class T>
+struct RowBuffer {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ RowBuffer(const T *row, int n, bool live) : r(__builtin_amdgcn_make_buffer_rsrc((void *)row, 0, live ? n * (int)sizeof(T) : 0, 0x00027000)) {}
+  // VEC: the row is aligned for four values and n is a multiple of four
+  template <bool VEC>
+  __device__ __forceinline__ f32x4 load(int col) const {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const int at = col * (int)sizeof(T);
+    if constexpr (VEC && sizeof(T) == 4) {
+      return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+    } else if constexpr (VEC) {
+      return __builtin_convertvector(__builtin_bit_cast(T4, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0)), f32x4);
+    } else {
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if constexpr (sizeof(T) == 4)
+          v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at + 4 * i, 0, 0));
+        else
+          v[i] = (float)__builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, at + 2 * i, 0, 0));
+      return v;
+    }
+  }
+};
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 
@@ -94,17 +124,30 @@ __global__ __launch_bounds__(kThreads) void k_few(Few<T> p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   f32x4 held[HELD][STEPS], d_held[GRADIENT ? HELD : 1][GRADIENT ? STEPS : 1];
   int labelled = 0;
+  bool takes[HELD];  // a row without a label is zeros in the gradient, whatever it holds
 #pragma unroll
   for (int h = 0; h < HELD; ++h) {
-    const bool there = h < p.held_rows;
-    const bool live = ROWS_HELD && there && (uint64_t)p.labels[h] < (uint64_t)p.classes;
+    const bool there = h < p.held_rows, live = ROWS_HELD && there && (uint64_t)p.labels[h] < (uint64_t)p.classes;
     labelled += live;
+    takes[h] = there && (!ROWS_HELD || !GRADIENT || live);
+  }
+  const auto load_held = [&](auto vec) {
 #pragma unroll
-    for (int c = 0; c < STEPS; ++c) {
-      // a row without a label is zeros in the gradient, whatever it holds
-      held[h][c] = there && (!ROWS_HELD || !GRADIENT || live) ? load4(p.held + h * p.ld_held, (c * kThreads + tid) * 4, p.features, p.vec_held) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if constexpr (GRADIENT) d_held[h][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int h = 0; h < HELD; ++h) {
+      const RowBuffer<T> row(p.held + h * p.ld_held, p.features, takes[h]);
+#pragma unroll
+      for (int c = 0; c < STEPS; ++c) held[h][c] = row.template load<vec()>((c * kThreads + tid) * 4);
     }
+  };
+  if (p.vec_held)
+    load_held(std::true_type{});
+  else
+    load_held(std::false_type{});
+  if constexpr (GRADIENT) {
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+#pragma unroll
+      for (int c = 0; c < STEPS; ++c) d_held[h][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   // this thread's sum of a batch
   const int mine = tid < N ? tid : 0, my_h = mine / BATCH, my_s = mine % BATCH;
@@ -121,14 +164,21 @@ __global__ __launch_bounds__(kThreads) void k_few(Few<T> p) {
 
   const int64_t stride = (int64_t)gridDim.x * BATCH;
   f32x4 v[BATCH][STEPS];
-  const auto load = [&](int64_t s0) {
+  const auto load_rows = [&](int64_t s0, auto vec) {
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
       const int64_t s = s0 + b;
       const bool live = s < p.stream_rows && (ROWS_HELD || !GRADIENT || (uint64_t)p.labels[s] < (uint64_t)p.classes);
+      const RowBuffer<T> row(p.stream + s * p.ld_stream, p.features, live);
 #pragma unroll
-      for (int c = 0; c < STEPS; ++c) v[b][c] = live ? load4(p.stream + s * p.ld_stream, (c * kThreads + tid) * 4, p.features, p.vec_stream) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int c = 0; c < STEPS; ++c) v[b][c] = row.template load<vec()>((c * kThreads + tid) * 4);
     }
+  };
+  const auto load = [&](int64_t s0) {
+    if (p.vec_stream)
+      load_rows(s0, std::true_type{});
+    else
+      load_rows(s0, std::false_type{});
   };
   int64_t s0 = (int64_t)blockIdx.x * BATCH;
   load(s0);
@@ -240,12 +290,15 @@ __global__ __launch_bounds__(kThreads) void k_few(Few<T> p) {
   }
 }
 
-// The held rows and columns that registers take, and how many streamed rows go at a time.
-enum Fit { kNone, kOneShort, kOneMiddle, kOneLong, kFourShort, kFourMiddle, kSixteen };
-inline Fit fit_of(int64_t held, int64_t features) {
+// The held rows and columns that registers take, and how many streamed rows go at a time. Up to 4 rows in fp32, where the
+// tiles first write the other matrix in two parts (65536 x 1024: loss 45 us for one row and 130 for four, 225 in
+// tiles); one row in bf16, whose gradient here has no rounding between its sums (88 us, 102 in tiles; the
+// tiles stream the loss of one row at 5.2 TB/s, this at 3.6, and are far ahead from two rows on).
+enum Fit { kNone, kOneShort, kOneMiddle, kOneLong, kFourShort, kFourMiddle };
+inline Fit fit_of(int64_t held, int64_t features, int32_t dtype) {
   if (held <= 1) return features <= kColumns ? kOneShort : features <= 4 * kColumns ? kOneMiddle : features <= 16 * kColumns ? kOneLong : kNone;
-  if (held <= 4) return features <= kColumns ? kFourShort : features <= 4 * kColumns ? kFourMiddle : kNone;
-  return held <= 16 && features <= kColumns ? kSixteen : kNone;
+  if (held <= 4 && dtype == SDNN_FP32) return features <= kColumns ? kFourShort : features <= 4 * kColumns ? kFourMiddle : kNone;
+  return kNone;
 }
 inline int batch_of(Fit f) { return f == kOneShort ? 8 : f == kFourShort ? 4 : f == kOneLong ? 1 : 2; }
 // Workgroups: two a CU (each has 16 KB or more of rows on its way), one where each leaves a slab.
@@ -260,9 +313,12 @@ sdnn_status launch(Fit fit, const Few<T> &p, hipStream_t stream, const char *wha
     case kOneShort: hipLaunchKernelGGL((k_few<T, 1, 1, 8, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p); break;
     case kOneMiddle: hipLaunchKernelGGL((k_few<T, 1, 4, 2, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p); break;
     case kOneLong: hipLaunchKernelGGL((k_few<T, 1, 16, 1, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p); break;
-    case kFourShort: hipLaunchKernelGGL((k_few<T, 4, 1, 4, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p); break;
-    case kFourMiddle: hipLaunchKernelGGL((k_few<T, 4, 4, 2, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p); break;
-    default: hipLaunchKernelGGL((k_few<T, 16, 1, 2, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p); break;
+    case kFourShort:
+      if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_few<T, 4, 1, 4, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p);
+      break;
+    default:
+      if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_few<T, 4, 4, 2, ROWS_HELD, GRADIENT>), grid, threads, 0, stream, p);
+      break;
   }
   return launched(what);
 }

@@ -16,7 +16,7 @@
 // w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G: it stays in the Infinity Cache
 // between the products.
 //
-// Few rows or few classes (at most 16, few.h) have no use for tiles: one kernel with fp32 arithmetic streams the
+// Few rows or few classes (few.h) have no use for tiles: one kernel with fp32 arithmetic streams the
 // other matrix past them, once.
 #include "dense.h"
 #include "few.h"
@@ -457,8 +457,8 @@ struct Sizes {
   Plan dw(int64_t n) const { return plan(kind(), n, features, rows, kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
   // Few rows are held rather than few classes.
-  bool rows_held() const { return few::fit_of(rows, features) != few::kNone && (rows <= classes || few::fit_of(classes, features) == few::kNone); }
-  few::Fit few() const { return few::fit_of(rows_held() ? rows : classes, features); }
+  bool rows_held() const { return few::fit_of(rows, features, dtype) != few::kNone && (rows <= classes || few::fit_of(classes, features, dtype) == few::kNone); }
+  few::Fit few() const { return few::fit_of(rows_held() ? rows : classes, features, dtype); }
 };
 
 bool usable_in_place(const void *p, int64_t ld, int64_t cols) {
@@ -544,8 +544,8 @@ few::Few<T> few_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t 
   p.held_rows = (int)(rows ? s.rows : s.classes);
   p.stream_rows = rows ? s.classes : s.rows;
   p.features = (int)s.features;
-  p.vec_held = vector_rows(p.held, p.ld_held);
-  p.vec_stream = vector_rows(p.stream, p.ld_stream);
+  p.vec_held = s.features % 4 == 0 && vector_rows(p.held, p.ld_held);
+  p.vec_stream = s.features % 4 == 0 && vector_rows(p.stream, p.ld_stream);
   p.labels = labels;
   p.classes = s.classes;
   return p;

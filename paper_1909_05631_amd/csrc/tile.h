@@ -101,7 +101,7 @@ struct Loader {
   int row;
 
   __device__ __forceinline__ void init(const Operand &op) {
-    const int t = threadIdx.x;
+    const int t = threadIdx.x % THREADS;
     row = t / (kRowBytes / 16);
     const int c = t % (kRowBytes / 16);
     chunk = ACROSS ? c ^ ((row << 1) & kTurn) : c ^ (row & 7);
@@ -152,7 +152,7 @@ struct ScaleLoader {
   int half;  // of the slab's 8 bytes
 
   __device__ __forceinline__ void init(const Operand &op) {
-    const int row = threadIdx.x >> 1;
+    const int row = threadIdx.x % THREADS >> 1;
     half = threadIdx.x & 1;
     offset = row < ROWS ? row * (op.pitch / 16) + half * 4 : kOut;
   }
@@ -258,31 +258,32 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 // clock to 1.9 GHz under them; at 1570 for the library's kernel in the same run), KIND_SPLIT 1430, 477 of fp32.
 // Four waves of 128 x 128 read less LDS and measured 1010, raised wave priorities during the products 7% less.
 //
-// GROUPS of WM x WN waves may share the block's outputs, each taking every GROUPS-th slab of the same stage, with their
-// sums joined through LDS at the end: a launch of few blocks runs through k in fewer meetings.
+// GROUPS of WM x WN waves may share the block's outputs, each loading and taking every GROUPS-th slab, with their sums joined
+// through LDS at the end: a launch of few blocks runs through k in fewer meetings.
 template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, int STAGES, int GROUPS = 1>
 struct Block {
-  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves * GROUPS;
+  static constexpr int kWaves = WM * WN, kGroup = 64 * kWaves, kThreads = kGroup * GROUPS;
   static constexpr int kTM = BM / WM / 16, kTN = BN / WN / 16;
-  using LoadA = Loader<KIND, BM, ACROSS_A, kThreads>;
-  using LoadB = Loader<KIND, BN, ACROSS_B, kThreads>;
-  using ScaleA = ScaleLoader<BM, kThreads>;
-  using ScaleB = ScaleLoader<BN, kThreads>;
+  using LoadA = Loader<KIND, BM, ACROSS_A, kGroup>;
+  using LoadB = Loader<KIND, BN, ACROSS_B, kGroup>;
+  using ScaleA = ScaleLoader<BM, kGroup>;
+  using ScaleB = ScaleLoader<BN, kGroup>;
   static constexpr bool kMx = KIND == KIND_MX;
   static constexpr int kValuesA = LoadA::kBytes, kValues = kValuesA + LoadB::kBytes;
   static constexpr int kPart = kValues + (kMx ? ScaleA::kBytes + ScaleB::kBytes : 0);  // a group's slab
   static constexpr int kStage = GROUPS * kPart;
   static constexpr int kLds = STAGES * kStage;
   static_assert(kLds <= 160 * 1024, "LDS of a CU");
-  static constexpr int kLoads = GROUPS * (LoadA::kRounds + LoadB::kRounds + (kMx ? ScaleA::kRounds + ScaleB::kRounds : 0));  // of a wave and stage
+  static constexpr int kLoads = LoadA::kRounds + LoadB::kRounds + (kMx ? ScaleA::kRounds + ScaleB::kRounds : 0);  // of a wave and stage
   static_assert(GROUPS == 1 || kStage * STAGES >= (GROUPS - 1) * BM * BN * 4, "the sums' room");
 
   f32x4 acc[kTM][kTN];
 
   __device__ __forceinline__ static int wave() { return uniform(threadIdx.x >> 6); }
-  __device__ __forceinline__ static int group() { return wave() / kWaves; }
-  __device__ __forceinline__ static int row0() { return (wave() % kWaves / WN) * (BM / WM); }
-  __device__ __forceinline__ static int col0() { return (wave() % WN) * (BN / WN); }
+  __device__ __forceinline__ static int group() { return GROUPS == 1 ? 0 : wave() / kWaves; }
+  __device__ __forceinline__ static int member() { return GROUPS == 1 ? wave() : wave() % kWaves; }
+  __device__ __forceinline__ static int row0() { return (member() / WN) * (BM / WM); }
+  __device__ __forceinline__ static int col0() { return (member() % WN) * (BN / WN); }
 
   template <class R>
   __device__ __forceinline__ static void read(const R &r, const char *lds, int q, i32x4 (&f)[kTN]) {
@@ -346,25 +347,23 @@ struct Block {
 #pragma unroll
       for (int j = 0; j < kTN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (s0 >= s1) return;
-    const int base = uniform((int)(uintptr_t)(lds_char *)lds), mine = base + wave() * 1024;
+    lds += group() * kPart;
+    s0 += group();
+    const int base = uniform((int)(uintptr_t)(lds_char *)lds), mine = base + member() * 1024;
     const auto load_scales = [&](int s, int to) {
       if constexpr (kMx) {
-        const int at = base + to + kValues + wave() * 256;
+        const int at = base + to + kValues + member() * 256;
         lsa.load(a, s, at);
         lsb.load(b, s, at + ScaleA::kBytes);
       }
     };
     const auto load = [&](int s, int to) {
-#pragma unroll
-      for (int g = 0; g < GROUPS; ++g) {
-        load_scales(s + g, to + g * kPart);
-        la.load(a, s + g, mine + to + g * kPart);
-        lb.load(b, s + g, mine + to + g * kPart + kValuesA);
-      }
+      load_scales(s, to);
+      la.load(a, s, mine + to);
+      lb.load(b, s, mine + to + kValuesA);
     };
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) load(s0 + i * GROUPS, i * kStage);
-    lds += group() * kPart;
     wait_loads<(STAGES - 1) * kLoads>();
     meet();
     constexpr int kEach = kMx ? 2 : ACROSS_A ? 2 : 1;                      // LDS reads with a subtile of A
@@ -379,7 +378,7 @@ struct Block {
 #pragma unroll
     for (int j = 0; j < kTN; ++j) sb[j] = kMx ? read_scale(lds + kValues + ScaleA::kBytes, col0(), j) : 0;
     int at = 0;
-    for (int s = s0; s < s1; s += GROUPS) {
+    for (int s = s0; s < s1 + group(); s += GROUPS) {  // as often in every group: past s1 a slab is zeros
       const int used = at * kStage;
       const char *now = lds + used;
       at = at + 1 == STAGES ? 0 : at + 1;
@@ -461,7 +460,7 @@ struct Block {
 #pragma unroll
       for (int j = 0; j < kTN; ++j) asm volatile("" : "+v"(acc[i][j]));  // stays ahead of the epilogue's branches
     if constexpr (GROUPS > 1) {
-      f32x4 *room = (f32x4 *)(lds - group() * kPart) + (wave() % kWaves) * (kTM * kTN * 64) + (threadIdx.x & 63);
+      f32x4 *room = (f32x4 *)(lds - group() * kPart) + member() * (kTM * kTN * 64) + (threadIdx.x & 63);
       __syncthreads();
       if (group() > 0) {
 #pragma unroll
