@@ -72,6 +72,49 @@ __device__ __forceinline__ void store4(__bf16 *p, f32x4 v, int n, bool vec) {
   }
 }
 
+// A subtile row of a block's results, columns [col, col + 16 * N) of row `to`, by the four lane groups that hold it: for
+// bf16 neighbouring groups exchange halves of two subtiles, so that a lane stores 16 bytes.
+template <class T, int N, class F>
+__device__ __forceinline__ void store_row(T *to, int64_t col, int64_t cols, bool vec, bool in, const F &value) {
+  const int j4 = (threadIdx.x & 63) >> 4;
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      typedef int i32x4 __attribute__((ext_vector_type(4)));
+      const i32x2 a = __builtin_bit_cast(i32x2, __builtin_convertvector(value(j), bf16x4)), b = __builtin_bit_cast(i32x2, __builtin_convertvector(value(j + 1), bf16x4));
+      const bool odd = j4 & 1;  // even groups take subtile j's 8 columns from 4 j4 on, odd ones subtile j + 1's from 4 (j4 - 1) on
+      i32x2 pass, own, got;
+      pass[0] = odd ? a[0] : b[0];
+      pass[1] = odd ? a[1] : b[1];
+      own[0] = odd ? b[0] : a[0];
+      own[1] = odd ? b[1] : a[1];
+      got[0] = __shfl_xor(pass[0], 16);
+      got[1] = __shfl_xor(pass[1], 16);
+      const int64_t c = col + 16 * (j + odd) + 4 * (j4 & 2);
+      const i32x4 both = odd ? i32x4{got[0], got[1], own[0], own[1]} : i32x4{own[0], own[1], got[0], got[1]};
+      if (in && c < cols) {
+        if (vec && c + 8 <= cols) {
+          *(i32x4 *)(to + c) = both;
+        } else {
+          typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+          const bf16x8 v = __builtin_bit_cast(bf16x8, both);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c + i < cols) to[c + i] = v[i];
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int64_t c = col + 16 * j + 4 * j4;
+      const f32x4 v = value(j);
+      if (in && c < cols) store4(to + c, v, (int)(cols - c < 4 ? cols - c : 4), vec);
+    }
+  }
+}
+
 // Where value k of a row lies in the split form: groups of 32 values, 64 bytes of high parts, 64 of low ones.
 __device__ __forceinline__ int64_t split_at(int64_t k) { return (k >> 5) * 128 + (k & 31) * 2; }
 constexpr int kLow = 64;
@@ -213,7 +256,8 @@ inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_split
     const ShapeCost &c = kCost[s];
     if ((symmetric && c.bm != c.bn) || ((s == kMiddle || s == kBroad) && form != kAlong)) continue;
     const double across = (double)ceil_div(cols, c.bn), blocks = symmetric ? across * (across + 1) / 2 : (double)ceil_div(rows, c.bm) * across;
-    for (int split = 1; split <= most_splits && (split == 1 || split * 2 <= slabs); ++split) {
+    for (int split : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+      if (split > most_splits || (split > 1 && split * 2 > slabs)) break;
       const double n = blocks * split * batch, rounds = std::ceil(n / (kCus * c.held));
       const double held = std::min<double>(c.held, std::ceil(n / kCus));
       // (a round's first loads and last stores overlap with other blocks' work where a CU holds several)

@@ -113,17 +113,10 @@ struct Store {
   bool vec;
   template <class B>
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
-    const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
-      const int64_t r = row0 + 16 * i + i16;
-      if (r >= rows) continue;
-#pragma unroll
-      for (int j = 0; j < B::kTN; ++j) {
-        const int64_t c = col0 + 16 * j + 4 * j4;
-        if (c >= cols) continue;
-        store4(out + r * ld + c, block.acc[i][j], (int)(cols - c < 4 ? cols - c : 4), vec);
-      }
+      const int64_t r = row0 + 16 * i + (threadIdx.x & 15);
+      store_row<T, B::kTN>(out + r * ld, col0, cols, vec, r < rows, [&](int j) { return block.acc[i][j]; });
     }
   }
 };
@@ -132,7 +125,7 @@ template <class T>
 sdnn_status product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales, int64_t rows, int64_t outputs, int64_t n, T *out, int64_t ld, hipStream_t stream) {
   const int64_t pitch = blocks_of(n) * 16;
   const Matrix a{(const char *)x_codes, pitch, rows, pitch, 0, x_scales}, b{(const char *)w_codes, pitch, outputs, pitch, 0, w_scales};
-  const Store<T> e{out, ld, rows, outputs, (uintptr_t)out % (4 * sizeof(T)) == 0 && ld % 4 == 0};
+  const Store<T> e{out, ld, rows, outputs, (uintptr_t)out % 16 == 0 && ld * sizeof(T) % 16 == 0};
   return run_shape<KIND_MX, false, false>(plan(KIND_MX, rows, outputs, n, 1, kAlong), a, b, rows, outputs, n, e, stream, "product");
 }
 

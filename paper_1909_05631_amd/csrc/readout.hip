@@ -299,14 +299,11 @@ struct WriteGrad {
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t t = row0 + 16 * i + i16;
-      if (t >= rows) continue;
-      const int64_t y = labels[t] - first;
-      const bool live = counted(labels, t, all);
+      const bool in = t < rows, live = in && counted(labels, t, all);
+      const int64_t y = in ? labels[t] - first : -1;
       const float z = live ? lse[t] : 0.0f;
-      float w = live ? (weights ? weights[t] : mean) : 0.0f;
-      if (KIND == KIND_SPLIT) w = 1 << kGradExponent;
-#pragma unroll
-      for (int j = 0; j < B::kTN; ++j) {
+      const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : live ? (weights ? weights[t] : mean) : 0.0f;
+      const auto value = [&](int j) {
         const int64_t v = col0 + 16 * j + 4 * j4;
         f32x4 o;
 #pragma unroll
@@ -316,11 +313,17 @@ struct WriteGrad {
           const float p = exp_of(s - z) - (v + c == y ? 1.0f : 0.0f);
           o[c] = live && v + c < classes ? w * p : 0.0f;
         }
-        if constexpr (KIND == KIND_SPLIT) {
-          if (split_at(v) < pitch) store_split4(g + t * pitch, v, o);
-        } else {
-          if (2 * v < pitch) store4((__bf16 *)(g + t * pitch) + v, o, 4, true);
+        return o;
+      };
+      if constexpr (KIND == KIND_SPLIT) {
+#pragma unroll
+        for (int j = 0; j < B::kTN; ++j) {
+          const int64_t v = col0 + 16 * j + 4 * j4;
+          const f32x4 o = value(j);
+          if (in && split_at(v) < pitch) store_split4(g + t * pitch, v, o);
         }
+      } else {
+        store_row<__bf16, B::kTN>((__bf16 *)(g + t * pitch), col0, pitch / 2, true, in, value);
       }
     }
   }
@@ -351,21 +354,23 @@ struct Store {
   int64_t ld, rows, cols;
   bool vec;
   OutScale scale;
+  const float *before = nullptr;  // sums of the pieces before
+  int64_t ld_before = 0;
   template <class B>
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
-    const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
+    const int i16 = threadIdx.x & 15;
     const OutScale::Found found = scale.find();
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t r = row0 + 16 * i + i16;
-      if (r >= rows) continue;
-      const float w = scale.weight(r);
-#pragma unroll
-      for (int j = 0; j < B::kTN; ++j) {
-        const int64_t c = col0 + 16 * j + 4 * j4;
-        if (c >= cols) continue;
-        store4(out + r * ld + c, scale.apply(found, w, block.acc[i][j]), (int)(cols - c < 4 ? cols - c : 4), vec);
-      }
+      const bool in = r < rows;
+      const float w = in ? scale.weight(r) : 0.0f;
+      store_row<T, B::kTN>(out + r * ld, col0, cols, vec, in, [&](int j) {
+        f32x4 v = block.acc[i][j];
+        const int64_t c = col0 + 16 * j + 4 * ((threadIdx.x & 63) >> 4);
+        if (before && in && c < ld_before) v += *(const f32x4 *)(before + r * ld_before + c);
+        return scale.apply(found, w, v);
+      });
     }
   }
 };
@@ -465,7 +470,9 @@ bool usable_in_place(const void *p, int64_t ld, int64_t cols) {
   return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld * 2 <= kMaxPitch;
 }
 
+// A call's workspace and the plans of its products.
 struct LossSpace {
+  Plan loss{};
   char *x, *w;
   int *ex, *ew;
   float2 *parts;
@@ -473,17 +480,19 @@ struct LossSpace {
   int64_t count;
   LossSpace(Carver &c, const Sizes &s) {
     const bool packed = s.few() == few::kNone;
+    if (packed) loss = s.loss();
     x = c.take<char>(packed ? s.packed(s.rows) : 0);
     w = c.take<char>(packed ? s.packed(s.classes) : 0);
     ex = c.take<int>(s.rows);
     ew = c.take<int>(s.classes);
-    count = !packed ? (s.rows_held() ? (int64_t)few::grid_of(s.few(), s.classes, false) * few::batch_of(s.few()) : 0) : ceil_div(s.classes, kWaveCols[s.loss().shape]);
+    count = !packed ? (s.rows_held() ? (int64_t)few::grid_of(s.few(), s.classes, false) * few::batch_of(s.few()) : 0) : ceil_div(s.classes, kWaveCols[loss.shape]);
     parts = c.take<float2>(s.rows * count);
     picked = c.take<float>(s.rows);
   }
 };
 
 struct GradSpace {
+  Plan logits[2], dx_plan, dw_plan[2];  // of a whole piece and of the last one
   char *x, *w, *xg, *g;
   Scalars *scalars;
   float *dx, *dw, *few;
@@ -498,11 +507,16 @@ struct GradSpace {
     w = c.take<char>(s.packed(s.classes));
     xg = c.take<char>(s.dtype == SDNN_FP32 ? s.packed(s.rows) : 0);
     g = c.take<char>((size_t)(s.rows * s.g_pitch()));
-    dx = c.take<float>(s.dx().splits > 1 || s.piece() < s.classes ? (size_t)(s.dx().splits * s.rows * s.ld_slab()) : 0);
+    const int64_t piece = s.piece(), rest = s.classes % piece;
+    dx_plan = s.dx();
+    dx = c.take<float>(dx_plan.splits > 1 || piece < s.classes ? (size_t)(dx_plan.splits * s.rows * s.ld_slab()) : 0);
     size_t most = 0;
-    for (int64_t n : {s.piece(), s.classes % std::max<int64_t>(1, s.piece())}) {
-      const Plan p = s.dw(n);
-      if (n > 0 && p.splits > 1) most = std::max(most, (size_t)(p.splits * n * s.ld_slab()));
+    for (int i = 0; i < 2; ++i) {
+      const int64_t n = i == 0 ? piece : rest;
+      if (n == 0) continue;
+      logits[i] = s.logits(n);
+      dw_plan[i] = s.dw(n);
+      if (dw_plan[i].splits > 1) most = std::max(most, (size_t)(dw_plan[i].splits * n * s.ld_slab()));
     }
     dw = c.take<float>(most);
   }
@@ -529,8 +543,8 @@ void split_rows(const Rows &x, const Rows &w, const Rows &xg, const Sizes &s, hi
 }
 
 template <class T>
-bool vector_rows(const T *p, int64_t ld) {
-  return (uintptr_t)p % (4 * sizeof(T)) == 0 && ld % 4 == 0;
+bool vector_rows(const T *p, int64_t ld) {  // aligned for 16 bytes
+  return (uintptr_t)p % 16 == 0 && ld * sizeof(T) % 16 == 0;
 }
 
 template <class T>
@@ -552,9 +566,12 @@ few::Few<T> few_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t 
 }
 
 template <int KIND, class T>
-sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t ldw, const int64_t *labels, float *loss, float *lse, void *workspace, hipStream_t stream) {
+sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t ldw, const int64_t *labels, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                    hipStream_t stream) {
   Carver carver{(char *)workspace};
   const LossSpace sp(carver, s);
+  sdnn_status st = check_workspace(workspace, workspace_bytes, carver.used);
+  if (st != SDNN_OK) return st;
   if (s.few() != few::kNone) {
     few::Few<T> p = few_of(s, x, ldx, w, ldw, labels);
     p.loss = loss;
@@ -562,7 +579,7 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     p.parts = sp.parts;
     p.picked = sp.picked;
     if (!s.rows_held()) return few::launch<false, false>(s.few(), p, stream, "loss");
-    const sdnn_status st = few::launch<true, false>(s.few(), p, stream, "loss");
+    st = few::launch<true, false>(s.few(), p, stream, "loss");
     return st != SDNN_OK ? st : join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
   }
   Matrix a, b;
@@ -576,10 +593,9 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     a = split_matrix(rx, s);
     b = split_matrix(rw, s);
   }
-  sdnn_status st = launched("rows");
-  if (st != SDNN_OK) return st;
+  if ((st = launched("rows")) != SDNN_OK) return st;
   const LossParts<KIND> e{{sp.ex, sp.ew, nullptr, nullptr}, labels, s.rows, s.classes, sp.parts, sp.count, sp.picked};
-  st = run_shape<KIND, false, false>(s.loss(), a, b, s.rows, s.classes, s.features, e, stream, "loss");
+  st = run_shape<KIND, false, false>(sp.loss, a, b, s.rows, s.classes, s.features, e, stream, "loss");
   if (st != SDNN_OK) return st;
   return join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
 }
@@ -602,9 +618,11 @@ __global__ __launch_bounds__(256) void k_zero_rows(T *out, int64_t ld, int64_t r
 
 template <int KIND, class T>
 sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t ldw, const int64_t *labels, const float *lse, const float *weights, T *dx, int64_t lddx, T *dw, int64_t lddw,
-                    void *workspace, hipStream_t stream) {
+                    void *workspace, size_t workspace_bytes, hipStream_t stream) {
   Carver carver{(char *)workspace};
   const GradSpace sp(carver, s);
+  sdnn_status st = check_workspace(workspace, workspace_bytes, carver.used);
+  if (st != SDNN_OK) return st;
   if (s.rows == 0) {
     if (dw) hipLaunchKernelGGL((k_zero_rows<T>), dim3(row_grid(s.classes)), dim3(256), 0, stream, dw, lddw, s.classes, s.features);
     return launched("gradient");
@@ -623,7 +641,7 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     p.slabs = d_held ? sp.few : nullptr;
     p.ld_slab = s.ld_slab();
     if (!held && !weights) hipLaunchKernelGGL(k_count, dim3(1), dim3(256), 0, stream, labels, s.rows, s.classes, sp.scalars);
-    const sdnn_status st = held ? few::launch<true, true>(s.few(), p, stream, "gradient") : few::launch<false, true>(s.few(), p, stream, "gradient");
+    st = held ? few::launch<true, true>(s.few(), p, stream, "gradient") : few::launch<false, true>(s.few(), p, stream, "gradient");
     if (st != SDNN_OK || !d_held) return st;
     const Store<T> to{d_held, ld_d_held, p.held_rows, s.features, vector_rows(d_held, ld_d_held), {nullptr, nullptr, nullptr}};
     return sum_slabs(sp.few, (int)few::grid_of(s.few(), p.stream_rows, true), s.ld_slab(), to, stream, "gradient");
@@ -651,10 +669,10 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     b = split_matrix(rw, s);
     ag = weighted ? split_matrix(rg, s) : a;
   }
-  sdnn_status st = launched("gradient");
+  st = launched("gradient");
   const float *mean = KIND == KIND_SPLIT && !weights ? &sp.scalars->mean : nullptr;
   const float *row_weights = KIND == KIND_SPLIT ? weights : nullptr;
-  const Plan px = s.dx();
+  const Plan &px = sp.dx_plan;
   const int64_t piece = s.piece();
   const bool through_x = px.splits > 1 || piece < s.classes;
   for (int64_t v0 = 0; v0 < s.classes && st == SDNN_OK; v0 += piece) {
@@ -664,16 +682,17 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     wp.data += v0 * b.pitch;
     wp.rows = n;
     const WriteGrad<KIND> e{{nullptr, nullptr, top_x, top_w}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
-    st = run_shape<KIND, false, false>(s.logits(n), a, wp, s.rows, n, s.features, e, stream, "gradient");
+    st = run_shape<KIND, false, false>(sp.logits[n < piece], a, wp, s.rows, n, s.features, e, stream, "gradient");
     if (st != SDNN_OK) return st;
     const int64_t wide = KIND == KIND_SPLIT ? ceil_div(n, 32) * 128 : ceil_div(n, 8) * 16;  // bytes of a row of G
     if (dx) {
-      const Store<T> to{dx, lddx, s.rows, s.features, vector_rows(dx, lddx), {row_weights, mean, top_w}};
-      st = product<KIND, false>(px, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, wp, n, sp.dx, s.ld_slab(), through_x, v0 > 0, last, to, stream, "gradient of the rows");
+      const Store<T> to{dx, lddx, s.rows, s.features, vector_rows(dx, lddx), {row_weights, mean, top_w}, v0 > 0 && px.splits == 1 ? sp.dx : nullptr, s.ld_slab()};
+      const bool direct = !through_x || (last && px.splits == 1);
+      st = product<KIND, false>(px, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, wp, n, sp.dx, s.ld_slab(), !direct, v0 > 0, last, to, stream, "gradient of the rows");
       if (st != SDNN_OK) return st;
     }
     if (dw) {
-      const Plan pw = s.dw(n);
+      const Plan &pw = sp.dw_plan[n < piece];
       const Store<T> to{dw + v0 * lddw, lddw, n, s.features, vector_rows(dw + v0 * lddw, lddw), {nullptr, mean, top_g}};
       st = product<KIND, true>(pw, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, ag, s.rows, sp.dw, s.ld_slab(), pw.splits > 1, false, true, to, stream, "gradient of the weights");
     }
@@ -711,10 +730,9 @@ sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t
   if ((st = check_matrix("w", w, ldw, n_features, dtype)) != SDNN_OK) return st;
   if (!labels || !loss) return fail(SDNN_EINVAL, "labels or loss is null");
   const Sizes s{n_rows, n_classes, n_features, dtype};
-  if ((st = check_workspace(workspace, workspace_bytes, sdnn_readout_workspace_bytes(n_rows, n_classes, n_features, dtype, 0))) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  return dtype == SDNN_BF16 ? loss_of<KIND_BF16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, loss, lse, workspace, stream)
-                            : loss_of<KIND_SPLIT>(s, (const float *)x, ldx, (const float *)w, ldw, labels, loss, lse, workspace, stream);
+  return dtype == SDNN_BF16 ? loss_of<KIND_BF16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream)
+                            : loss_of<KIND_SPLIT>(s, (const float *)x, ldx, (const float *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream);
 }
 
 sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t dtype, const int64_t *labels, const float *lse, const float *row_grad, int64_t n_rows,
@@ -730,11 +748,10 @@ sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t
   if (dw && (st = check_matrix("dw", dw, lddw, n_features, dtype)) != SDNN_OK) return st;
   if ((!dx || n_rows == 0) && !dw) return SDNN_OK;
   const Sizes s{n_rows, n_classes, n_features, dtype};
-  if ((st = check_workspace(workspace, workspace_bytes, sdnn_readout_workspace_bytes(n_rows, n_classes, n_features, dtype, 1))) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (dtype == SDNN_BF16)
-    return grad_of<KIND_BF16, __bf16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, lse, row_grad, (__bf16 *)dx, lddx, (__bf16 *)dw, lddw, workspace, stream);
-  return grad_of<KIND_SPLIT, float>(s, (const float *)x, ldx, (const float *)w, ldw, labels, lse, row_grad, (float *)dx, lddx, (float *)dw, lddw, workspace, stream);
+    return grad_of<KIND_BF16, __bf16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, lse, row_grad, (__bf16 *)dx, lddx, (__bf16 *)dw, lddw, workspace, workspace_bytes, stream);
+  return grad_of<KIND_SPLIT, float>(s, (const float *)x, ldx, (const float *)w, ldw, labels, lse, row_grad, (float *)dx, lddx, (float *)dw, lddw, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

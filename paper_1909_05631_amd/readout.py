@@ -14,36 +14,39 @@ DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
 def _dtype(t: torch.dtype) -> int:
-    if t not in DTYPES:
+    code = DTYPES.get(t)
+    if code is None:
         raise ValueError(f"{t} is neither float32 nor bfloat16")
-    return DTYPES[t]
+    return code
 
 
 def _on_gpu(name: str, t, like=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} is no tensor on the GPU")
-    if like is not None and t.device != like.device:
+    if like is not None and t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
 
 
-def _rows(name: str, t, shape, dtype, like=None) -> tuple[int, int]:
-    """Address and row stride of a matrix of `shape` (None: any) and `dtype`."""
+def _rows(name: str, t, rows, cols, dtype, like=None) -> tuple[int, int]:
+    """Address and row stride of a matrix of rows x cols (None: any) and `dtype`."""
     _on_gpu(name, t, like)
-    if t.dim() != 2 or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name} has shape {tuple(shape)}, not ({rows}, {cols})")
     if t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype}, not {dtype}")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    m, n = shape
+    ld, step = t.stride()
+    if n > 1 and step != 1:
         raise ValueError(f"the values within a row of {name} are not contiguous")
-    if rows > 1 and t.stride(0) < cols:
+    if m > 1 and ld < n:
         raise ValueError(f"the rows of {name} overlap")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), ld if m > 1 else n
 
 
 def _vector(name: str, t, n: int, dtype, like) -> int:
     _on_gpu(name, t, like)
-    if tuple(t.shape) != (n,) or t.dtype != dtype or (n > 1 and t.stride(0) != 1):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name} is not {n} contiguous values of {dtype}")
     return t.data_ptr()
 
@@ -53,6 +56,18 @@ def _workspace(t, like) -> tuple[int | None, int]:
     if not t.is_contiguous():
         raise ValueError("workspace is not contiguous")
     return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _call(like, name: str, *args) -> None:
+    """The library's call, on the device of `like`."""
+    entry = getattr(load_library(), name)
+    if torch.cuda.current_device() == like.get_device():
+        status = entry(*args)
+    else:
+        with torch.cuda.device(like.device):
+            status = entry(*args)
+    if status:
+        _check(status)
 
 
 def workspace_bytes(n_rows: int, n_classes: int, n_features: int, dtype: torch.dtype, gradient: bool = True) -> int:
@@ -66,14 +81,12 @@ def loss(x, w, labels, loss, lse, workspace, stream=None) -> None:
     lse (or None): float32, written."""
     _on_gpu("x", x)
     dt = _dtype(x.dtype)
-    px, ldx = _rows("x", x, (None, None), x.dtype)
-    pw, ldw = _rows("w", w, (None, x.shape[1]), x.dtype, x)
-    n, ws = x.shape[0], _workspace(workspace, x)
-    with torch.cuda.device(x.device):
-        _check(load_library().sdnn_readout_loss(
-            px, ldx, pw, ldw, dt, _vector("labels", labels, n, torch.int64, x), n, w.shape[0], x.shape[1],
-            _vector("loss", loss, n, torch.float32, x), None if lse is None else _vector("lse", lse, n, torch.float32, x),
-            *ws, _stream_handle(stream)))
+    px, ldx = _rows("x", x, None, None, x.dtype)
+    n, d = x.shape
+    pw, ldw = _rows("w", w, None, d, x.dtype, x)
+    _call(x, "sdnn_readout_loss", px, ldx, pw, ldw, dt, _vector("labels", labels, n, torch.int64, x), n, w.shape[0], d,
+          _vector("loss", loss, n, torch.float32, x), None if lse is None else _vector("lse", lse, n, torch.float32, x),
+          *_workspace(workspace, x), _stream_handle(stream))
 
 
 def gradient(x, w, labels, lse, dx, dw, workspace, row_grad=None, stream=None) -> None:
@@ -81,16 +94,15 @@ def gradient(x, w, labels, lse, dx, dw, workspace, row_grad=None, stream=None) -
     written to dx and dw (either may be None) in their type; lse as `loss` left it."""
     _on_gpu("x", x)
     dt = _dtype(x.dtype)
-    px, ldx = _rows("x", x, (None, None), x.dtype)
-    pw, ldw = _rows("w", w, (None, x.shape[1]), x.dtype, x)
-    pdx, lddx = (None, 0) if dx is None else _rows("dx", dx, x.shape, x.dtype, x)
-    pdw, lddw = (None, 0) if dw is None else _rows("dw", dw, w.shape, x.dtype, x)
-    n, ws = x.shape[0], _workspace(workspace, x)
-    with torch.cuda.device(x.device):
-        _check(load_library().sdnn_readout_grad(
-            px, ldx, pw, ldw, dt, _vector("labels", labels, n, torch.int64, x), _vector("lse", lse, n, torch.float32, x),
-            None if row_grad is None else _vector("row_grad", row_grad, n, torch.float32, x), n, w.shape[0], x.shape[1],
-            pdx, lddx, pdw, lddw, *ws, _stream_handle(stream)))
+    px, ldx = _rows("x", x, None, None, x.dtype)
+    n, d = x.shape
+    pw, ldw = _rows("w", w, None, d, x.dtype, x)
+    v = w.shape[0]
+    pdx, lddx = (None, 0) if dx is None else _rows("dx", dx, n, d, x.dtype, x)
+    pdw, lddw = (None, 0) if dw is None else _rows("dw", dw, v, d, x.dtype, x)
+    _call(x, "sdnn_readout_grad", px, ldx, pw, ldw, dt, _vector("labels", labels, n, torch.int64, x),
+          _vector("lse", lse, n, torch.float32, x), None if row_grad is None else _vector("row_grad", row_grad, n, torch.float32, x),
+          n, v, d, pdx, lddx, pdw, lddw, *_workspace(workspace, x), _stream_handle(stream))
 
 
 def orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
@@ -104,7 +116,7 @@ def _matrices(name: str, t, like=None) -> tuple[int, int, int]:
         raise ValueError(f"{name} is neither a matrix nor a batch of them")
     if t.numel() == 0:
         raise ValueError(f"{name} is empty")
-    p, ld = _rows(name, t if t.dim() == 2 else t[0], (None, None), t.dtype)
+    p, ld = _rows(name, t if t.dim() == 2 else t[0], None, None, t.dtype)
     return p, ld, t.stride(0) if t.dim() == 3 else 0
 
 
@@ -119,15 +131,13 @@ def orthogonalize(g, out, workspace, steps: int = 5, coefficients=(3.4445, -4.77
     po, ldo, batch_o = _matrices("out", out, g)
     batch, (rows, cols) = g.shape[0] if g.dim() == 3 else 1, g.shape[-2:]
     coef = (ctypes.c_float * 3)(*coefficients)
-    ws = _workspace(workspace, g)
-    with torch.cuda.device(g.device):
-        _check(load_library().sdnn_orthogonalize(pg, ldg, batch_g, po, ldo, batch_o, dt, batch, rows, cols, steps, coef, eps,
-                                                 *ws, _stream_handle(stream)))
+    _call(g, "sdnn_orthogonalize", pg, ldg, batch_g, po, ldo, batch_o, dt, batch, rows, cols, steps, coef, eps,
+          *_workspace(workspace, g), _stream_handle(stream))
 
 
 def mx_blocks(n_values: int) -> int:
-    """Blocks of 32 values that hold a row of n_values: 16 bytes of codes and one of scale each."""
-    return int(load_library().sdnn_mx_blocks(n_values))
+    """Blocks of 32 values that hold a row of n_values: 16 bytes of codes and one of scale each (sdnn_mx_blocks)."""
+    return 4 * -(-n_values // 128) if 1 <= n_values <= 1 << 20 else 0
 
 
 def mx_linear_workspace_bytes(n_rows: int, n_values: int) -> int:
@@ -150,24 +160,22 @@ def mx_quantize(x, codes, scales, stream=None) -> None:
     """codes (rows, 16 * mx_blocks(n)) and scales (rows, mx_blocks(n)), bytes, of x (rows, n)."""
     _on_gpu("x", x)
     dt = _dtype(x.dtype)
-    px, ldx = _rows("x", x, (None, None), x.dtype)
+    px, ldx = _rows("x", x, None, None, x.dtype)
     pc, ps, rows = _codes("x", codes, scales, x.shape[1], x)
     if rows != x.shape[0]:
         raise ValueError(f"{rows} rows of codes for {x.shape[0]} rows of x")
-    with torch.cuda.device(x.device):
-        _check(load_library().sdnn_mx_quantize(px, ldx, dt, rows, x.shape[1], pc, ps, _stream_handle(stream)))
+    _call(x, "sdnn_mx_quantize", px, ldx, dt, rows, x.shape[1], pc, ps, _stream_handle(stream))
 
 
 def mx_dequantize(codes, scales, out, stream=None) -> None:
     """out (rows, n) = the values that the codes stand for."""
     _on_gpu("out", out)
     dt = _dtype(out.dtype)
-    po, ldo = _rows("out", out, (None, None), out.dtype)
+    po, ldo = _rows("out", out, None, None, out.dtype)
     pc, ps, rows = _codes("the input", codes, scales, out.shape[1], out)
     if rows != out.shape[0]:
         raise ValueError(f"{rows} rows of codes for {out.shape[0]} rows of out")
-    with torch.cuda.device(out.device):
-        _check(load_library().sdnn_mx_dequantize(pc, ps, rows, out.shape[1], po, ldo, dt, _stream_handle(stream)))
+    _call(out, "sdnn_mx_dequantize", pc, ps, rows, out.shape[1], po, ldo, dt, _stream_handle(stream))
 
 
 def mx_product(x_codes, x_scales, w_codes, w_scales, n_values: int, out, stream=None) -> None:
@@ -176,19 +184,16 @@ def mx_product(x_codes, x_scales, w_codes, w_scales, n_values: int, out, stream=
     dt = _dtype(out.dtype)
     pxc, pxs, rows = _codes("x", x_codes, x_scales, n_values, out)
     pwc, pws, outputs = _codes("w", w_codes, w_scales, n_values, out)
-    po, ldo = _rows("out", out, (rows, outputs), out.dtype)
-    with torch.cuda.device(out.device):
-        _check(load_library().sdnn_mx_product(pxc, pxs, pwc, pws, rows, outputs, n_values, po, ldo, dt, _stream_handle(stream)))
+    po, ldo = _rows("out", out, rows, outputs, out.dtype)
+    _call(out, "sdnn_mx_product", pxc, pxs, pwc, pws, rows, outputs, n_values, po, ldo, dt, _stream_handle(stream))
 
 
 def mx_linear(x, w_codes, w_scales, out, workspace, stream=None) -> None:
     """out (rows, outputs) = x w^T, x (rows, n) quantised on the way; out has x's type."""
     _on_gpu("x", x)
     dt = _dtype(x.dtype)
-    px, ldx = _rows("x", x, (None, None), x.dtype)
+    px, ldx = _rows("x", x, None, None, x.dtype)
     pwc, pws, outputs = _codes("w", w_codes, w_scales, x.shape[1], x)
-    po, ldo = _rows("out", out, (x.shape[0], outputs), x.dtype, x)
-    ws = _workspace(workspace, x)
-    with torch.cuda.device(x.device):
-        _check(load_library().sdnn_mx_linear(px, ldx, dt, pwc, pws, x.shape[0], outputs, x.shape[1], po, ldo, *ws,
-                                             _stream_handle(stream)))
+    po, ldo = _rows("out", out, x.shape[0], outputs, x.dtype, x)
+    _call(x, "sdnn_mx_linear", px, ldx, dt, pwc, pws, x.shape[0], outputs, x.shape[1], po, ldo, *_workspace(workspace, x),
+          _stream_handle(stream))
