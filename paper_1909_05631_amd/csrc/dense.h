@@ -144,6 +144,30 @@ __device__ __forceinline__ int split_exponent(float top) {
   return top > 0.0f && top < __builtin_inff() ? 14 - ilogbf(top) : 0;
 }
 
+// Sums kept in fp32, one slab per part of k (and matrix of a batch); with `add`, on what is there already.
+struct Accumulate {
+  float *slabs;
+  int64_t ld, rows, cols;
+  bool add;
+  template <class B>
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int split, bool) const {
+    const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
+    float *slab = slabs + ((int64_t)split * gridDim.y + blockIdx.y) * rows * ld;
+#pragma unroll
+    for (int i = 0; i < B::kTM; ++i) {
+      const int64_t r = row0 + 16 * i + i16;
+      if (r >= rows) continue;
+#pragma unroll
+      for (int j = 0; j < B::kTN; ++j) {
+        const int64_t c = col0 + 16 * j + 4 * j4;
+        if (c >= ld) continue;
+        f32x4 *p = (f32x4 *)(slab + r * ld + c);
+        *p = add ? *p + block.acc[i][j] : block.acc[i][j];
+      }
+    }
+  }
+};
+
 // Outputs of a launch in blocks. Workgroup ids go round the XCDs, so each XCD gets a run of consecutive
 // blocks, and those go down 8 blocks of rows before the next column: an XCD's 32 CUs work on 8 x 4 blocks,
 // which share their operands in its L2.
@@ -205,9 +229,10 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
   c = tile::uniform(c);
   int s0, s1;
   blocks.range(split, s0, s1);
+  const int64_t row0 = (int64_t)r * BM + B::row0(), col0 = (int64_t)c * BN + B::col0();
   B block;
   block.run(a.template at<KIND, BM, ACROSS_A>(r), b.template at<KIND, BN, ACROSS_B>(c), s0, s1, lds);
-  if (B::holds()) epilogue(block, (int64_t)r * BM + B::row0(), (int64_t)c * BN + B::col0(), split, r != c);
+  if (B::holds()) epilogue(block, row0, col0, split, r != c);
 }
 
 // Launches the blocks of one shape. What the sizes need of it is the caller's rule.
@@ -242,6 +267,7 @@ constexpr ShapeCost kCost[kShapes] = {{256, 256, 1, 1.65, 1.65}, {256, 192, 1, 1
 struct Plan {
   Shape shape;
   int splits;
+  double us;  // what the model makes of it
 };
 enum Form { kAnyForm, kAlong };  // kAlong: both operands are (rows of 192 columns make no whole loads)
 
@@ -250,8 +276,7 @@ enum Form { kAnyForm, kAlong };  // kAlong: both operands are (rows of 192 colum
 inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_splits, Form form = kAnyForm, int64_t batch = 1, bool symmetric = false) {
   const int64_t slabs = ceil_div(k, kind == tile::KIND_BF16 ? 64 : kind == tile::KIND_SPLIT ? 32 : 256);
   const double longer = kind == tile::KIND_SPLIT ? 1.4 : 1.0;
-  Plan best = {kWide, 1};
-  double least = 1e30;
+  Plan best = {kWide, 1, 1e30};
   for (int s = 0; s < kShapes; ++s) {
     const ShapeCost &c = kCost[s];
     if ((symmetric && c.bm != c.bn) || ((s == kMiddle || s == kBroad) && form != kAlong)) continue;
@@ -263,10 +288,7 @@ inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_split
       // (a round's first loads and last stores overlap with other blocks' work where a CU holds several)
       double t = rounds * (longer * (double)ceil_div(slabs, split) * std::max(c.alone, held * c.full) + 5.0 / std::sqrt(held));
       if (split > 1) t += 5.0 + 2e-6 * rows * cols * split * batch;
-      if (t < least) {
-        least = t;
-        best = {(Shape)s, split};
-      }
+      if (t < best.us) best = {(Shape)s, split, t};
     }
   }
   return best;

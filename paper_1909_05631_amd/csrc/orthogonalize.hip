@@ -158,6 +158,23 @@ struct Square {
   }
 };
 
+// A from the slabs of a product whose k was split: 4 columns a lane.
+__global__ __launch_bounds__(256) void k_square(const float *slabs, int splits, int64_t size, int64_t pitch, char *out, Bound bound, const Info *info) {
+  const float limit = bound_of(bound, info);
+  const int e = a_exponent(limit) - 2 * x_exponent(limit);
+  const int per = (int)(pitch / 16);
+  char *to = out + blockIdx.y * (size * pitch);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per, c = (i - r * per) * 4;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) v += *(const f32x4 *)(slabs + (((int64_t)s * gridDim.y + blockIdx.y) * size + r) * (pitch / 4) + c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = ldexpf(v[k], e);
+    store_split4(to + r * pitch, c, v);
+  }
+}
+
 // X's next value, a X + the product's sums: the next factor in two parts, or the answer.
 template <class T>
 struct Update {
@@ -198,6 +215,286 @@ struct Update {
   }
 };
 
+// Small matrices: one workgroup does all steps of one matrix, whose X (m x n, m <= n, transposed on the way in and out where
+// rows > cols) and square factor stay in LDS in two parts. The launches of the large form cost 17 times 6 us whatever their
+// size. 16 waves share the 32 x 32 tiles of each product; every wave computes its tiles into registers, all meet,
+// and the tiles are written. LDS holds 32 columns of all rows at a time (a slab), 128 bytes a row as in
+// tile.h, chunks permuted by the row; both products' fragments are read from that one form.
+constexpr int kRoom = 152 * 1024;
+inline int64_t pad32(int64_t x) { return ceil_div(x, 32) * 32; }
+inline bool is_small(int64_t rows, int64_t cols) {
+  const int64_t m = pad32(std::min(rows, cols)), n = pad32(std::max(rows, cols));
+  return m <= 128 && (m * n + m * m) * 4 <= kRoom;  // at most 16 tiles of the square, at most 3 tiles of X a wave
+}
+
+struct Steps {
+  int count;
+  float a, b, c;
+  Bound bounds[kMaxSteps + 1];
+};
+__device__ __forceinline__ float limit_of(const Steps &s, int k, float log2_f) { return fminf(s.bounds[k].u, log2_f + s.bounds[k].l); }
+
+// A 16-row fragment of k = 32 values: part q of rows first ... first + 15 of a slab.
+__device__ __forceinline__ tile::i32x4 fragment_along(const char *slab, int first, int q, int lane) {
+  const int row = first + (lane & 15);
+  return *(const tile::i32x4 *)(slab + row * 128 + (((4 * q + (lane >> 4)) ^ (row & 7)) * 16));
+}
+// The same of 16 columns (half `half` of the slab's 32) over rows k ... k + 31.
+__device__ __forceinline__ tile::i32x4 fragment_across(const char *slab, int k, int half, int q, int lane) {
+  typedef __attribute__((address_space(3))) tile::i16x4 lds_i16x4;
+  const int r = (lane & 15) >> 2, p = lane & 3, chunk = 4 * q + 2 * half + (p >> 1);
+  tile::i16x4 h[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int row = k + 8 * (lane >> 4) + 4 * u + r;
+    h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(slab + row * 128 + ((chunk ^ (4 * u + r)) * 16) + (p & 1) * 8));
+  }
+  return __builtin_bit_cast(tile::i32x4, h);
+}
+
+struct Tile32 {
+  f32x4 v[2][2];  // [rows 16 i + lane % 16][columns 16 j + 4 (lane / 16)]
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i >> 1][i & 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  __device__ __forceinline__ void multiply(const tile::i32x4 (&a)[2][2], const tile::i32x4 (&b)[2][2]) {
+#pragma unroll
+    for (int part = 2; part >= 0; --part)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) v[i][j] = tile::mfma<KIND_SPLIT>(b[j][part == 1], a[i][part == 2], v[i][j]);
+  }
+};
+
+// Where part q of four neighbours lies.
+__device__ __forceinline__ char *place(char *slab, int row, int col, int q) { return slab + row * 128 + (((4 * q + ((col & 31) >> 3)) ^ (row & 7)) * 16) + (col & 4) * 2; }
+__device__ __forceinline__ void put(char *slab, int row, int col, f32x4 v) {
+  f16x4 hi, lo;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    _Float16 h, l;
+    split(v[i], h, l);
+    hi[i] = h;
+    lo[i] = l;
+  }
+  *(f16x4 *)place(slab, row, col, 0) = hi;
+  *(f16x4 *)place(slab, row, col, 1) = lo;
+}
+__device__ __forceinline__ f32x4 get(char *slab, int row, int col) {
+  const f16x4 hi = *(const f16x4 *)place(slab, row, col, 0), lo = *(const f16x4 *)place(slab, row, col, 1);
+  f32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (float)hi[i] + (float)lo[i];
+  return v;
+}
+
+template <class T>
+__global__ __launch_bounds__(1024) void k_small(Source<T> g, T *out, int64_t ldo, int64_t batch_o, bool vec, double eps, Steps steps) {
+  __shared__ __attribute__((aligned(1024))) char room[kRoom];
+  __shared__ double part[16];
+  const int tid = threadIdx.x, wave = tile::uniform(tid >> 6);
+  int lane = tid & 63;
+  const bool tall = g.rows > g.cols;
+  const int M = (int)(tall ? g.cols : g.rows), N = (int)(tall ? g.rows : g.cols);
+  const int m = (M + 31) & ~31, n = (N + 31) & ~31, slab = m * 128, row_tiles = m / 32, slabs = n / 32;
+  char *x = room, *square = room + m * n * 4;
+  const T *src = g.data + blockIdx.x * g.batch;
+  T *dst = out + blockIdx.x * batch_o;
+
+  // g's values go to LDS as they are, four where their two parts will lie, while their squares are summed. (Lanes
+  // go along g's rows; reads outside it are clamped to its last value and dropped, so that all are on their way at once.)
+  const int wide = tall ? m : n / 4, items = m * n / 4;
+  const auto walk = [&](auto f) {
+    int fast = tid % wide, slow = tid / wide;
+    const int fast_step = 1024 % wide, slow_step = 1024 / wide;
+#pragma unroll 4
+    for (int i = tid; i < items; i += 1024) {
+      f(tall ? fast : slow, 4 * (tall ? slow : fast));
+      fast += fast_step;
+      slow += slow_step;
+      if (fast >= wide) {
+        fast -= wide;
+        ++slow;
+      }
+    }
+  };
+  double s = 0.0;
+  walk([&](int r, int c) {
+    f32x4 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int rr = min(r, M - 1), cc = min(c + k, N - 1);
+      const float w = load_as_float(tall ? src + (int64_t)cc * g.ld + rr : src + (int64_t)rr * g.ld + cc);
+      v[k] = r < M && c + k < N ? w : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s = fma((double)v[k], (double)v[k], s);
+    char *slab_of = x + (c >> 5) * slab;
+    *(float2 *)place(slab_of, r, c, 0) = float2{v[0], v[1]};
+    *(float2 *)place(slab_of, r, c, 1) = float2{v[2], v[3]};
+  });
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if (lane == 0) part[wave] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < 16; ++w) s += part[w];
+  const double norm = sqrt(s), inverse = 1.0 / (norm + eps);
+  const float log2_f = (float)log2(norm * inverse);
+  const int e0 = x_exponent(limit_of(steps, 0, log2_f));
+  walk([&](int r, int c) {
+    char *slab_of = x + (c >> 5) * slab;
+    const float2 one = *(const float2 *)place(slab_of, r, c, 0), two = *(const float2 *)place(slab_of, r, c, 1);
+    f32x4 v = {one.x, one.y, two.x, two.y};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = ldexpf((float)(v[k] * inverse), e0);
+    put(slab_of, r, c, v);
+  });
+  __syncthreads();
+  // this wave's tile of the square; for A, as many waves share a tile's k as the room takes their sums
+  const int square_tiles = row_tiles * row_tiles, group = wave / square_tiles, tile = wave % square_tiles;
+  const int groups = max(1, min(min(16 / square_tiles, slabs / 2), 1 + (kRoom - (m * n + m * m) * 4) / (square_tiles * 4096)));
+  f32x4 *sums = (f32x4 *)(square + m * m * 4);
+  const int ti = tile / row_tiles, tj = tile % row_tiles;
+  const bool squares = group == 0;
+  Tile32 next[3];
+  for (int step = 0; step < steps.count; ++step) {
+    asm volatile("" : "+v"(lane));  // (addresses that do not change are found again each step: kept, they would fill the registers)
+    const int i16 = lane & 15, j4 = lane >> 4;
+    const float limit = limit_of(steps, step, log2_f);
+    const int ex = x_exponent(limit), ea = a_exponent(limit), eb = b_exponent(limit, steps.b, steps.c);
+    Tile32 t;
+    // A = X X^T
+    if (group < groups) {
+      t.clear();
+#pragma unroll 1
+      for (int k = group; k < slabs; k += groups) {
+        tile::i32x4 a[2][2], b[2][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i >> 1][i & 1] = fragment_along(x + k * slab, ti * 32 + 16 * (i >> 1), i & 1, lane);
+          b[i >> 1][i & 1] = fragment_along(x + k * slab, tj * 32 + 16 * (i >> 1), i & 1, lane);
+        }
+        t.multiply(a, b);
+      }
+      if (group > 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[(((group - 1) * square_tiles + tile) * 4 + i) * 64 + lane] = t.v[i >> 1][i & 1];
+    }
+    if (groups > 1) __syncthreads();
+    if (squares) {
+      for (int u = 1; u < groups; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t.v[i >> 1][i & 1] += sums[(((u - 1) * square_tiles + tile) * 4 + i) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          f32x4 v = t.v[i][j];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = ldexpf(v[k], ea - 2 * ex);
+          put(square + tj * slab, ti * 32 + 16 * i + i16, tj * 32 + 16 * j + 4 * j4, v);
+        }
+    }
+    __syncthreads();
+    // b A + c A A
+    if (squares) {
+      t.clear();
+#pragma unroll 1
+      for (int k = 0; k < row_tiles; ++k) {
+        tile::i32x4 a[2][2], b[2][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i >> 1][i & 1] = fragment_along(square + k * slab, ti * 32 + 16 * (i >> 1), i & 1, lane);
+          b[i >> 1][i & 1] = fragment_along(square + k * slab, tj * 32 + 16 * (i >> 1), i & 1, lane);
+        }
+        t.multiply(a, b);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const f32x4 one = get(square + tj * slab, ti * 32 + 16 * i + i16, tj * 32 + 16 * j + 4 * j4);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) t.v[i][j][k] = ldexpf(steps.b * ldexpf(one[k], -ea) + steps.c * ldexpf(t.v[i][j][k], -2 * ea), eb);
+        }
+    }
+    __syncthreads();
+    if (squares)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) put(square + tj * slab, ti * 32 + 16 * i + i16, tj * 32 + 16 * j + 4 * j4, t.v[i][j]);
+    __syncthreads();
+    // a X + B X: up to three tiles a wave, held until all have read X
+    const bool last = step + 1 == steps.count;
+    const int en = last ? 0 : x_exponent(limit_of(steps, step + 1, log2_f)), tiles = row_tiles * slabs;
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      const int id = wave + 16 * u;
+      if (id >= tiles) continue;
+      const int r = id % row_tiles, c = id / row_tiles;
+      next[u].clear();
+#pragma unroll 1
+      for (int k = 0; k < row_tiles; ++k) {
+        tile::i32x4 a[2][2], b[2][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i >> 1][i & 1] = fragment_along(square + k * slab, r * 32 + 16 * (i >> 1), i & 1, lane);
+          b[i >> 1][i & 1] = fragment_across(x + c * slab, k * 32, i >> 1, i & 1, lane);
+        }
+        next[u].multiply(a, b);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int row = r * 32 + 16 * i + i16, col = c * 32 + 16 * j + 4 * j4;
+          const f32x4 old = get(x + c * slab, row, col);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            next[u].v[i][j][k] = ldexpf(steps.a * ldexpf(old[k], -ex) + ldexpf(next[u].v[i][j][k], -ex - eb), en);
+          }
+        }
+    }
+    if (last) break;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      const int id = wave + 16 * u;
+      if (id >= tiles) continue;
+      const int r = id % row_tiles, c = id / row_tiles;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) put(x + c * slab, r * 32 + 16 * i + i16, c * 32 + 16 * j + 4 * j4, next[u].v[i][j]);
+    }
+    __syncthreads();
+  }
+  // the last step's tiles are the answer
+  const int i16 = lane & 15, j4 = lane >> 4;
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {
+    const int id = wave + 16 * u;
+    if (id >= row_tiles * slabs) continue;
+    const int r = id % row_tiles, c = id / row_tiles;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = r * 32 + 16 * i + i16, col = c * 32 + 16 * j + 4 * j4;
+        if (tall) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (row < M && col + k < N) dst[(int64_t)(col + k) * ldo + row] = (T)next[u].v[i][j][k];
+        } else if (row < M && col < N) {
+          store4(dst + row * ldo + col, next[u].v[i][j], min(N - col, 4), vec);
+        }
+      }
+  }
+}
+
 // No step: the start itself.
 template <class T>
 __global__ __launch_bounds__(256) void k_scale(Source<T> g, const double *parts, int count, double eps, T *out, int64_t ld, int64_t batch) {
@@ -233,16 +530,27 @@ void reach(double a, double b, double c, double u, double &value, double &slope)
 }
 
 struct Space {
+  Plan gram, power, update;
+  bool split;  // A's k is split: all its blocks are computed, and k_square joins them
   double *parts;
   Info *info;
   char *x[2], *a, *b;
+  float *slabs;
   Space(Carver &c, int64_t batch, int64_t rows, int64_t cols) {
-    const int64_t m = std::min(rows, cols);
+    const int64_t m = std::min(rows, cols), k = std::max(rows, cols);
+    const bool tall = rows > cols;
+    gram = plan(KIND_SPLIT, m, m, k, 1, tall ? kAnyForm : kAlong, batch, true);
+    const Plan joined = plan(KIND_SPLIT, m, m, k, kMaxSplits, tall ? kAnyForm : kAlong, batch);
+    split = joined.splits > 1 && joined.us < gram.us;
+    if (split) gram = joined;
+    power = plan(KIND_SPLIT, m, m, m, 1, kAlong, batch, true);
+    update = plan(KIND_SPLIT, rows, cols, m, 1, tall ? kAlong : kAnyForm, batch);
     parts = c.take<double>((size_t)(batch * kNormBlocks));
     info = c.take<Info>((size_t)batch);
     for (char *&p : x) p = c.take<char>((size_t)(batch * rows * ceil_div(cols, 32) * 128));
     a = c.take<char>((size_t)(batch * m * ceil_div(m, 32) * 128));
     b = c.take<char>((size_t)(batch * m * ceil_div(m, 32) * 128));
+    slabs = c.take<float>(split ? (size_t)(gram.splits * batch * m * ceil_div(m, 32) * 32) : 0);
   }
 };
 
@@ -252,13 +560,8 @@ sdnn_status orthogonalize(const T *g, int64_t ldg, int64_t batch_g, T *out, int6
   Carver carver{(char *)workspace};
   const Space sp(carver, batch, rows, cols);
   const Source<T> src{g, ldg, batch_g, rows, cols};
-  const unsigned norm_blocks = (unsigned)std::min<int64_t>(rows, kNormBlocks), row_blocks = (unsigned)std::min<int64_t>(rows, 2048);
-  hipLaunchKernelGGL((k_squares<T>), dim3(norm_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts);
-  if (steps == 0) {
-    hipLaunchKernelGGL((k_scale<T>), dim3(row_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts, (int)norm_blocks, (double)eps, out, ldo, batch_o);
-    return launched("orthogonalize");
-  }
-  Bound bounds[kMaxSteps + 1];
+  Steps plan_of{steps, coef[0], coef[1], coef[2], {}};
+  Bound *bounds = plan_of.bounds;
   double u = 1.0, l = 1.0;
   for (int k = 0; k <= steps; ++k) {
     bounds[k] = {(float)std::log2(u), (float)std::log2(l)};
@@ -267,28 +570,46 @@ sdnn_status orthogonalize(const T *g, int64_t ldg, int64_t batch_g, T *out, int6
     u = std::min(1e30, std::max(1e-30, 1.01 * value));  // what rounding adds is far below a hundredth
     l = std::min(1e30, std::max(1e-30, 1.01 * slope * l));
   }
+  const bool vec = (uintptr_t)out % (4 * sizeof(T)) == 0 && ldo % 4 == 0 && batch_o % 4 == 0;
+  if (steps > 0 && is_small(rows, cols)) {
+    hipLaunchKernelGGL((k_small<T>), dim3((unsigned)batch), dim3(1024), 0, stream, src, out, ldo, batch_o, vec, (double)eps, plan_of);
+    return launched("orthogonalize");
+  }
+  const unsigned norm_blocks = (unsigned)std::min<int64_t>(rows, kNormBlocks), row_blocks = (unsigned)std::min<int64_t>(rows, 2048);
+  hipLaunchKernelGGL((k_squares<T>), dim3(norm_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts);
+  if (steps == 0) {
+    hipLaunchKernelGGL((k_scale<T>), dim3(row_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts, (int)norm_blocks, (double)eps, out, ldo, batch_o);
+    return launched("orthogonalize");
+  }
   const int64_t pitch = ceil_div(cols, 32) * 128, m = std::min(rows, cols), square = ceil_div(m, 32) * 128;
   hipLaunchKernelGGL((k_start<T>), dim3(row_blocks, (unsigned)batch), dim3(256), 0, stream, src, sp.parts, (int)norm_blocks, (double)eps, bounds[0], sp.info, sp.x[0], pitch);
   sdnn_status st = launched("orthogonalize");
   const bool tall = rows > cols;
-  const Plan gram = plan(KIND_SPLIT, m, m, std::max(rows, cols), 1, tall ? kAnyForm : kAlong, batch, true);
-  const Plan power = plan(KIND_SPLIT, m, m, m, 1, kAlong, batch, true);
-  const Plan update = plan(KIND_SPLIT, rows, cols, m, 1, tall ? kAlong : kAnyForm, batch);
   for (int k = 0; k < steps && st == SDNN_OK; ++k) {
     const char *x = sp.x[k & 1];
     char *next = k + 1 < steps ? sp.x[(k + 1) & 1] : nullptr;
     const Matrix mx{x, pitch, rows, pitch, rows * pitch}, ma{sp.a, square, m, square, m * square}, mb{sp.b, square, m, square, m * square};
     Square e{nullptr, sp.a, m, square, coef[1], coef[2], bounds[k], sp.info};
-    st = tall ? run_shape<KIND_SPLIT, true, true>(gram, mx, mx, m, m, rows, e, stream, "orthogonalize", true, (int)batch)
-              : run_shape<KIND_SPLIT, false, false>(gram, mx, mx, m, m, cols, e, stream, "orthogonalize", true, (int)batch);
+    if (sp.split) {
+      const Accumulate parts{sp.slabs, square / 4, m, m, false};
+      st = tall ? run_shape<KIND_SPLIT, true, true>(sp.gram, mx, mx, m, m, rows, parts, stream, "orthogonalize", false, (int)batch)
+                : run_shape<KIND_SPLIT, false, false>(sp.gram, mx, mx, m, m, cols, parts, stream, "orthogonalize", false, (int)batch);
+      if (st != SDNN_OK) return st;
+      hipLaunchKernelGGL(k_square, dim3((unsigned)std::min<int64_t>(ceil_div(m * (square / 16), 256), 2048), (unsigned)batch), dim3(256), 0, stream, sp.slabs, sp.gram.splits, m, square, sp.a, bounds[k],
+                         sp.info);
+      st = launched("orthogonalize");
+    } else {
+      st = tall ? run_shape<KIND_SPLIT, true, true>(sp.gram, mx, mx, m, m, rows, e, stream, "orthogonalize", true, (int)batch)
+                : run_shape<KIND_SPLIT, false, false>(sp.gram, mx, mx, m, m, cols, e, stream, "orthogonalize", true, (int)batch);
+    }
     if (st != SDNN_OK) return st;
     e.a = sp.a;
     e.out = sp.b;
-    st = run_shape<KIND_SPLIT, false, false>(power, ma, ma, m, m, m, e, stream, "orthogonalize", true, (int)batch);
+    st = run_shape<KIND_SPLIT, false, false>(sp.power, ma, ma, m, m, m, e, stream, "orthogonalize", true, (int)batch);
     if (st != SDNN_OK) return st;
-    const Update<T> last{x, next, out, ldo, batch_o, rows, cols, pitch, (uintptr_t)out % (4 * sizeof(T)) == 0 && ldo % 4 == 0 && batch_o % 4 == 0, coef[0], coef[1], coef[2], bounds[k], bounds[k + 1], sp.info};
-    st = tall ? run_shape<KIND_SPLIT, false, false>(update, mx, mb, rows, cols, m, last, stream, "orthogonalize", false, (int)batch)
-              : run_shape<KIND_SPLIT, false, true>(update, mb, mx, rows, cols, m, last, stream, "orthogonalize", false, (int)batch);
+    const Update<T> last{x, next, out, ldo, batch_o, rows, cols, pitch, vec, coef[0], coef[1], coef[2], bounds[k], bounds[k + 1], sp.info};
+    st = tall ? run_shape<KIND_SPLIT, false, false>(sp.update, mx, mb, rows, cols, m, last, stream, "orthogonalize", false, (int)batch)
+              : run_shape<KIND_SPLIT, false, true>(sp.update, mb, mx, rows, cols, m, last, stream, "orthogonalize", false, (int)batch);
   }
   return st;
 }

@@ -375,30 +375,6 @@ struct Store {
   }
 };
 
-// Sums kept in fp32, one slab per part of k; with `add`, on what the pieces before left there.
-struct Accumulate {
-  float *slabs;
-  int64_t ld, rows, cols;
-  bool add;
-  template <class B>
-  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int split, bool) const {
-    const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
-    float *slab = slabs + split * rows * ld;
-#pragma unroll
-    for (int i = 0; i < B::kTM; ++i) {
-      const int64_t r = row0 + 16 * i + i16;
-      if (r >= rows) continue;
-#pragma unroll
-      for (int j = 0; j < B::kTN; ++j) {
-        const int64_t c = col0 + 16 * j + 4 * j4;
-        if (c >= ld) continue;
-        f32x4 *p = (f32x4 *)(slab + r * ld + c);
-        *p = add ? *p + block.acc[i][j] : block.acc[i][j];
-      }
-    }
-  }
-};
-
 // The slabs' sum, rounded to the output's type: 256 / GROUPS items a workgroup, each group taking every GROUPS-th slab.
 template <class T, int GROUPS>
 __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int splits, int64_t ld_slab, Store<T> to) {
