@@ -19,12 +19,8 @@ constexpr int kNanScale = 255;
 
 __host__ __device__ inline int64_t blocks_of(int64_t n) { return 4 * ceil_div(n, 128); }
 
-// Magnitude code of a >= 0: the grid's middles, ties to the even code.
-__device__ __forceinline__ uint32_t code_of(float a) {
-  return (uint32_t)(a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
-}
-
-// Eight values' codes and, from the four lanes of a block together, the block's scale byte.
+// Eight values' codes and, from the four lanes of a block together, the block's scale byte. The values are multiplied by
+// a power of two, exactly; the conversion instruction rounds to nearest, ties to even, and saturates.
 __device__ __forceinline__ uint32_t quantize8(const float (&v)[8], uint32_t &scale) {
   uint32_t top = 0;
 #pragma unroll
@@ -37,17 +33,16 @@ __device__ __forceinline__ uint32_t quantize8(const float (&v)[8], uint32_t &sca
     const uint32_t o = __shfl_xor(top, d);
     top = o > top ? o : top;
   }
-  if (top >= 0x7f800000u) {
-    scale = kNanScale;
-    return 0;
-  }
+  const bool bad = top >= 0x7f800000u;
   const uint32_t field = top >> 23;
-  scale = field > 2 ? field - 2 : 0;
-  const float inverse = __uint_as_float((254 - scale) << 23);  // 2^(127 - scale), exact
+  scale = bad ? kNanScale : field > 2 ? field - 2 : 0;
+  const float inverse = bad ? 0.0f : __uint_as_float((254 - scale) << 23);  // 2^(127 - scale)
   uint32_t codes = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) codes |= (code_of(fabsf(v[i] * inverse)) | (__float_as_uint(v[i]) >> 31) << 3) << (4 * i);
-  return codes;
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[0] * inverse, v[1] * inverse, 1.0f, 0);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[2] * inverse, v[3] * inverse, 1.0f, 1);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[4] * inverse, v[5] * inverse, 1.0f, 2);
+  codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, v[6] * inverse, v[7] * inverse, 1.0f, 3);
+  return bad ? 0 : codes;
 }
 
 template <class T>
@@ -80,28 +75,52 @@ __global__ __launch_bounds__(256) void k_quantize(const T *x, int64_t ld, int64_
   }
 }
 
-__device__ __forceinline__ float value_of(uint32_t code, uint32_t scale) {
-  // the magnitude as a float: codes 2 ... 7 are 1.m 2^(e-1) with two bits of e and one of m, code 1 is a half
-  const uint32_t m = code & 7;
-  const float a = m < 2 ? 0.5f * m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-  const float v = ldexpf(code & 8 ? -a : a, (int)scale - 127);
-  return scale == kNanScale ? __builtin_nanf("") : v;
+// Byte BYTE's two values.
+template <int BYTE>
+__device__ __forceinline__ void values_of(uint32_t word, float scale, float *v) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2 two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, BYTE);
+  v[0] = two[0] * scale;
+  v[1] = two[1] * scale;
+}
+__device__ __forceinline__ float scale_of(uint32_t s) {
+  return s == kNanScale ? __builtin_nanf("") : __uint_as_float(s ? s << 23 : 1u << 22);  // 2^-127 is not normal
 }
 
+// 16 bytes of values a lane: a wave stores a run of 1024. Bound by memory, most of it the values written.
 template <class T>
 __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t n, int64_t blocks, T *out, int64_t ld, bool vec) {
-  const int per = (int)ceil_div(n, 8);
+  constexpr int kEach = 16 / sizeof(T);
+  const int per = (int)ceil_div(n, kEach);
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-    const uint8_t *from = codes + r * blocks * 16, *scale_of = scales + r * blocks;
+    const uint8_t *from = codes + r * blocks * 16, *scales_from = scales + r * blocks;
     for (int c = blockIdx.x * 256 + threadIdx.x; c < per; c += gridDim.x * 256) {
-      const uint32_t word = *(const uint32_t *)(from + c * 4), scale = scale_of[c >> 2];
-      f32x4 v[2];
+      const float scale = scale_of(scales_from[c * kEach / 32]);
+      float v[kEach];
+      uint32_t word;
+      if constexpr (kEach == 8)
+        word = *(const uint32_t *)(from + c * 4);
+      else
+        word = *(const uint16_t *)(from + c * 2);
+      values_of<0>(word, scale, v);
+      values_of<1>(word, scale, v + 2);
+      if constexpr (kEach == 8) {
+        values_of<2>(word, scale, v + 4);
+        values_of<3>(word, scale, v + 6);
+      }
+      typedef T Out __attribute__((ext_vector_type(kEach)));
+      Out o;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j >> 2][j & 3] = value_of(word >> (4 * j) & 15, scale);
-      T *to = out + r * ld + c * 8;
-      const int left = min((int)n - c * 8, 8);
-      store4(to, v[0], left < 4 ? left : 4, vec);
-      if (left > 4) store4(to + 4, v[1], left - 4, vec);
+      for (int k = 0; k < kEach; ++k) o[k] = (T)v[k];
+      T *to = out + r * ld + (int64_t)c * kEach;
+      const int left = min((int)n - c * kEach, kEach);
+      if (vec && left == kEach) {
+        *(Out *)to = o;
+      } else {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+          if (k < left) to[k] = o[k];
+      }
     }
   }
 }
@@ -127,6 +146,86 @@ sdnn_status product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8
   const Matrix a{(const char *)x_codes, pitch, rows, pitch, 0, x_scales}, b{(const char *)w_codes, pitch, outputs, pitch, 0, w_scales};
   const Store<T> e{out, ld, rows, outputs, (uintptr_t)out % 16 == 0 && ld * sizeof(T) % 16 == 0};
   return run_shape<KIND_MX, false, false>(plan(KIND_MX, rows, outputs, n, 1, kAlong), a, b, rows, outputs, n, e, stream, "product");
+}
+
+// Few rows: one launch that quantises x into LDS, every workgroup for itself, and streams w from memory to the matrix
+// instructions, each byte once and without LDS. A workgroup takes 16 outputs at a time and its four waves share k, 1024
+// values of a wave on their way at once; their sums meet in LDS. Bound by w's bytes: 65536 x 4096 (143 MB) takes 28 us
+// for one row, 5.2 TB/s. Every workgroup's own quantisation is what limits it: four rows of that take 32 us, 26 in
+// tiles. So it takes up to 4096 values, or up to 65536 where the outputs make no more workgroups than there are
+// CUs (1000 x 1024: 4 us; in tiles k would be one long chain: 4096 x 65536 takes 106 us there).
+constexpr int kFewRows = 16, kFewValues = 65536;
+inline bool is_few(int64_t rows, int64_t outputs, int64_t n) {
+  const int64_t values = rows * ceil_div(n, 256) * 256;
+  return rows <= kFewRows && (values <= 4096 || (values <= kFewValues && outputs <= 16 * kCus));
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void k_few(const T *x, int64_t ldx, bool vec_x, int rows, int n, const uint8_t *w_codes, const uint8_t *w_scales, int64_t outputs, T *out, int64_t ldo, bool vec) {
+  using tile::i32x4;
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kFewValues / 2];
+  __shared__ __attribute__((aligned(16))) uint8_t scales[kFewValues / 32];
+  __shared__ f32x4 sums[4][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tile::uniform(tid >> 6), i16 = lane & 15, j4 = lane >> 4;
+  const int blocks = (int)blocks_of(n), slabs = (blocks + 7) / 8, wide = slabs * 8;  // blocks of a row: in memory, in LDS
+  const int64_t pitch = (int64_t)blocks * 16;
+  for (int i = tid; i < rows * wide * 4; i += 256) {
+    const int r = i / (wide * 4), c = i - r * (wide * 4);
+    float v[8];
+    load8(x + r * ldx, (int64_t)c * 8, n, vec_x, v);
+    uint32_t scale;
+    *(uint32_t *)(codes + i * 4) = quantize8(v, scale);
+    if ((c & 3) == 0) scales[i >> 2] = (uint8_t)scale;
+  }
+  __syncthreads();
+  const int per = (slabs + 3) / 4, s0 = wave * per, s1 = min(s0 + per, slabs);  // this wave's k
+  const bool mine = i16 < rows;
+  for (int64_t first = (int64_t)blockIdx.x * 16; first < outputs; first += (int64_t)gridDim.x * 16) {
+    const int there = outputs - first < 16 ? (int)(outputs - first) : 16;
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void *)(w_codes + first * pitch), 0, there * (int)pitch, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(w_scales + first * blocks), 0, there * blocks, 0x00027000);
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = s0; s < s1; s += 4) {
+      i32x4 b[4][2];
+      int sb[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int block = (s + u) * 8 + 2 * j4;
+        const bool in = s + u < s1 && block < blocks;  // past them: zeros
+#pragma unroll
+        for (int q = 0; q < 2; ++q) b[u][q] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, in ? i16 * (int)pitch + (block + q) * 16 : tile::kOut, 0, 0));
+        sb[u] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, in ? i16 * blocks + block : tile::kOut, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int at = (i16 * wide + min(s + u, slabs - 1) * 8 + 2 * j4);
+        i32x4 a[2] = {};
+        int sa = 0;
+        if (mine) {
+          a[0] = *(const i32x4 *)(codes + at * 16);
+          a[1] = *(const i32x4 *)(codes + at * 16 + 16);
+          sa = *(const uint16_t *)(scales + at);
+        }
+        acc = tile::mfma_mx<0>(b[u][0], a[0], acc, sb[u], s + u < s1 ? sa : 0);
+        acc = tile::mfma_mx<1>(b[u][1], a[1], acc, sb[u], s + u < s1 ? sa : 0);
+      }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0) {
+      const f32x4 v = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+      const int64_t c = first + 4 * j4;
+      if (mine && c < outputs) store4(out + i16 * ldo + c, v, (int)(outputs - c < 4 ? outputs - c : 4), vec);
+    }
+    __syncthreads();
+  }
+}
+
+template <class T>
+sdnn_status few(const T *x, int64_t ldx, const uint8_t *w_codes, const uint8_t *w_scales, int64_t rows, int64_t outputs, int64_t n, T *out, int64_t ldo, hipStream_t stream) {
+  const bool vec_x = (uintptr_t)x % 16 == 0 && ldx * sizeof(T) % 16 == 0, vec = (uintptr_t)out % (4 * sizeof(T)) == 0 && ldo % 4 == 0;
+  hipLaunchKernelGGL((k_few<T>), dim3((unsigned)std::min<int64_t>(ceil_div(outputs, 16), 4 * kCus)), dim3(256), 0, stream, x, ldx, vec_x, (int)rows, (int)n, w_codes, w_scales, outputs, out, ldo, vec);
+  return launched("linear");
 }
 
 // Workgroups along a row of `items` lanes, and down the rows: 16 to 32 a CU where there is work for them.
@@ -183,8 +282,8 @@ sdnn_status sdnn_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int6
   if ((st = check_mx("the input", codes, scales)) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
   const int64_t blocks = blocks_of(n_values);
-  const dim3 grid = grid_of(n_rows, ceil_div(n_values, 8));
-  const bool vec = (uintptr_t)out % (4 * dtype_bytes(dtype)) == 0 && ldo % 4 == 0;
+  const dim3 grid = grid_of(n_rows, ceil_div(n_values, 16 / dtype_bytes(dtype)));
+  const bool vec = (uintptr_t)out % 16 == 0 && ldo * dtype_bytes(dtype) % 16 == 0;
   if (dtype == SDNN_BF16)
     hipLaunchKernelGGL((k_dequantize<__bf16>), grid, dim3(256), 0, stream, codes, scales, n_rows, n_values, blocks, (__bf16 *)out, ldo, vec);
   else
@@ -222,6 +321,11 @@ sdnn_status sdnn_mx_linear(const void *x, int64_t ldx, int32_t dtype, const uint
   if ((st = check_mx("w", w_codes, w_scales)) != SDNN_OK) return st;
   if ((st = check_matrix("out", out, ldo, n_outputs, dtype)) != SDNN_OK) return st;
   if ((st = check_workspace(workspace, workspace_bytes, sdnn_mx_linear_workspace_bytes(n_rows, n_values))) != SDNN_OK) return st;
+  if (is_few(n_rows, n_outputs, n_values)) {
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    return dtype == SDNN_BF16 ? few((const __bf16 *)x, ldx, w_codes, w_scales, n_rows, n_outputs, n_values, (__bf16 *)out, ldo, stream)
+                              : few((const float *)x, ldx, w_codes, w_scales, n_rows, n_outputs, n_values, (float *)out, ldo, stream);
+  }
   Carver c{(char *)workspace};
   uint8_t *codes = c.take<uint8_t>((size_t)(n_rows * blocks_of(n_values) * 16)), *scales = c.take<uint8_t>((size_t)(n_rows * blocks_of(n_values)));
   if ((st = sdnn_mx_quantize(x, ldx, dtype, n_rows, n_values, codes, scales, hip_stream)) != SDNN_OK) return st;
