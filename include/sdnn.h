@@ -230,7 +230,8 @@ sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t
  *   dx: n_rows x n_features, dw: n_classes x n_features, of `dtype`, row strides lddx and lddw; overwritten. Either
  *   may be NULL: not computed. Neither may overlap an input.
  * Rows without a label add nothing to dw and have a dx of zeros, whatever x, lse and row_grad hold there. For bf16 G is
- * rounded to bf16 once, between two fp32 sums; for fp32 it is held in two fp16 parts. */
+ * rounded to bf16 once (as a fraction of the largest row_grad), between two fp32 sums; for fp32 it is held in two
+ * fp16 parts. */
 sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t dtype,
                               const int64_t *labels, const float *lse, const float *row_grad, int64_t n_rows,
                               int64_t n_classes, int64_t n_features, void *dx, int64_t lddx, void *dw, int64_t lddw,

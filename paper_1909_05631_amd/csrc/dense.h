@@ -272,13 +272,14 @@ struct Plan {
 enum Form { kAnyForm, kAlong };  // kAlong: both operands are (rows of 192 columns make no whole loads)
 
 // The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs (1.4 as long for
-// three products a slab), and for a split sum its slabs' traffic (at 4 TB/s) and one launch more.
+// three products a slab, 2.3 in fp32), and for a split sum its slabs' traffic (at 4 TB/s) and one launch more.
 inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_splits, Form form = kAnyForm, int64_t batch = 1, bool symmetric = false) {
-  const int64_t slabs = ceil_div(k, kind == tile::KIND_BF16 ? 64 : kind == tile::KIND_SPLIT ? 32 : 256);
-  const double longer = kind == tile::KIND_SPLIT ? 1.4 : 1.0;
-  Plan best = {kWide, 1, 1e30};
+  const int64_t slabs = ceil_div(k, kind == tile::KIND_BF16 ? 64 : kind == tile::KIND_MX ? 256 : 32);
+  const double longer = kind == tile::KIND_SPLIT ? 1.4 : kind == tile::KIND_F32 ? 2.3 : 1.0;
+  Plan best = {kStream, 1, 1e30};
   for (int s = 0; s < kShapes; ++s) {
     const ShapeCost &c = kCost[s];
+    if (kind == tile::KIND_F32 && s < kStream) continue;  // memory bounds it: small blocks, of which a CU holds several
     if ((symmetric && c.bm != c.bn) || ((s == kMiddle || s == kBroad) && form != kAlong)) continue;
     const double across = (double)ceil_div(cols, c.bn), blocks = symmetric ? across * (across + 1) / 2 : (double)ceil_div(rows, c.bm) * across;
     for (int split : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
@@ -297,6 +298,14 @@ inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_split
 template <int KIND, bool AA, bool AB, class E>
 sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
   constexpr int kPair = KIND == tile::KIND_MX ? 1 : 2;  // (its scales need LDS too: two blocks a CU instead)
+  if constexpr (KIND == tile::KIND_F32) {
+    switch (p.shape) {
+      case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      case kFlat: return launch<KIND, 32, 128, 1, 4, 3, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      case kTall: return launch<KIND, 128, 32, 4, 1, 3, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      default: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    }
+  } else {
   switch (p.shape) {
     case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kBroad:
@@ -309,6 +318,7 @@ sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t r
     case kSmall: return launch<KIND, 64, 64, 2, 2, 4, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     default: return launch<KIND, 128, 32, 4, 1, 3, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+  }
   }
 }
 

@@ -21,15 +21,19 @@
 #include "dense.h"
 #include "few.h"
 
+#include <type_traits>
+
 using namespace dense;
 using tile::Block;
 using tile::KIND_BF16;
+using tile::KIND_F32;
 using tile::KIND_SPLIT;
 
 namespace {
 
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
+constexpr int64_t kPlain = 128;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kTopBlocks = 512;
 constexpr int kGradExponent = 15;  // fp16 parts of exp(l - lse) - [v = y] hold it times 2^15
@@ -46,6 +50,7 @@ __device__ __forceinline__ bool counted(const int64_t *labels, int64_t t, int64_
 struct Scalars {
   float top[3][kTopBlocks];  // largest finite magnitudes of x (counted rows), of w, of x times its rows' weights, by workgroup
   float mean;                // 1 / (number of counted rows), at most 1
+  float heaviest;            // the largest magnitude of the counted rows' weights (1 if that is 0)
 };
 
 __device__ __forceinline__ float finite_magnitude(float v) {
@@ -61,21 +66,29 @@ __device__ __forceinline__ float max_of_workgroup(float m, float (&part)[4]) {
   return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
 }
 
-// The number of counted rows, by a workgroup of 256.
-__device__ __forceinline__ void count_rows(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) {
+// The number of counted rows and their heaviest weight, by a workgroup of 256.
+__device__ __forceinline__ void count_rows(const int64_t *labels, int64_t rows, int64_t classes, const float *weights, Scalars *out) {
   __shared__ int part[4];
+  __shared__ float tops[4];
   int n = 0;
+  float top = 0.0f;
 #pragma unroll 8
-  for (int64_t t = threadIdx.x; t < rows; t += 256) n += counted(labels, t, classes);
+  for (int64_t t = threadIdx.x; t < rows; t += 256) {
+    const bool live = counted(labels, t, classes);
+    n += live;
+    if (weights && live) top = fmaxf(top, finite_magnitude(weights[t]));
+  }
+  if (weights) top = max_of_workgroup(top, tops);
   for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
   __syncthreads();
   if (threadIdx.x == 0) {
     n = part[0] + part[1] + part[2] + part[3];
     out->mean = 1.0f / (float)(n > 1 ? n : 1);
+    out->heaviest = top > 0.0f ? top : 1.0f;
   }
 }
-__global__ __launch_bounds__(256) void k_count(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) { count_rows(labels, rows, classes, out); }
+__global__ __launch_bounds__(256) void k_count(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) { count_rows(labels, rows, classes, nullptr, out); }
 
 __device__ __forceinline__ float top4(f32x4 v, float w) {
   return fmaxf(fmaxf(finite_magnitude(v[0] * w), finite_magnitude(v[1] * w)), fmaxf(finite_magnitude(v[2] * w), finite_magnitude(v[3] * w)));
@@ -98,7 +111,7 @@ struct Rows {
 // first workgroup). Bound by memory.
 __global__ __launch_bounds__(256) void k_survey(Rows x, Rows w, Rows xg, int64_t cols, const int64_t *labels, int64_t classes, Scalars *scalars) {
   __shared__ float part[4];
-  if (blockIdx.x == 0) return count_rows(labels, x.rows, classes, scalars);
+  if (blockIdx.x == 0) return count_rows(labels, x.rows, classes, nullptr, scalars);
   const int which = (blockIdx.x - 1) / kTopBlocks, block = (blockIdx.x - 1) % kTopBlocks;
   const Rows &m = which == 0 ? x : which == 1 ? w : xg;
   float top = 0.0f;
@@ -154,27 +167,29 @@ __global__ __launch_bounds__(256) void k_split_rows(Rows x, Rows w, Rows xg, int
   }
 }
 
-// bf16 rows on 16-byte aligned rows of `pitch` values, zeros past `cols` and in rows without a label. With `scalars`, the
-// last workgroup counts the rows that have one.
-__global__ __launch_bounds__(256) void k_copy_rows(const __bf16 *x, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, const int64_t *labels, int64_t classes, bool vec, __bf16 *out,
+// Rows on 16-byte aligned rows of `pitch` values, zeros past `cols` and in rows without a label. With `scalars`, the last
+// workgroup counts the rows that have one and finds the heaviest weight.
+template <class T>
+__global__ __launch_bounds__(256) void k_copy_rows(const T *x, int64_t ld, int64_t rows, int64_t cols, int64_t pitch, const int64_t *labels, int64_t classes, const float *weights, bool vec, T *out,
                                                    Scalars *scalars) {
-  if (scalars && blockIdx.x == gridDim.x - 1) return count_rows(labels, rows, classes, scalars);
+  if (scalars && blockIdx.x == gridDim.x - 1) return count_rows(labels, rows, classes, weights, scalars);
+  constexpr int kEach = 16 / sizeof(T);
+  typedef T Chunk __attribute__((ext_vector_type(kEach)));
   const int step = (int)gridDim.x - (scalars ? 1 : 0);
   for (int64_t r = blockIdx.x; r < rows; r += step) {
     const bool live = !labels || counted(labels, r, classes);
-    for (int64_t k = threadIdx.x * 8; k < pitch; k += 2048) {
-      typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-      bf16x8 v = {};
+    for (int64_t k = threadIdx.x * kEach; k < pitch; k += 256 * kEach) {
+      Chunk v = {};
       if (live) {
-        if (vec && k + 8 <= cols) {
-          v = *(const bf16x8 *)(x + r * ld + k);
+        if (vec && k + kEach <= cols) {
+          v = *(const Chunk *)(x + r * ld + k);
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kEach; ++i)
             if (k + i < cols) v[i] = x[r * ld + k + i];
         }
       }
-      *(bf16x8 *)(out + r * pitch + k) = v;
+      *(Chunk *)(out + r * pitch + k) = v;
     }
   }
 }
@@ -186,7 +201,7 @@ struct LogitScale {
 };
 template <int KIND>
 __device__ __forceinline__ int whole_exponent(const LogitScale &s) {
-  if (KIND == KIND_BF16 || s.row) return 0;
+  if (KIND != KIND_SPLIT || s.row) return 0;
   return split_exponent(top_of(s.top_x)) + split_exponent(top_of(s.top_w));
 }
 
@@ -281,12 +296,14 @@ sdnn_status join_parts(const float2 *parts, int64_t count, const float *picked, 
   return launched("loss");
 }
 
-// Gradient: the piece's G. bf16: with the row's weight; split: without it, times 2^15.
+// Gradient: the piece's exp(l - lse) - [v = y], zeros in rows without a label. Split: times 2^15, weights are left to the
+// products. bf16: times the row's weight over the heaviest, so that equal weights (a mean's) are a factor of one and the
+// label's -1 is exact; a common factor that were rounded here would be off by as much in every row's gradient.
 template <int KIND>
 struct WriteGrad {
   LogitScale scale;
   const int64_t *labels;
-  const float *lse, *weights;  // weights == nullptr: the mean over the counted rows
+  const float *lse, *weights;
   const Scalars *scalars;
   int64_t rows, all, first, classes;  // all classes; the piece's first and number
   char *g;
@@ -295,14 +312,14 @@ struct WriteGrad {
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
     const int e = whole_exponent<KIND>(scale);
-    const float mean = weights ? 0.0f : scalars->mean;
+    const float heaviest = KIND != KIND_SPLIT && weights ? scalars->heaviest : 1.0f;
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t t = row0 + 16 * i + i16;
       const bool in = t < rows, live = in && counted(labels, t, all);
       const int64_t y = in ? labels[t] - first : -1;
       const float z = live ? lse[t] : 0.0f;
-      const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : live ? (weights ? weights[t] : mean) : 0.0f;
+      const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : weights && live ? weights[t] / heaviest : 1.0f;
       const auto value = [&](int j) {
         const int64_t v = col0 + 16 * j + 4 * j4;
         f32x4 o;
@@ -323,7 +340,8 @@ struct WriteGrad {
           if (in && split_at(v) < pitch) store_split4(g + t * pitch, v, o);
         }
       } else {
-        store_row<__bf16, B::kTN>((__bf16 *)(g + t * pitch), col0, pitch / 2, true, in, value);
+        using G = std::conditional_t<KIND == KIND_F32, float, __bf16>;
+        store_row<G, B::kTN>((G *)(g + t * pitch), col0, pitch / (int)sizeof(G), true, in, value);
       }
     }
   }
@@ -333,7 +351,7 @@ struct WriteGrad {
 // the row's weight. A sum of zero stays zero whatever the weight: rows without a label.
 struct OutScale {
   const float *rows;
-  const float *mean;
+  const float *mean;  // or another common factor
   const float *top;  // of the operand that was split (nullptr: none)
   struct Found {
     float mean;
@@ -423,9 +441,11 @@ struct Sizes {
   int32_t dtype;
   int64_t per_slab() const { return dtype == SDNN_BF16 ? 64 : 32; }
   int64_t groups() const { return ceil_div(features, 32); }
-  int64_t pitch_values() const { return ceil_div(features, 8) * 8; }  // bf16 rows that had to be copied
-  size_t packed(int64_t n) const { return dtype == SDNN_BF16 ? (size_t)(n * pitch_values() * 2) : (size_t)(n * groups() * 128); }
-  int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : KIND_SPLIT; }
+  int64_t pitch_values() const { return ceil_div(features, 8) * 8; }  // rows that had to be copied
+  size_t packed(int64_t n) const { return kind() == KIND_SPLIT ? (size_t)(n * groups() * 128) : (size_t)(n * pitch_values() * dtype_bytes(dtype)); }
+  // fp32 operands go to the fp32 matrix instructions as they are up to kPlain rows or classes: the other matrix is
+  // then the larger one, and writing it in two parts would cost more than its products.
+  int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, classes) <= kPlain ? KIND_F32 : KIND_SPLIT; }
   // Classes of a piece: 2^26 values of G, whole blocks of 256 classes.
   int64_t piece() const {
     const int64_t p = std::max<int64_t>(256, std::min(kPieceClasses, kPieceValues / std::max<int64_t>(rows, 1)) / 256 * 256);
@@ -442,8 +462,8 @@ struct Sizes {
   few::Fit few() const { return few::fit_of(rows_held() ? rows : classes, features, dtype); }
 };
 
-bool usable_in_place(const void *p, int64_t ld, int64_t cols) {
-  return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld * 2 <= kMaxPitch;
+bool usable_in_place(const void *p, int64_t ld, int64_t cols, int bytes) {
+  return ((uintptr_t)p & 15) == 0 && ld * bytes % 16 == 0 && cols * bytes % 16 == 0 && ld * bytes <= kMaxPitch;
 }
 
 // A call's workspace and the plans of its products.
@@ -481,7 +501,7 @@ struct GradSpace {
     }
     x = c.take<char>(s.packed(s.rows));
     w = c.take<char>(s.packed(s.classes));
-    xg = c.take<char>(s.dtype == SDNN_FP32 ? s.packed(s.rows) : 0);
+    xg = c.take<char>(s.kind() == KIND_SPLIT ? s.packed(s.rows) : 0);
     g = c.take<char>((size_t)(s.rows * s.g_pitch()));
     const int64_t piece = s.piece(), rest = s.classes % piece;
     dx_plan = s.dx();
@@ -502,12 +522,15 @@ unsigned row_grid(int64_t rows) { return (unsigned)std::max<int64_t>(1, std::min
 
 bool aligned16(const void *p, int64_t ld, int bytes) { return ((uintptr_t)p & 15) == 0 && ld * bytes % 16 == 0; }
 
-// bf16 rows as an operand: in place, or copied into `space` (always with labels; then the counted rows are counted too).
-Matrix bf16_rows(const __bf16 *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, Scalars *scalars, char *space, hipStream_t stream) {
-  if (!labels && usable_in_place(data, ld, s.features)) return {(const char *)data, ld * 2, rows, s.features * 2, 0};
-  hipLaunchKernelGGL(k_copy_rows, dim3(row_grid(rows) + (scalars ? 1 : 0)), dim3(256), 0, stream, data, ld, rows, s.features, s.pitch_values(), labels, s.classes, aligned16(data, ld, 2), (__bf16 *)space,
-                     scalars);
-  return {space, s.pitch_values() * 2, rows, s.pitch_values() * 2, 0};
+// Rows as an operand of their own type: in place, or copied into `space` (always with labels; then the counted rows are
+// counted too).
+template <class T>
+Matrix plain_rows(const T *data, int64_t ld, int64_t rows, const Sizes &s, const int64_t *labels, const float *weights, Scalars *scalars, char *space, hipStream_t stream) {
+  constexpr int kBytes = sizeof(T);
+  if (!labels && usable_in_place(data, ld, s.features, kBytes)) return {(const char *)data, ld * kBytes, rows, s.features * kBytes, 0};
+  hipLaunchKernelGGL((k_copy_rows<T>), dim3(row_grid(rows) + (scalars ? 1 : 0)), dim3(256), 0, stream, data, ld, rows, s.features, s.pitch_values(), labels, s.classes, weights,
+                     aligned16(data, ld, kBytes), (T *)space, scalars);
+  return {space, s.pitch_values() * kBytes, rows, s.pitch_values() * kBytes, 0};
 }
 
 Matrix split_matrix(const Rows &r, const Sizes &s) { return {r.out, s.groups() * 128, r.rows, s.groups() * 128, 0}; }
@@ -559,9 +582,9 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     return st != SDNN_OK ? st : join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
   }
   Matrix a, b;
-  if constexpr (KIND == KIND_BF16) {
-    a = bf16_rows(x, ldx, s.rows, s, nullptr, nullptr, sp.x, stream);
-    b = bf16_rows(w, ldw, s.classes, s, nullptr, nullptr, sp.w, stream);
+  if constexpr (KIND != KIND_SPLIT) {
+    a = plain_rows(x, ldx, s.rows, s, nullptr, nullptr, nullptr, sp.x, stream);
+    b = plain_rows(w, ldw, s.classes, s, nullptr, nullptr, nullptr, sp.w, stream);
   } else {
     const Rows rx{x, ldx, s.rows, nullptr, nullptr, nullptr, sp.ex, sp.x, aligned16(x, ldx, 4)};
     const Rows rw{w, ldw, s.classes, nullptr, nullptr, nullptr, sp.ew, sp.w, aligned16(w, ldw, 4)};
@@ -622,11 +645,11 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     const Store<T> to{d_held, ld_d_held, p.held_rows, s.features, vector_rows(d_held, ld_d_held), {nullptr, nullptr, nullptr}};
     return sum_slabs(sp.few, (int)few::grid_of(s.few(), p.stream_rows, true), s.ld_slab(), to, stream, "gradient");
   }
-  Matrix a, b, ag;  // ag: dw's other operand: the rows, in fp32 times their weights (in bf16 G holds the weights)
+  Matrix a, b, ag;  // ag: dw's other operand: the rows, in fp32 times their weights
   float *top_x = nullptr, *top_w = nullptr, *top_g = nullptr;
-  if constexpr (KIND == KIND_BF16) {
-    ag = a = bf16_rows(x, ldx, s.rows, s, labels, sp.scalars, sp.x, stream);
-    b = bf16_rows(w, ldw, s.classes, s, nullptr, nullptr, sp.w, stream);
+  if constexpr (KIND != KIND_SPLIT) {
+    ag = a = plain_rows(x, ldx, s.rows, s, labels, weights, sp.scalars, sp.x, stream);
+    b = plain_rows(w, ldw, s.classes, s, nullptr, nullptr, nullptr, sp.w, stream);
   } else {
     const bool weighted = weights && dw;
     top_x = sp.scalars->top[0];
@@ -646,7 +669,8 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     ag = weighted ? split_matrix(rg, s) : a;
   }
   st = launched("gradient");
-  const float *mean = KIND == KIND_SPLIT && !weights ? &sp.scalars->mean : nullptr;
+  // what the products are multiplied by in the end: the mean's factor, or the weights
+  const float *mean = !weights ? &sp.scalars->mean : KIND != KIND_SPLIT ? &sp.scalars->heaviest : nullptr;
   const float *row_weights = KIND == KIND_SPLIT ? weights : nullptr;
   const Plan &px = sp.dx_plan;
   const int64_t piece = s.piece();
@@ -660,7 +684,7 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     const WriteGrad<KIND> e{{nullptr, nullptr, top_x, top_w}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
     st = run_shape<KIND, false, false>(sp.logits[n < piece], a, wp, s.rows, n, s.features, e, stream, "gradient");
     if (st != SDNN_OK) return st;
-    const int64_t wide = KIND == KIND_SPLIT ? ceil_div(n, 32) * 128 : ceil_div(n, 8) * 16;  // bytes of a row of G
+    const int64_t wide = KIND == KIND_SPLIT ? ceil_div(n, 32) * 128 : ceil_div(n * (int64_t)sizeof(T), 16) * 16;  // bytes of a row of G
     if (dx) {
       const Store<T> to{dx, lddx, s.rows, s.features, vector_rows(dx, lddx), {row_weights, mean, top_w}, v0 > 0 && px.splits == 1 ? sp.dx : nullptr, s.ld_slab()};
       const bool direct = !through_x || (last && px.splits == 1);
@@ -707,8 +731,9 @@ sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t
   if (!labels || !loss) return fail(SDNN_EINVAL, "labels or loss is null");
   const Sizes s{n_rows, n_classes, n_features, dtype};
   const hipStream_t stream = (hipStream_t)hip_stream;
-  return dtype == SDNN_BF16 ? loss_of<KIND_BF16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream)
-                            : loss_of<KIND_SPLIT>(s, (const float *)x, ldx, (const float *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream);
+  if (dtype == SDNN_BF16) return loss_of<KIND_BF16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream);
+  if (s.kind() == KIND_F32) return loss_of<KIND_F32>(s, (const float *)x, ldx, (const float *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream);
+  return loss_of<KIND_SPLIT>(s, (const float *)x, ldx, (const float *)w, ldw, labels, loss, lse, workspace, workspace_bytes, stream);
 }
 
 sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t dtype, const int64_t *labels, const float *lse, const float *row_grad, int64_t n_rows,
@@ -727,6 +752,8 @@ sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (dtype == SDNN_BF16)
     return grad_of<KIND_BF16, __bf16>(s, (const __bf16 *)x, ldx, (const __bf16 *)w, ldw, labels, lse, row_grad, (__bf16 *)dx, lddx, (__bf16 *)dw, lddw, workspace, workspace_bytes, stream);
+  if (s.kind() == KIND_F32)
+    return grad_of<KIND_F32, float>(s, (const float *)x, ldx, (const float *)w, ldw, labels, lse, row_grad, (float *)dx, lddx, (float *)dw, lddw, workspace, workspace_bytes, stream);
   return grad_of<KIND_SPLIT, float>(s, (const float *)x, ldx, (const float *)w, ldw, labels, lse, row_grad, (float *)dx, lddx, (float *)dw, lddw, workspace, workspace_bytes, stream);
 }
 

@@ -9,6 +9,8 @@
 //               operands give it, at a third of the fp16 matrix rate (the fp32 matrix instructions run at a
 //               sixteenth of it).
 //   KIND_MX     256 4-bit values a slab with one power-of-two scale per 32 (see mx.hip).
+//   KIND_F32    32 fp32 values a slab as they are, on the fp32 matrix instructions: exact products at a sixteenth of
+//               the bf16 rate, for products that memory bounds and whose operands are not worth writing in two parts.
 //
 // An operand is "along" (rows of k: k is contiguous, 128 bytes of each row make the slab) or "across" (rows are k:
 // the slab is 64 or 32 rows of BM or BN values, read from LDS through the transposing reads).
@@ -26,7 +28,7 @@
 
 namespace tile {
 
-enum Kind { KIND_BF16 = 0, KIND_SPLIT = 1, KIND_MX = 2 };
+enum Kind { KIND_BF16 = 0, KIND_SPLIT = 1, KIND_MX = 2, KIND_F32 = 3 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -53,7 +55,7 @@ struct Operand {
 // Values per slab, bytes per value of an across operand.
 template <int KIND>
 struct Geometry {
-  static constexpr int kPerSlab = KIND == KIND_BF16 ? 64 : KIND == KIND_SPLIT ? 32 : 256;
+  static constexpr int kPerSlab = KIND == KIND_BF16 ? 64 : KIND == KIND_MX ? 256 : 32;
   static constexpr int kBytes = KIND == KIND_BF16 ? 2 : 4;
 };
 
@@ -92,9 +94,10 @@ struct Loader {
   static constexpr int kRowsPerRound = kRound / kRowBytes;
   static constexpr int kSlabRows = kData / kRowBytes;
   static_assert(kData % kRound == 0 || kRounds == 1, "whole rounds");
-  static_assert(kRound % kRowBytes == 0 && kRowsPerRound % (ACROSS ? 4 : 8) == 0, "the permutation repeats every round");
+  static_assert(kRound % kRowBytes == 0 && kRowsPerRound % (ACROSS ? KIND == KIND_F32 ? 1 : 4 : 8) == 0, "the permutation repeats every round");
 
-  static constexpr int kTurn = (kRowBytes / 16 - 1) & 6;  // chunk bits that an across row's number permutes
+  // chunk bits that an across row's number permutes (fp32 columns are read value by value and stay)
+  static constexpr int kTurn = KIND == KIND_F32 ? 0 : (kRowBytes / 16 - 1) & 6;
 
   uint32_t offset;  // this lane's bytes from the slab's origin
   int chunk;        // its 16-byte chunk within the row
@@ -179,7 +182,10 @@ struct Reader {
   // wave's part is wider than 32.
   __device__ __forceinline__ void init(int first) {
     const int lane = threadIdx.x & 63, i = lane & 15, j = lane >> 4;
-    if (ACROSS) {
+    if constexpr (ACROSS && KIND == KIND_F32) {
+      // group j takes rows of k 4 j ... 4 j + 3, as it does of an along row's 16-byte chunk
+      at[0] = 4 * j * kRowBytes + (first + i) * 4;
+    } else if (ACROSS) {
       // lane i of 16 points at row i / 4 of four rows of k, 8 bytes (4 columns) at i % 4; after the
       // transposing read it holds column i of the four rows
       const int r = i >> 2;
@@ -209,6 +215,11 @@ struct Reader {
   __device__ __forceinline__ i32x4 read(const char *lds, int i, int q) const {
     if constexpr (!ACROSS) {
       return *(const i32x4 *)(lds + at[q] + i * (16 * kSlab));
+    } else if constexpr (KIND == KIND_F32) {
+      i32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *(const int *)(lds + at[0] + (16 * q + e) * kRowBytes + i * 64);
+      return v;
     } else {
       int a;
       if constexpr (KIND == KIND_SPLIT) {
@@ -238,7 +249,13 @@ __device__ __forceinline__ f32x4 mfma_mx(i32x4 a, i32x4 b, f32x4 c, int scale_a,
 
 template <int KIND>
 __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
-  if constexpr (KIND == KIND_BF16)
+  if constexpr (KIND == KIND_F32) {
+    // value e of every lane group's four: k = 4 j + e
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+    return c;
+  } else if constexpr (KIND == KIND_BF16)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -317,7 +334,7 @@ struct Block {
   // The order that the scheduler is to keep: products and LDS reads as they are written.
   template <int SUBTILES>
   __device__ __forceinline__ static void products() {
-    if constexpr (SUBTILES > 0) __builtin_amdgcn_sched_group_barrier(0x008, SUBTILES * kTN, 0);
+    if constexpr (SUBTILES > 0) __builtin_amdgcn_sched_group_barrier(0x008, SUBTILES * kTN * (KIND == KIND_F32 ? 4 : 1), 0);
   }
   template <int READS>
   __device__ __forceinline__ static void reads() {
@@ -366,8 +383,9 @@ struct Block {
     for (int i = 0; i < STAGES; ++i) load(s0 + i * GROUPS, i * kStage);
     wait_loads<(STAGES - 1) * kLoads>();
     meet();
-    constexpr int kEach = kMx ? 2 : ACROSS_A ? 2 : 1;                      // LDS reads with a subtile of A
-    constexpr int kAll = kTN * (kMx ? 2 : ACROSS_B ? 2 : 1);               // with all of B
+    constexpr int kAcross = KIND == KIND_F32 ? 4 : 2;                      // LDS reads of a fragment across
+    constexpr int kEach = kMx ? 2 : ACROSS_A ? kAcross : 1;                // with a subtile of A
+    constexpr int kAll = kTN * (kMx ? 2 : ACROSS_B ? kAcross : 1);         // with all of B
     i32x4 fa[kTM], fb[kTN], gb[kTN];
     int sa[kTM], sb[kTN];
     read(rb, lds + kValuesA, 0, fb);
@@ -384,7 +402,7 @@ struct Block {
       at = at + 1 == STAGES ? 0 : at + 1;
       const char *then = lds + at * kStage;
       read(rb, now + kValuesA, 1, gb);
-      reads<kTN * (ACROSS_B ? 2 : 1)>();
+      reads<kTN * (ACROSS_B ? kAcross : 1)>();
       if constexpr (KIND == KIND_SPLIT) {
 #pragma unroll
         for (int i = 0; i < kTM; ++i) multiply<0>(i, fa[i], fb, 0, sb);
@@ -395,7 +413,7 @@ struct Block {
         multiply<0>(i, fa[i], KIND == KIND_SPLIT ? gb : fb, sa[i], sb);
         fa[i] = ra.read(now, i, 1);
         products<1>();
-        reads<ACROSS_A ? 2 : 1>();
+        reads<ACROSS_A ? kAcross : 1>();
       }
       constexpr int kDelay = kTM < 4 ? kTM / 2 : 2;
 #pragma unroll

@@ -212,6 +212,20 @@ def test_wide_range():
     c.check()
 
 
+def test_equal_weights_cost_no_precision():
+    """bf16, every row's weight the same and halfway between two bf16 values: a weight rounded by itself would move every
+    gradient by u16. G's and the output's own roundings are independent, each at most 0.5 u16 on average over a binade in
+    the root mean square, so together under 0.75 u16."""
+    log("readout equal weights")
+    c = Case(400, 500, 256, "bfloat16", seed=12)
+    g = c.torch.full((400,), 1.0 + 0.999 * U16 / 2, device="cuda")
+    c.run(g)
+    c.check(g)
+    _, _, dx, dw = reference(c.torch, c.x, c.w, c.y, g)
+    for got, want in ((c.dx, dx[0]), (c.dw, dw[0])):
+        assert float((got.double() - want).norm() / want.norm()) <= 0.75 * U16
+
+
 @pytest.mark.parametrize("what", ["dx", "dw"])
 def test_one_gradient_alone(what):
     log(f"readout {what} alone")
