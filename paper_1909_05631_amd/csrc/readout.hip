@@ -34,6 +34,7 @@ namespace {
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
 constexpr int64_t kPlain = 128;
+constexpr int64_t kSplitLogits = 1 << 22;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kTopBlocks = 512;
 constexpr int kGradExponent = 15;  // fp16 parts of exp(l - lse) - [v = y] hold it times 2^15
@@ -288,6 +289,37 @@ __global__ __launch_bounds__(256) void k_loss(const float2 *parts, int64_t count
   }
 }
 
+// The loss from logits whose k was split: a workgroup sums a row's slabs and takes its softmax.
+template <int KIND>
+__global__ __launch_bounds__(256) void k_loss_slabs(const float *slabs, int splits, int64_t ld, LogitScale scale, const int64_t *labels, int64_t rows, int64_t classes, float *loss, float *lse) {
+  __shared__ float2 shared[4];
+  __shared__ float picked;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t t = blockIdx.x, y = labels[t];
+  Softmax a{-__builtin_inff(), 0.0f};
+  for (int64_t v = threadIdx.x; v < classes; v += 256) {
+    float l = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) l += slabs[(s * rows + t) * ld + v];
+    if (KIND == KIND_SPLIT) l = ldexpf(l, -scale.row[t] - scale.col[v]);
+    if (v == y) picked = l;
+    a.join(l, l == -__builtin_inff() ? 0.0f : 1.0f);
+  }
+  for (int d = 32; d; d >>= 1) {
+    const float top = __shfl_xor(a.top, d), sum = __shfl_xor(a.sum, d);
+    a.join(top, sum);
+  }
+  if (lane == 0) shared[wave] = float2{a.top, a.sum};
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a = {shared[0].x, shared[0].y};
+    for (int w = 1; w < 4; ++w) a.join(shared[w].x, shared[w].y);
+    const float s = a.top + logf(a.sum);
+    if (lse) lse[t] = s;
+    loss[t] = counted(labels, t, classes) ? s - picked : 0.0f;
+  }
+}
+
 sdnn_status join_parts(const float2 *parts, int64_t count, const float *picked, const int64_t *labels, int64_t rows, int64_t classes, float *loss, float *lse, hipStream_t stream) {
   if (count > 256 && rows < 8 * kCus)
     hipLaunchKernelGGL((k_loss<4>), dim3((unsigned)rows), dim3(256), 0, stream, parts, count, picked, labels, rows, classes, loss, lse);
@@ -308,6 +340,17 @@ struct WriteGrad {
   int64_t rows, all, first, classes;  // all classes; the piece's first and number
   char *g;
   int64_t pitch;  // bytes
+  // Four neighbours of a row, from class v of the piece on.
+  __device__ __forceinline__ f32x4 gradient(f32x4 l, int64_t v, int64_t y, bool live, float z, float w, int e) const {
+    f32x4 o;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float s = KIND == KIND_SPLIT ? ldexpf(l[c], -e) : l[c];
+      const float p = exp_of(s - z) - (v + c == y ? 1.0f : 0.0f);
+      o[c] = live && v + c < classes ? w * p : 0.0f;
+    }
+    return o;
+  }
   template <class B>
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
@@ -320,18 +363,7 @@ struct WriteGrad {
       const int64_t y = in ? labels[t] - first : -1;
       const float z = live ? lse[t] : 0.0f;
       const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : weights && live ? weights[t] / heaviest : 1.0f;
-      const auto value = [&](int j) {
-        const int64_t v = col0 + 16 * j + 4 * j4;
-        f32x4 o;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float s = block.acc[i][j][c];
-          if (KIND == KIND_SPLIT) s = ldexpf(s, -e);
-          const float p = exp_of(s - z) - (v + c == y ? 1.0f : 0.0f);
-          o[c] = live && v + c < classes ? w * p : 0.0f;
-        }
-        return o;
-      };
+      const auto value = [&](int j) { return gradient(block.acc[i][j], col0 + 16 * j + 4 * j4, y, live, z, w, e); };
       if constexpr (KIND == KIND_SPLIT) {
 #pragma unroll
         for (int j = 0; j < B::kTN; ++j) {
@@ -346,6 +378,33 @@ struct WriteGrad {
     }
   }
 };
+
+// The same from logits whose k was split.
+template <int KIND>
+__global__ __launch_bounds__(256) void k_grad_slabs(const float *slabs, int splits, int64_t ld, WriteGrad<KIND> to) {
+  const int e = whole_exponent<KIND>(to.scale);
+  const float heaviest = KIND != KIND_SPLIT && to.weights ? to.scalars->heaviest : 1.0f;
+  const int64_t t = blockIdx.y;
+  const bool live = counted(to.labels, t, to.all);
+  const int64_t y = to.labels[t] - to.first;
+  const float z = live ? to.lse[t] : 0.0f;
+  const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : to.weights && live ? to.weights[t] / heaviest : 1.0f;
+  char *row = to.g + t * to.pitch;
+  const int64_t wide = KIND == KIND_BF16 ? to.pitch / 2 : to.pitch / 4;
+  for (int64_t v = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; v < wide; v += (int64_t)gridDim.x * 1024) {
+    f32x4 l = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (v < ld)
+#pragma unroll 4
+      for (int s = 0; s < splits; ++s) l += *(const f32x4 *)(slabs + (s * to.rows + t) * ld + v);
+    const f32x4 o = to.gradient(l, v, y, live, z, w, e);
+    if constexpr (KIND == KIND_SPLIT)
+      store_split4(row, v, o);
+    else if constexpr (KIND == KIND_F32)
+      store4((float *)row + v, o, 4, true);
+    else
+      store4((__bf16 *)row + v, o, 4, true);
+  }
+}
 
 // What a product's sums are multiplied by: the mean and the split operands' powers of two (found once a wave), and
 // the row's weight. A sum of zero stays zero whatever the weight: rows without a label.
@@ -452,8 +511,10 @@ struct Sizes {
     return std::min(p, classes);
   }
   int64_t g_pitch() const { return ceil_div(piece(), per_slab()) * 128; }
-  Plan loss() const { return plan(kind(), rows, classes, features, 1, kAlong); }
-  Plan logits(int64_t n) const { return plan(kind(), rows, n, features, 1, kAlong); }
+  // The logits' k may be split where they are few: their slabs are joined by a row's workgroup.
+  int logit_splits(int64_t n) const { return rows * n <= kSplitLogits && rows <= 65535 ? kMaxSplits : 1; }
+  Plan logits(int64_t n) const { return plan(kind(), rows, n, features, logit_splits(n), kAlong); }
+  size_t logit_slabs(const Plan &p, int64_t n) const { return p.splits > 1 ? (size_t)(p.splits * rows * (ceil_div(n, 4) * 4)) : 0; }
   Plan dx() const { return plan(kind(), rows, features, piece(), kMaxSplits); }
   Plan dw(int64_t n) const { return plan(kind(), n, features, rows, kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
@@ -472,11 +533,11 @@ struct LossSpace {
   char *x, *w;
   int *ex, *ew;
   float2 *parts;
-  float *picked;
+  float *picked, *slabs;
   int64_t count;
   LossSpace(Carver &c, const Sizes &s) {
     const bool packed = s.few() == few::kNone;
-    if (packed) loss = s.loss();
+    if (packed) loss = s.logits(s.classes);
     x = c.take<char>(packed ? s.packed(s.rows) : 0);
     w = c.take<char>(packed ? s.packed(s.classes) : 0);
     ex = c.take<int>(s.rows);
@@ -484,6 +545,7 @@ struct LossSpace {
     count = !packed ? (s.rows_held() ? (int64_t)few::grid_of(s.few(), s.classes, false) * few::batch_of(s.few()) : 0) : ceil_div(s.classes, kWaveCols[loss.shape]);
     parts = c.take<float2>(s.rows * count);
     picked = c.take<float>(s.rows);
+    slabs = c.take<float>(packed ? s.logit_slabs(loss, s.classes) : 0);
   }
 };
 
@@ -491,7 +553,7 @@ struct GradSpace {
   Plan logits[2], dx_plan, dw_plan[2];  // of a whole piece and of the last one
   char *x, *w, *xg, *g;
   Scalars *scalars;
-  float *dx, *dw, *few;
+  float *dx, *dw, *few, *slabs;
   GradSpace(Carver &c, const Sizes &s) {
     scalars = c.take<Scalars>(1);
     if (s.few() != ::few::kNone) {
@@ -515,6 +577,7 @@ struct GradSpace {
       if (dw_plan[i].splits > 1) most = std::max(most, (size_t)(dw_plan[i].splits * n * s.ld_slab()));
     }
     dw = c.take<float>(most);
+    slabs = c.take<float>(std::max(s.logit_slabs(logits[0], piece), rest ? s.logit_slabs(logits[1], rest) : 0));
   }
 };
 
@@ -593,7 +656,15 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     b = split_matrix(rw, s);
   }
   if ((st = launched("rows")) != SDNN_OK) return st;
-  const LossParts<KIND> e{{sp.ex, sp.ew, nullptr, nullptr}, labels, s.rows, s.classes, sp.parts, sp.count, sp.picked};
+  const LogitScale scale{sp.ex, sp.ew, nullptr, nullptr};
+  if (sp.loss.splits > 1) {
+    const int64_t ld = ceil_div(s.classes, 4) * 4;
+    st = run_shape<KIND, false, false>(sp.loss, a, b, s.rows, s.classes, s.features, Accumulate{sp.slabs, ld, s.rows, s.classes, false}, stream, "loss");
+    if (st != SDNN_OK) return st;
+    hipLaunchKernelGGL((k_loss_slabs<KIND>), dim3((unsigned)s.rows), dim3(256), 0, stream, sp.slabs, sp.loss.splits, ld, scale, labels, s.rows, s.classes, loss, lse);
+    return launched("loss");
+  }
+  const LossParts<KIND> e{scale, labels, s.rows, s.classes, sp.parts, sp.count, sp.picked};
   st = run_shape<KIND, false, false>(sp.loss, a, b, s.rows, s.classes, s.features, e, stream, "loss");
   if (st != SDNN_OK) return st;
   return join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
@@ -682,7 +753,16 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     wp.data += v0 * b.pitch;
     wp.rows = n;
     const WriteGrad<KIND> e{{nullptr, nullptr, top_x, top_w}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
-    st = run_shape<KIND, false, false>(sp.logits[n < piece], a, wp, s.rows, n, s.features, e, stream, "gradient");
+    const Plan &pl = sp.logits[n < piece];
+    if (pl.splits > 1) {
+      const int64_t ld = ceil_div(n, 4) * 4;
+      st = run_shape<KIND, false, false>(pl, a, wp, s.rows, n, s.features, Accumulate{sp.slabs, ld, s.rows, n, false}, stream, "gradient");
+      if (st != SDNN_OK) return st;
+      hipLaunchKernelGGL((k_grad_slabs<KIND>), dim3((unsigned)std::min<int64_t>(ceil_div(s.g_pitch(), 2048), 64), (unsigned)s.rows), dim3(256), 0, stream, sp.slabs, pl.splits, ld, e);
+      st = launched("gradient");
+    } else {
+      st = run_shape<KIND, false, false>(pl, a, wp, s.rows, n, s.features, e, stream, "gradient");
+    }
     if (st != SDNN_OK) return st;
     const int64_t wide = KIND == KIND_SPLIT ? ceil_div(n, 32) * 128 : ceil_div(n * (int64_t)sizeof(T), 16) * 16;  // bytes of a row of G
     if (dx) {
