@@ -523,8 +523,9 @@ struct Sizes {
   few::Fit few() const { return few::fit_of(rows_held() ? rows : classes, features, dtype); }
 };
 
+// Rows that the tiles read as they are: whole dwords.
 bool usable_in_place(const void *p, int64_t ld, int64_t cols, int bytes) {
-  return ((uintptr_t)p & 15) == 0 && ld * bytes % 16 == 0 && cols * bytes % 16 == 0 && ld * bytes <= kMaxPitch;
+  return ((uintptr_t)p & 3) == 0 && ld * bytes % 4 == 0 && cols * bytes % 4 == 0 && ld * bytes <= kMaxPitch;
 }
 
 // A call's workspace and the plans of its products.

@@ -43,7 +43,8 @@ constexpr uint32_t kOut = 0x7fffff00;  // an offset past every operand: reads ze
 
 // One operand of a block. along: `base` is the block's first row, `rows` its rows inside the operand,
 // `extent` the bytes of k. across: `base` is the block's first column, `rows` the rows of k, `extent` the
-// bytes of columns inside the operand. `pitch`: bytes from row to row; 16-byte aligned, as is base.
+// bytes of columns inside the operand. `pitch`: bytes from row to row; 4-byte aligned, as are base
+// and an along extent.
 // 256 pitches stay under 2^31 (checked on the host).
 // KIND_MX: `scales` is the first row's scale bytes, pitch / 16 of them a row.
 struct Operand {
@@ -331,6 +332,14 @@ struct Block {
     op.extent = uniform(op.extent);
   }
 
+  // The last slab of rows that end within a 16-byte chunk holds what follows them there: zeros take its place.
+  template <int ROWS, int THREADS>
+  __device__ __forceinline__ static void trim(char *lds, int extent) {
+    const int chunk = (extent % kSlab) / 16, first = extent % 16 / 4;
+    for (int r = threadIdx.x % THREADS; r < ROWS; r += THREADS)
+      for (int i = first; i < 4; ++i) *(int *)(lds + r * kSlab + ((chunk ^ (r & 7)) * 16) + i * 4) = 0;
+  }
+
   // The order that the scheduler is to keep: products and LDS reads as they are written.
   template <int SUBTILES>
   __device__ __forceinline__ static void products() {
@@ -383,6 +392,16 @@ struct Block {
     for (int i = 0; i < STAGES; ++i) load(s0 + i * GROUPS, i * kStage);
     wait_loads<(STAGES - 1) * kLoads>();
     meet();
+    const bool ragged_a = !ACROSS_A && (a.extent & 15), ragged_b = !ACROSS_B && (b.extent & 15);
+    const auto trim_last = [&](int s, char *stage) {
+      if (!ragged_a && !ragged_b) return;
+      const int s_a = (a.extent - 1) / kSlab, s_b = (b.extent - 1) / kSlab, round = s - group();
+      const bool now_a = ragged_a && s_a >= round && s_a < round + GROUPS, now_b = ragged_b && s_b >= round && s_b < round + GROUPS;
+      if (now_a && s_a == s) trim<BM, kGroup>(stage, a.extent);
+      if (now_b && s_b == s) trim<BN, kGroup>(stage + kValuesA, b.extent);
+      if (now_a || now_b) meet();
+    };
+    if constexpr (KIND != KIND_SPLIT && !kMx) trim_last(s0, lds);
     constexpr int kAcross = KIND == KIND_F32 ? 4 : 2;                      // LDS reads of a fragment across
     constexpr int kEach = kMx ? 2 : ACROSS_A ? kAcross : 1;                // with a subtile of A
     constexpr int kAll = kTN * (kMx ? 2 : ACROSS_B ? kAcross : 1);         // with all of B
@@ -426,6 +445,7 @@ struct Block {
       // slab s + 1 has arrived; all fragments of slab s are in registers
       wait_loads<(STAGES - 2) * kLoads>();
       meet();
+      if constexpr (KIND != KIND_SPLIT && !kMx) trim_last(s + GROUPS, lds + at * kStage);
       constexpr bool kSpread = kTM >= 8 && GROUPS == 1;  // a small block has no time to spread its loads over
       if constexpr (kSpread)
         load_scales(s + STAGES, used);
