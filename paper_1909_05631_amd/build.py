@@ -9,7 +9,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libsdnn.so")
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("sdnn.hip", "readout.hip", "orthogonalize.hip", "mx.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("library.hip", "readout.hip", "orthogonalize.hip", "mx.hip")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

@@ -14,6 +14,7 @@
 
 namespace dense {
 
+using sdnn_error::fail;
 using tile::f32x4;
 
 constexpr int kXcds = 8;

@@ -56,12 +56,11 @@
 #include <utility>
 #include <vector>
 
-#include "error.h"
 #include "sdnn.h"
 
 namespace {
+
 thread_local std::string g_err;
-}  // namespace
 
 sdnn_status fail(sdnn_status s, const char *fmt, ...) {
   char buf[512];
@@ -76,8 +75,6 @@ sdnn_status fail(sdnn_status s, const char *fmt, ...) {
   }
   return s;
 }
-
-namespace {
 
 // The answer of an entry point in which an allocation on the host failed: no exception crosses the ABI.
 sdnn_status no_memory() { return fail(SDNN_ENOMEM, "out of host memory"); }
