@@ -190,7 +190,7 @@ const char *sdnn_last_error(void);
  * 1 = tiles gathered from global memory (widths too large for LDS). -1 for NULL. */
 int32_t sdnn_kernel_path(const sdnn_net *net);
 
-/* ---------------------------------------------------------------------------------------------------------
+/* ---------------------------------------------------------------------------------------------------------------
  * The dense readout: a layer of n_classes outputs on rows of n_features values, such as a network's final rows
  * (sdnn_final_rows) on the device. These calls need no handle. All matrices are row-major in device memory; a
  * stride is the distance of two rows in values and at least the row's length. Everything is enqueued on
@@ -207,19 +207,21 @@ typedef enum {
 } sdnn_dtype;
 
 /* Bytes of workspace for sdnn_readout_loss (gradient = 0) or for both calls (gradient = 1). It grows with
- * n_rows * n_features and n_features * n_classes (fp32 operands are held in two 16-bit parts), not with
- * n_rows * n_classes. 0 for sizes that the calls refuse: n_rows in [0, 2^24], n_classes in [1, 2^24], n_features in
- * [1, 2^20]. */
+ * n_rows * n_features and n_features * n_classes (fp32 operands are held in two 16-bit parts, unaligned ones are
+ * copied), not with n_rows * n_classes past 2^26 of them. 0 for sizes that the calls refuse: n_rows in [0, 2^24],
+ * n_classes in [1, 2^24], n_features in [1, 2^20]. */
 size_t sdnn_readout_workspace_bytes(int64_t n_rows, int64_t n_classes, int64_t n_features, int32_t dtype,
                                     int32_t gradient);
 
-/* Softmax cross entropy of the logits l = x w^T, which are not kept.
+/* Softmax cross entropy of the logits l = x w^T, which are not kept (where there are at most 2^24 of
+ * them, sums of parts of them may pass through the workspace).
  *   x: n_rows x n_features, w: n_classes x n_features, both of `dtype`, row strides ldx and ldw.
  *   labels: n_rows int64. A label outside [0, n_classes) leaves its row out: its loss is 0.
  *   loss: n_rows fp32, lse_t - l_{t, label}.  lse: n_rows fp32 (or NULL), log sum_v exp l_tv, also of rows
  *   that are left out; sdnn_readout_grad needs it.
- * Sums are fp32, of exact products for bf16 inputs; fp32 inputs are multiplied as two fp16 parts each (22 bits or
- * more of each value down to 2^-17 of its row's largest). A row that holds an infinity or a NaN has a NaN loss. */
+ * Sums are fp32, of exact products for bf16 inputs; fp32 inputs are multiplied as they are or as two fp16 parts each
+ * (22 bits or more of each value down to 2^-17 of its row's largest). A row that holds an infinity or a NaN has a NaN
+ * loss. */
 sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t dtype,
                               const int64_t *labels, int64_t n_rows, int64_t n_classes, int64_t n_features,
                               float *loss, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -8,7 +8,8 @@
 //   gradient: G_hs from l_hs and the given lse;  d stream_s = sum_h G_hs held_h  is written,
 //             d held_h += G_hs stream_s  stays in registers, one slab per workgroup at the end
 //
-// Bound by memory: the streamed matrix once, its gradient once. A sum across 64 lanes of N values takes N + log2(64 / N)
+// Bound by memory where rows are long (the streamed matrix once, its gradient once: 65536 x 1024 fp32 against one row 45 us,
+// 6.0 TB/s), by the sums across lanes where they are short. A sum across 64 lanes of N values takes N + log2(64 / N)
 // shuffles: each step a lane hands on the half of the values that its neighbour keeps.
 #ifndef SDNN_FEW_H
 #define SDNN_FEW_H
@@ -290,15 +291,24 @@ __global__ __launch_bounds__(kThreads) void k_few(Few<T> p) {
   }
 }
 
-// The held rows and columns that registers take, and how many streamed rows go at a time. Up to 4 rows in fp32, where the
-// tiles first write the other matrix in two parts (65536 x 1024: loss 45 us for one row and 130 for four, 225 in
-// tiles); one row in bf16, whose gradient here has no rounding between its sums (88 us, 102 in tiles; the
-// tiles stream the loss of one row at 5.2 TB/s, this at 3.6, and are far ahead from two rows on).
+// The held rows and columns that registers take, and how many streamed rows go at a time: up to 4 rows in fp32, one in
+// bf16, where all of the few go at once (two bf16 rows are far ahead in tiles). Past that it is a matter of two costs.
+// A streamed row costs its sum across the workgroup, about 2 ns for four held rows, whatever its length; the tiles
+// cost launches (us for the loss / the gradient, here and in tiles):
+//   few streamed rows, where launches count: 4 x 2048 x 1024 fp32 13/18 and 19/28, 4 x 8192 x 1024 22/47 and 25/46,
+//     one row of bf16 8192 x 1024 12/18 and 12/29, 1000 x 16384 13/31 and 31/41 (but 4096 x 16384 33/132 and 38/98);
+//   many rows: only long ones are worth their sums. Four held, fp32: 200000 x 100 381/882 and 46/139, 30000 x 1500
+//     52/173 and 41/139, 30000 x 2048 53/183 and 49/196, 32768 x 4096 95/261 and 123/428. One, fp32: 100000 x 256
+//     49/117 and 40/109, 100000 x 512 50/143 and 62/174, 65536 x 1024 45/127 and 56/230. One, bf16: 200000 x 100 121/315
+//     and 24/89, 30000 x 2048 37/88 and 25/91, 32768 x 4096 42/140 and 47/222, 16384 x 8192 94/328 and 85/235.
 enum Fit { kNone, kOneShort, kOneMiddle, kOneLong, kFourShort, kFourMiddle };
-inline Fit fit_of(int64_t held, int64_t features, int32_t dtype) {
-  if (held <= 1) return features <= kColumns ? kOneShort : features <= 4 * kColumns ? kOneMiddle : features <= 16 * kColumns ? kOneLong : kNone;
-  if (held <= 4 && dtype == SDNN_FP32) return features <= kColumns ? kFourShort : features <= 4 * kColumns ? kFourMiddle : kNone;
-  return kNone;
+inline Fit fit_of(int64_t held, int64_t streamed, int64_t features, int32_t dtype) {
+  const bool fp32 = dtype == SDNN_FP32;
+  if (held > (fp32 ? 4 : 1) || features > (held > 1 ? 4 : 16) * kColumns) return kNone;
+  const bool long_bf16 = !fp32 && features > 4 * kColumns;
+  if (streamed > (long_bf16 ? 1024 : 8192) && (long_bf16 || (fp32 ? features < (held > 1 ? 2048 : 512) : features <= 2048))) return kNone;
+  if (held > 1) return features <= kColumns ? kFourShort : kFourMiddle;
+  return features <= kColumns ? kOneShort : features <= 4 * kColumns ? kOneMiddle : kOneLong;
 }
 inline int batch_of(Fit f) { return f == kOneShort ? 8 : f == kFourShort ? 4 : f == kOneLong ? 1 : 2; }
 // Workgroups: two a CU (each has 16 KB or more of rows on its way), one where each leaves a slab.

@@ -7,24 +7,34 @@
 // A row whose label is outside [0, n_classes) is left out: loss 0, gradient 0, and nothing of it reaches dw,
 // whatever it holds.
 //
-// Loss: one pass over w. A block of 64 ... 256 rows by as many classes has its logits in registers; the epilogue takes
+// Loss: one pass over w. A block of up to 256 rows by as many classes has its logits in registers; the epilogue takes
 // the maximum and the sum of exponentials of its columns per row (fp32), k_loss joins them. Nothing of size
-// n_rows x n_classes is written.
+// n_rows x n_classes is written. Where there are few logits (at most 2^24) and blocks for only a part of the
+// CUs, the features are split instead, and a workgroup a row joins the slabs and takes the softmax.
 // Gradient: piece by piece, the logits are computed again (2 of 8 T V D operations, against a logit matrix in memory),
 // the epilogue writes the piece's G in 16 bits (bf16; fp32 inputs: two fp16 parts), and two products read it, dx +=
 // G w (over the piece's classes) and dw = G^T x (over the rows), both through the transposing LDS reads, so neither
 // w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G: it stays in the Infinity Cache
 // between the products.
 //
-// Few rows or few classes (few.h) have no use for tiles: one kernel with fp32 arithmetic streams the
-// other matrix past them, once.
+// What bounds it, measured on this card (a copy runs at 4.8 TB/s, the library's bf16 product at 1570-1650 TFLOP/s):
+//   8192 x 4096 x 32768, bf16: 6.5 ms, matrix instructions: loss 1.60-1.63 ms (1350-1376 TFLOP/s), each of four pieces
+//     0.42-0.44 ms logits and G, 0.39-0.44 ms dx, 0.37-0.38 ms dw (1480).
+//   64 x 1024 x 65536, bf16: 140 us, memory: w three times (23-25 us each, 5.8 TB/s), dw once (41 us, 3.3 TB/s).
+//   1021 x 1000 x 10007, fp32: 315 us: four products of 65-74 us, 280-310 TFLOP/s of fp32 against 477 of the largest (212
+//     blocks for 256 CUs in the logits, 256 in dx, 160 in dw), 38 us for writing x and w in two parts twice, 12 us
+//     for their largest values.
+//   2000 x 1024 x 10, fp32: 45 us, eight launches of 4 to 9 us.
+//
+// fp32 inputs go as two fp16 parts (tile.h), or, where rows or classes are at most 128, to the fp32 matrix instructions
+// as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts). One to four rows or classes
+// (few.h) mostly have no use for tiles: one kernel with fp32 arithmetic streams the other matrix past them, once.
 #include "dense.h"
 #include "few.h"
 
 #include <type_traits>
 
 using namespace dense;
-using tile::Block;
 using tile::KIND_BF16;
 using tile::KIND_F32;
 using tile::KIND_SPLIT;
@@ -33,8 +43,8 @@ namespace {
 
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
-constexpr int64_t kPlain = 128;
-constexpr int64_t kSplitLogits = 1 << 22;
+constexpr int64_t kPlain = 128;            // fp32 rows or classes for the plain fp32 products: see Sizes::kind
+constexpr int64_t kSplitLogits = 1 << 24;  // logits whose features may be split: past that there is a 256 x 256 block for every CU
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kTopBlocks = 512;
 constexpr int kGradExponent = 15;  // fp16 parts of exp(l - lse) - [v = y] hold it times 2^15
@@ -503,7 +513,8 @@ struct Sizes {
   int64_t pitch_values() const { return ceil_div(features, 8) * 8; }  // rows that had to be copied
   size_t packed(int64_t n) const { return kind() == KIND_SPLIT ? (size_t)(n * groups() * 128) : (size_t)(n * pitch_values() * dtype_bytes(dtype)); }
   // fp32 operands go to the fp32 matrix instructions as they are up to kPlain rows or classes: the other matrix is
-  // then the larger one, and writing it in two parts would cost more than its products.
+  // then the larger one, and writing it in two parts costs more than products that are three times as fast save
+  // (loss and gradient of 128 x 1024 x 65536 613 us; of 129 rows, in two parts, 748; of 16 rows 289 and 609).
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, classes) <= kPlain ? KIND_F32 : KIND_SPLIT; }
   // Classes of a piece: 2^26 values of G, whole blocks of 256 classes.
   int64_t piece() const {
@@ -511,16 +522,19 @@ struct Sizes {
     return std::min(p, classes);
   }
   int64_t g_pitch() const { return ceil_div(piece(), per_slab()) * 128; }
-  // The logits' k may be split where they are few: their slabs are joined by a row's workgroup.
+  // The logits' k may be split where they are few: their slabs are joined by a row's workgroup (5 x 5000 x 1000 fp32: loss
+  // 21 us, 102 unsplit; gradient 42 and 127; 2100 x 2100 x 8192 bf16: 83 and 283, unsplit 125 and 331;
+  // 500 x 12000 x 4096 bf16: 72 us either way).
   int logit_splits(int64_t n) const { return rows * n <= kSplitLogits && rows <= 65535 ? kMaxSplits : 1; }
   Plan logits(int64_t n) const { return plan(kind(), rows, n, features, logit_splits(n), kAlong); }
   size_t logit_slabs(const Plan &p, int64_t n) const { return p.splits > 1 ? (size_t)(p.splits * rows * (ceil_div(n, 4) * 4)) : 0; }
   Plan dx() const { return plan(kind(), rows, features, piece(), kMaxSplits); }
   Plan dw(int64_t n) const { return plan(kind(), n, features, rows, kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
+  few::Fit fit(bool rows_held) const { return rows_held ? few::fit_of(rows, classes, features, dtype) : few::fit_of(classes, rows, features, dtype); }
   // Few rows are held rather than few classes.
-  bool rows_held() const { return few::fit_of(rows, features, dtype) != few::kNone && (rows <= classes || few::fit_of(classes, features, dtype) == few::kNone); }
-  few::Fit few() const { return few::fit_of(rows_held() ? rows : classes, features, dtype); }
+  bool rows_held() const { return fit(true) != few::kNone && (rows <= classes || fit(false) == few::kNone); }
+  few::Fit few() const { return fit(rows_held()); }
 };
 
 // Rows that the tiles read as they are: whole dwords.

@@ -623,3 +623,47 @@ def test_example():
     got = example.main()
     log(str(got))
     assert got["rows"] > 1000 and got["last loss"] < 0.1 * got["first loss"] and got["right"] > 0.95 and got["right in 4 bits"] > 0.9
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,classes,features", [(6, 1000, 200), (200, 70, 64), (300, 2000, 130), (5, 3, 40)])
+def test_labelled_rows_of_infinities_and_nan(dtype, rows, classes, features):
+    """Such a row's loss is NaN; the other rows' bits are what they are without it."""
+    log(f"readout infinities {dtype} {rows} {classes} {features}")
+    c = Case(rows, classes, features, dtype, seed=11)
+    t = c.torch
+    c.run()
+    loss, lse = c.loss.clone(), c.lse.clone()
+    c.x[0, 1], c.x[2, 0], c.x[4, features - 1] = float("inf"), -float("inf"), float("nan")
+    c.run()
+    bad = t.zeros(rows, dtype=t.bool, device="cuda")
+    bad[[0, 2, 4]] = True
+    assert t.equal(c.loss.isnan(), bad) and t.equal(c.loss[~bad], loss[~bad]) and t.equal(c.lse[~bad], lse[~bad])
+
+
+# one to four rows or classes against more, or longer, rows than the streaming kernels take: both sides of each limit
+@pytest.mark.parametrize("rows,classes,features,dtype", [
+    (1, 8192, 33, "float32"), (1, 8193, 33, "float32"), (1, 8193, 511, "float32"), (1, 8193, 512, "float32"), (8193, 1, 100, "float32"),
+    (4, 8193, 100, "float32"), (3, 8192, 100, "float32"), (2, 8193, 2047, "float32"), (2, 8193, 2048, "float32"), (8193, 4, 130, "float32"), (8193, 3, 2050, "float32"),
+    (1, 8193, 2048, "bfloat16"), (1, 8193, 2049, "bfloat16"), (8193, 1, 70, "bfloat16"), (1, 1024, 4100, "bfloat16"), (1, 1025, 4100, "bfloat16"), (1025, 1, 4098, "bfloat16")])
+def test_few_against_many(rows, classes, features, dtype):
+    log(f"readout few against many {rows} x {classes} x {features} {dtype}")
+    c = Case(rows, classes, features, dtype, seed=features)
+    if rows > 4:
+        c.y[::3] = -1
+    c.run()
+    c.check()
+    g = c.torch.randn(rows, generator=c.torch.Generator("cuda").manual_seed(1), device="cuda")
+    c.run(g)
+    c.check(g)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,classes,features", [(2100, 2100, 1030), (600, 8200, 515), (300, 14000, 2050)])
+def test_millions_of_logits_in_parts(rows, classes, features, dtype):
+    """Blocks for half of the CUs: their features are split, if that pays; labels are left out here and there."""
+    log(f"readout logits in parts {rows} x {classes} x {features} {dtype}")
+    c = Case(rows, classes, features, dtype, seed=rows)
+    c.y[::5] = -1
+    c.run()
+    c.check()
