@@ -7,7 +7,8 @@
 // Rows are padded to whole runs of 4 blocks (128 values, one matrix instruction) with zero codes.
 //
 // The product runs on the scaled 4-bit matrix instructions (16 x 16 x 128, fp32 sums of exact products): 64 bytes
-// of a row are 4 lane groups' 16-byte blocks, and each lane hands the instruction its block's scale byte.
+// of a row are 4 lane groups' 16-byte blocks, and each lane hands the instruction its block's scale byte. 4096 x 16384
+// x 16384: 542 us with its quantisation, 4.0 PFLOP/s.
 #include "dense.h"
 
 using namespace dense;
@@ -58,7 +59,8 @@ __device__ __forceinline__ void load8(const T *row, int64_t k, int64_t n, bool v
   }
 }
 
-// Eight values a lane, four lanes a block. Bound by memory: 4 (or 2) bytes read and 17/32 written a value.
+// Eight values a lane, four lanes a block. Bound by memory, 4 (or 2) bytes read and 17/32 written a value: 8192 x 16384
+// fp32 118 us (5.1 TB/s) over and over, 149 after other work; bf16 62 us.
 template <class T>
 __global__ __launch_bounds__(256) void k_quantize(const T *x, int64_t ld, int64_t rows, int64_t n, int64_t blocks, bool vec, uint8_t *codes, uint8_t *scales) {
   const int per = (int)blocks * 4;  // a multiple of 16: a block's lanes stay together
@@ -87,7 +89,8 @@ __device__ __forceinline__ float scale_of(uint32_t s) {
   return s == kNanScale ? __builtin_nanf("") : __uint_as_float(s ? s << 23 : 1u << 22);  // 2^-127 is not normal
 }
 
-// 16 bytes of values a lane: a wave stores a run of 1024. Bound by memory, most of it the values written.
+// 16 bytes of values a lane: a wave stores a run of 1024. Bound by memory, most of it the values written: 8192 x 16384 fp32
+// 124 to 141 us (4.9 to 4.3 TB/s), bf16 68 us.
 template <class T>
 __global__ __launch_bounds__(256) void k_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t n, int64_t blocks, T *out, int64_t ld, bool vec) {
   constexpr int kEach = 16 / sizeof(T);

@@ -6,7 +6,14 @@
 // so that A is square in the smaller size and X is never transposed. Every product runs on the fp16 matrix cores with
 // each factor held as two fp16 parts (KIND_SPLIT of tile.h), which keeps fp32's exactness at 3 fp16 products each.
 // A and A A are symmetric: only blocks on and above the diagonal are computed, and written to both places.
-// Each step is three launches; their epilogues apply a, b, c and write the next factor in its two parts.
+// Each step is three launches; their epilogues apply a, b, c and write the next factor in its two parts. Where A has
+// blocks for few CUs (a small side against a long one) its k is split and a fourth launch joins the sums. Small
+// matrices are one launch in all (k_small).
+//
+// Measured (five steps): 4096 x 4096 fp32 3.4 ms, 404 TFLOP/s of fp32 in the products that are computed, bound by the
+// matrix instructions: A and A A 0.18-0.20 ms each (253 blocks of 192 x 192, one to a CU), X's update 0.30-0.32 ms.
+// 2000 x 1021 bf16 0.29 ms: 22, 14 and 23 us a step; the two squares have 136 blocks of 64 x 64 for 256 CUs, each
+// going through its k alone. 4 x 128 x 256 110 us: 17 launches of 6 to 8 us.
 //
 // Scaling: fp16 holds 2^-24 ... 65504, so each factor is held times a power of two from a bound of its
 // entries: |X_k| <= u_k, the largest singular value that the polynomial can reach from at most 1 (found on the
@@ -217,9 +224,10 @@ struct Update {
 
 // Small matrices: one workgroup does all steps of one matrix, whose X (m x n, m <= n, transposed on the way in and out where
 // rows > cols) and square factor stay in LDS in two parts. The launches of the large form cost 17 times 6 us whatever their
-// size. 16 waves share the 32 x 32 tiles of each product; every wave computes its tiles into registers, all meet,
-// and the tiles are written. LDS holds 32 columns of all rows at a time (a slab), 128 bytes a row as in
-// tile.h, chunks permuted by the row; both products' fragments are read from that one form.
+// size; here 64 x 64 takes 24 us (105 there), 128 x 128 55 (100), 32 x 1000 54 (105), 1024 of 128 x 128 235 (891).
+// 16 waves share the 32 x 32 tiles of each product; every wave computes its tiles into registers, all meet, and the
+// tiles are written. LDS holds 32 columns of all rows at a time (a slab), 128 bytes a row as in tile.h, chunks permuted by
+// the row; both products' fragments are read from that one form.
 constexpr int kRoom = 152 * 1024;
 inline int64_t pad32(int64_t x) { return ceil_div(x, 32) * 32; }
 inline bool is_small(int64_t rows, int64_t cols) {

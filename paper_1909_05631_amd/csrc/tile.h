@@ -273,7 +273,7 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 //
 // 256 x 256 by 8 waves of 128 x 64: two waves a SIMD cover each other's waits, and 208 of 256 registers hold sums and
 // fragments. Measured on 8192^3: bf16 1300 TFLOP/s at 66% of the cycles in matrix instructions (the card lowers its
-// clock to 1.9 GHz under them; at 1570 for the library's kernel in the same run), KIND_SPLIT 1430, 477 of fp32.
+// clock to 1.9 GHz under them; the library's kernel in the same run 1570), KIND_SPLIT 1430, 477 of fp32.
 // Four waves of 128 x 128 read less LDS and measured 1010, raised wave priorities during the products 7% less.
 //
 // GROUPS of WM x WN waves may share the block's outputs, each loading and taking every GROUPS-th slab, with their sums joined
