@@ -207,7 +207,7 @@ typedef enum {
 } sdnn_dtype;
 
 /* Bytes of workspace for sdnn_readout_loss (gradient = 0) or for both calls (gradient = 1). It grows with
- * n_rows * n_features and n_features * n_classes (fp32 operands are held in two 16-bit parts, unaligned ones are
+ * n_rows * n_features and n_features * n_classes (fp32 operands are held in 16-bit parts, unaligned ones are
  * copied), not with n_rows * n_classes past 2^26 of them. 0 for sizes that the calls refuse: n_rows in [0, 2^24],
  * n_classes in [1, 2^24], n_features in [1, 2^20]. */
 size_t sdnn_readout_workspace_bytes(int64_t n_rows, int64_t n_classes, int64_t n_features, int32_t dtype,
@@ -232,8 +232,9 @@ sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t
  *   dx: n_rows x n_features, dw: n_classes x n_features, of `dtype`, row strides lddx and lddw; overwritten. Either
  *   may be NULL: not computed. Neither may overlap an input.
  * Rows without a label add nothing to dw and have a dx of zeros, whatever x, lse and row_grad hold there. For bf16 G is
- * rounded to bf16 once (as a fraction of the largest row_grad), between two fp32 sums; for fp32 it is held in two
- * fp16 parts. */
+ * rounded to bf16 once (as a fraction of the largest row_grad), between two fp32 sums. For fp32 inputs the logits are
+ * the loss's, and G, w and x are multiplied as they are or as three bf16 parts each (all 24 bits of a value down to 2^-110),
+ * so that values of very different sizes keep what fp32 keeps of them. */
 sdnn_status sdnn_readout_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t dtype,
                               const int64_t *labels, const float *lse, const float *row_grad, int64_t n_rows,
                               int64_t n_classes, int64_t n_features, void *dx, int64_t lddx, void *dw, int64_t lddw,

@@ -21,7 +21,7 @@ constexpr int kXcds = 8;
 constexpr int kCus = 256;  // compute units: what a launch has to fill
 constexpr int64_t kMaxRows = 1 << 24, kMaxClasses = 1 << 24, kMaxFeatures = 1 << 20;
 constexpr int kMaxSplits = 64;
-constexpr int64_t kMaxPitch = 1 << 22;  // bytes from row to row that the tiles' 32-bit offsets reach over 256 rows
+constexpr int64_t kMaxPitch = 6 << 20;  // bytes from row to row: the longest row in three parts; the tiles' 32-bit offsets reach over 256 rows
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 __host__ __device__ inline int64_t ceil_div(int64_t x, int64_t a) { return (x + a - 1) / a; }
@@ -139,6 +139,32 @@ __device__ __forceinline__ void store_split4(char *row, int64_t k, f32x4 v) {
   *(f16x4 *)(row + split_at(k) + kLow) = lo;
 }
 
+// v as high + middle + low in bf16, exactly (while low stays normal); a value past bf16's largest has its high part cut, not
+// rounded to infinity.
+__device__ __forceinline__ void split3(float v, __bf16 &hi, __bf16 &mid, __bf16 &lo) {
+  hi = (__bf16)v;
+  if (!__builtin_isfinite((float)hi) && __builtin_isfinite(v)) hi = (__bf16)__uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  const float r = __builtin_isfinite((float)hi) ? v - (float)hi : 0.0f;
+  mid = (__bf16)r;
+  lo = (__bf16)(r - (float)mid);
+}
+// Four neighbours of a row in the form of KIND_THREE.
+__device__ __forceinline__ void store_three4(char *row, int64_t k, f32x4 v) {
+  bf16x4 hi, mid, lo;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __bf16 h, m, l;
+    split3(v[i], h, m, l);
+    hi[i] = h;
+    mid[i] = m;
+    lo[i] = l;
+  }
+  char *to = row + (k >> 6) * tile::kGroup3 + (k & 63) * 2;
+  *(bf16x4 *)to = hi;
+  *(bf16x4 *)(to + tile::kSlab) = mid;
+  *(bf16x4 *)(to + 2 * tile::kSlab) = lo;
+}
+
 // The power of two that takes a largest magnitude to [2^14, 2^15), as an exponent: high parts stay finite in
 // fp16 and values down to 2^-17 of the largest keep all their bits.
 __device__ __forceinline__ int split_exponent(float top) {
@@ -206,13 +232,17 @@ struct Matrix {
   const char *data;
   int64_t pitch;   // bytes
   int64_t rows;    // along: rows; across: rows of k
-  int64_t extent;  // bytes in a row: of k (along), of columns (across)
+  int64_t extent;  // bytes in a row: of k (along), of columns (across); KIND_THREE: of one part
   int64_t batch;   // bytes from one matrix of a batch (blockIdx.y) to the next
   const uint8_t *scales = nullptr;  // KIND_MX: pitch / 16 bytes a row
   template <int KIND, int SIZE, bool ACROSS>
   __device__ __forceinline__ tile::Operand at(int block) const {
     const int64_t first = (int64_t)block * SIZE;
     const char *here = data + blockIdx.y * batch;
+    if (ACROSS && KIND == tile::KIND_THREE) {
+      const int64_t group = first / 64;
+      return {here + group * tile::kGroup3, (int)pitch, (int)rows, (int)(extent - group * tile::kSlab), nullptr, (int)(first % 64) * 2};
+    }
     if (ACROSS) {
       const int64_t skip = first * tile::Geometry<KIND>::kBytes;
       return {here + skip, (int)pitch, (int)rows, (int)(extent - skip)};
@@ -242,7 +272,7 @@ sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols,
                    int batch) {
   using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES, GROUPS>;
   Blocks blocks;
-  blocks.slabs = (int)ceil_div(k, tile::Geometry<KIND>::kPerSlab);
+  blocks.slabs = (int)ceil_div(k, tile::Geometry<KIND>::kPerSlab) * tile::Geometry<KIND>::kSlabs;
   blocks.per = (int)ceil_div(blocks.slabs, splits);
   blocks.splits = splits;
   const int64_t r = ceil_div(rows, BM), c = ceil_div(cols, BN);
@@ -275,7 +305,7 @@ enum Form { kAnyForm, kAlong };  // kAlong: both operands are (rows of 192 colum
 // The shape and split that a model of the launch finds fastest: rounds of resident blocks times slabs (1.4 as long for
 // three products a slab, 2.3 in fp32), and for a split sum its slabs' traffic (at 4 TB/s) and one launch more.
 inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_splits, Form form = kAnyForm, int64_t batch = 1, bool symmetric = false) {
-  const int64_t slabs = ceil_div(k, kind == tile::KIND_BF16 ? 64 : kind == tile::KIND_MX ? 256 : 32);
+  const int64_t slabs = kind == tile::KIND_THREE ? 6 * ceil_div(k, 64) : ceil_div(k, kind == tile::KIND_BF16 ? 64 : kind == tile::KIND_MX ? 256 : 32);
   const double longer = kind == tile::KIND_SPLIT ? 1.4 : kind == tile::KIND_F32 ? 2.3 : 1.0;
   Plan best = {kStream, 1, 1e30};
   for (int s = 0; s < kShapes; ++s) {

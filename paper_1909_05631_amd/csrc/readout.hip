@@ -12,7 +12,7 @@
 // n_rows x n_classes is written. Where there are few logits (at most 2^24) and blocks for only a part of the
 // CUs, the features are split instead, and a workgroup a row joins the slabs and takes the softmax.
 // Gradient: piece by piece, the logits are computed again (2 of 8 T V D operations, against a logit matrix in memory),
-// the epilogue writes the piece's G in 16 bits (bf16; fp32 inputs: two fp16 parts), and two products read it, dx +=
+// the epilogue writes the piece's G (bf16; fp32 inputs: three bf16 parts), and two products read it, dx +=
 // G w (over the piece's classes) and dw = G^T x (over the rows), both through the transposing LDS reads, so neither
 // w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G: it stays in the Infinity Cache
 // between the products.
@@ -26,8 +26,11 @@
 //     for their largest values.
 //   2000 x 1024 x 10, fp32: 45 us, eight launches of 4 to 9 us.
 //
-// fp32 inputs go as two fp16 parts (tile.h), or, where rows or classes are at most 128, to the fp32 matrix instructions
-// as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts). One to four rows or classes
+// fp32 inputs go to the logits as two fp16 parts under a power of two per row of x and of w, which the logits' own
+// rows and columns take back. The gradient's products cannot: their sums run over the rows of x or the classes, whose
+// sizes may lie any number of powers of two apart, and one row of x or of w far larger than the others would leave
+// these no bits. So G, w and x go there as three bf16 parts, which need no common scale. Where rows or classes are at
+// most 128, all go to the fp32 matrix instructions as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts). One to four rows or classes
 // (few.h) mostly have no use for tiles: one kernel with fp32 arithmetic streams the other matrix past them, once.
 #include "dense.h"
 #include "few.h"
@@ -38,6 +41,7 @@ using namespace dense;
 using tile::KIND_BF16;
 using tile::KIND_F32;
 using tile::KIND_SPLIT;
+using tile::KIND_THREE;
 
 namespace {
 
@@ -46,8 +50,6 @@ constexpr int64_t kPieceClasses = 1 << 19;
 constexpr int64_t kPlain = 128;            // fp32 rows or classes for the plain fp32 products: see Sizes::kind
 constexpr int64_t kSplitLogits = 1 << 24;  // logits whose features may be split: past that there is a 256 x 256 block for every CU
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kTopBlocks = 512;
-constexpr int kGradExponent = 15;  // fp16 parts of exp(l - lse) - [v = y] hold it times 2^15
 
 // exp, by the hardware's exponential of base 2 (one rounding of the argument, which is at most 0 in the sums: the
 // terms that matter have arguments near 0).
@@ -59,9 +61,8 @@ __device__ __forceinline__ bool counted(const int64_t *labels, int64_t t, int64_
 
 // What the kernels of one call hand on in device memory.
 struct Scalars {
-  float top[3][kTopBlocks];  // largest finite magnitudes of x (counted rows), of w, of x times its rows' weights, by workgroup
-  float mean;                // 1 / (number of counted rows), at most 1
-  float heaviest;            // the largest magnitude of the counted rows' weights (1 if that is 0)
+  float mean;      // 1 / (number of counted rows), at most 1
+  float heaviest;  // the largest magnitude of the counted rows' weights (1 if that is 0)
 };
 
 __device__ __forceinline__ float finite_magnitude(float v) {
@@ -101,79 +102,47 @@ __device__ __forceinline__ void count_rows(const int64_t *labels, int64_t rows, 
 }
 __global__ __launch_bounds__(256) void k_count(const int64_t *labels, int64_t rows, int64_t classes, Scalars *out) { count_rows(labels, rows, classes, nullptr, out); }
 
-__device__ __forceinline__ float top4(f32x4 v, float w) {
-  return fmaxf(fmaxf(finite_magnitude(v[0] * w), finite_magnitude(v[1] * w)), fmaxf(finite_magnitude(v[2] * w), finite_magnitude(v[3] * w)));
+__device__ __forceinline__ float top4(f32x4 v) {
+  return fmaxf(fmaxf(finite_magnitude(v[0]), finite_magnitude(v[1])), fmaxf(finite_magnitude(v[2]), finite_magnitude(v[3])));
 }
 
-// A matrix's rows for the kernels that go over x and w in one launch. Rows without a label (labels != nullptr) are
-// skipped or become zeros; the others are multiplied by their weights, if there are any.
+// An fp32 matrix's rows for the kernel that goes over x and w in one launch. Rows without a label (labels != nullptr)
+// become zeros.
 struct Rows {
   const float *data;
   int64_t ld, rows;
   const int64_t *labels;
-  const float *weights;
-  float *top;      // the largest finite magnitudes, one per workgroup
-  int *exponents;  // of each row (nullptr: one of the whole matrix, from top)
-  char *out;       // the split form
+  int *exponents;  // of each row in two parts
+  char *out;       // in two parts, 32 * groups values a row
+  char *three;     // in three parts, whole groups of 64 (nullptr: not wanted)
   bool vec;        // rows are 16-byte aligned
 };
 
-// Largest finite magnitudes of x, w and the weighted x (kTopBlocks workgroups each), and the number of counted rows (the
-// first workgroup). Bound by memory.
-__global__ __launch_bounds__(256) void k_survey(Rows x, Rows w, Rows xg, int64_t cols, const int64_t *labels, int64_t classes, Scalars *scalars) {
+// fp32 rows in their parts, zeros past `cols`: `first` workgroups on x, the rest on w. With `scalars`, the last
+// workgroup counts the rows that have a label.
+__global__ __launch_bounds__(256) void k_split_rows(Rows x, Rows w, int first, int64_t cols, int64_t groups, const int64_t *labels, int64_t classes, Scalars *scalars) {
   __shared__ float part[4];
-  if (blockIdx.x == 0) return count_rows(labels, x.rows, classes, nullptr, scalars);
-  const int which = (blockIdx.x - 1) / kTopBlocks, block = (blockIdx.x - 1) % kTopBlocks;
-  const Rows &m = which == 0 ? x : which == 1 ? w : xg;
-  float top = 0.0f;
-  for (int64_t r = block; r < m.rows; r += kTopBlocks) {
-    if (m.labels && !counted(m.labels, r, classes)) continue;
-    const float weight = m.weights ? m.weights[r] : 1.0f;
-#pragma unroll 2
-    for (int64_t c = threadIdx.x * 4; c < cols; c += 1024) top = fmaxf(top, top4(few::load4(m.data + r * m.ld, (int)c, (int)cols, m.vec), weight));
-  }
-  top = max_of_workgroup(top, part);
-  if (threadIdx.x == 0) m.top[block] = top;
-}
-
-// What k_survey found, by one wave (all of its lanes get it).
-__device__ __forceinline__ float top_of(const float *top) {
-  float m = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kTopBlocks / 64; ++i) m = fmaxf(m, top[i * 64 + (threadIdx.x & 63)]);
-  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  return m;
-}
-
-// fp32 rows in the split form, 32 * groups values each, zeros past `cols`: `first` workgroups on x, `second` on w, the
-// rest on the weighted x.
-__global__ __launch_bounds__(256) void k_split_rows(Rows x, Rows w, Rows xg, int first, int second, int64_t cols, int64_t groups, int64_t classes) {
-  __shared__ float part[4];
-  const int b = blockIdx.x, which = b < first ? 0 : b < first + second ? 1 : 2;
-  const Rows &m = which == 0 ? x : which == 1 ? w : xg;
-  const int block = which == 0 ? b : which == 1 ? b - first : b - first - second;
-  const int step = which == 0 ? first : which == 1 ? second : (int)gridDim.x - first - second;
-  const int whole = m.exponents ? 0 : split_exponent(top_of(m.top));
-  for (int64_t r = block; r < m.rows; r += step) {
+  const int work = (int)gridDim.x - (scalars ? 1 : 0), b = blockIdx.x;
+  if (b == work) return count_rows(labels, x.rows, classes, nullptr, scalars);
+  const Rows &m = b < first ? x : w;
+  const int64_t pitch3 = ceil_div(cols, 64) * tile::kGroup3, wide = m.three ? pitch3 / 6 : groups * 32;
+  for (int64_t r = b < first ? b : b - first; r < m.rows; r += b < first ? first : work - first) {
     const float *row = m.data + r * m.ld;
     const bool live = !m.labels || counted(m.labels, r, classes);
-    const float weight = m.weights && live ? m.weights[r] : 1.0f;
-    int e = whole;
-    if (m.exponents) {
-      float top = 0.0f;
-      if (live)
-        for (int64_t k = threadIdx.x * 4; k < cols; k += 1024) top = fmaxf(top, top4(few::load4(row, (int)k, (int)cols, m.vec), weight));
-      e = split_exponent(max_of_workgroup(top, part));
-      if (threadIdx.x == 0) m.exponents[r] = e;
-    }
+    float top = 0.0f;
+    if (live)
+      for (int64_t k = threadIdx.x * 4; k < cols; k += 1024) top = fmaxf(top, top4(few::load4(row, (int)k, (int)cols, m.vec)));
+    const int e = split_exponent(max_of_workgroup(top, part));
+    if (threadIdx.x == 0) m.exponents[r] = e;
     char *to = m.out + r * groups * 128;
 #pragma unroll 2
-    for (int64_t k = threadIdx.x * 4; k < groups * 32; k += 1024) {
+    for (int64_t k = threadIdx.x * 4; k < wide; k += 1024) {
       f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
       if (live) v = few::load4(row, (int)k, (int)cols, m.vec);
+      if (m.three) store_three4(m.three + r * pitch3, k, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i] * weight, e);
-      store_split4(to, k, v);
+      for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], e);
+      if (k < groups * 32) store_split4(to, k, v);
     }
   }
 }
@@ -205,16 +174,10 @@ __global__ __launch_bounds__(256) void k_copy_rows(const T *x, int64_t ld, int64
   }
 }
 
-// What turns a block's sums into logits: the operands' powers of two.
+// What turns a block's sums into logits: the exponents of the operands' rows and columns (split).
 struct LogitScale {
-  const int *row, *col;            // exponents by row and column (split, loss)
-  const float *top_x, *top_w;      // or of the whole matrices (split, gradient)
+  const int *row, *col;
 };
-template <int KIND>
-__device__ __forceinline__ int whole_exponent(const LogitScale &s) {
-  if (KIND != KIND_SPLIT || s.row) return 0;
-  return split_exponent(top_of(s.top_x)) + split_exponent(top_of(s.top_w));
-}
 
 // Loss: per row and the wave's columns, the largest logit and the sum of exponentials against it.
 template <int KIND>
@@ -338,48 +301,58 @@ sdnn_status join_parts(const float2 *parts, int64_t count, const float *picked, 
   return launched("loss");
 }
 
-// Gradient: the piece's exp(l - lse) - [v = y], zeros in rows without a label. Split: times 2^15, weights are left to the
-// products. bf16: times the row's weight over the heaviest, so that equal weights (a mean's) are a factor of one and the
-// label's -1 is exact; a common factor that were rounded here would be off by as much in every row's gradient.
+// Gradient: the piece's exp(l - lse) - [v = y], zeros in rows without a label, times the row's weight. Three parts of
+// fp32: as that is. Else: over the heaviest weight, so that equal weights (a mean's) are a factor of one and, in bf16,
+// the label's -1 is exact; a common factor that were rounded here would be off by as much in every row's gradient.
 template <int KIND>
 struct WriteGrad {
-  LogitScale scale;
+  LogitScale scale;  // the piece's columns
   const int64_t *labels;
   const float *lse, *weights;
   const Scalars *scalars;
   int64_t rows, all, first, classes;  // all classes; the piece's first and number
   char *g;
   int64_t pitch;  // bytes
+  __device__ __forceinline__ float heaviest() const { return KIND != KIND_SPLIT && weights ? scalars->heaviest : 1.0f; }
+  // What a row's values have in common.
+  struct Row {
+    bool live;
+    int64_t y;
+    float z, w;
+    int e;
+  };
+  __device__ __forceinline__ Row row(int64_t t, bool in, float heaviest) const {
+    const bool live = in && counted(labels, t, all);
+    return {live, in ? labels[t] - first : -1, live ? lse[t] : 0.0f, weights && live ? weights[t] / heaviest : 1.0f, KIND == KIND_SPLIT && in ? scale.row[t] : 0};
+  }
   // Four neighbours of a row, from class v of the piece on.
-  __device__ __forceinline__ f32x4 gradient(f32x4 l, int64_t v, int64_t y, bool live, float z, float w, int e) const {
+  __device__ __forceinline__ f32x4 gradient(f32x4 l, int64_t v, const Row &r) const {
     f32x4 o;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const float s = KIND == KIND_SPLIT ? ldexpf(l[c], -e) : l[c];
-      const float p = exp_of(s - z) - (v + c == y ? 1.0f : 0.0f);
-      o[c] = live && v + c < classes ? w * p : 0.0f;
+      const bool in = v + c < classes;
+      const float s = KIND == KIND_SPLIT ? ldexpf(l[c], -r.e - (in ? scale.col[v + c] : 0)) : l[c];
+      const float p = exp_of(s - r.z) - (v + c == r.y ? 1.0f : 0.0f);
+      o[c] = r.live && in ? r.w * p : 0.0f;
     }
     return o;
   }
   template <class B>
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int lane = threadIdx.x & 63, i16 = lane & 15, j4 = lane >> 4;
-    const int e = whole_exponent<KIND>(scale);
-    const float heaviest = KIND != KIND_SPLIT && weights ? scalars->heaviest : 1.0f;
+    const float heavy = heaviest();
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t t = row0 + 16 * i + i16;
-      const bool in = t < rows, live = in && counted(labels, t, all);
-      const int64_t y = in ? labels[t] - first : -1;
-      const float z = live ? lse[t] : 0.0f;
-      const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : weights && live ? weights[t] / heaviest : 1.0f;
-      const auto value = [&](int j) { return gradient(block.acc[i][j], col0 + 16 * j + 4 * j4, y, live, z, w, e); };
+      const bool in = t < rows;
+      const Row r = row(t, in, heavy);
+      const auto value = [&](int j) { return gradient(block.acc[i][j], col0 + 16 * j + 4 * j4, r); };
       if constexpr (KIND == KIND_SPLIT) {
 #pragma unroll
         for (int j = 0; j < B::kTN; ++j) {
           const int64_t v = col0 + 16 * j + 4 * j4;
           const f32x4 o = value(j);
-          if (in && split_at(v) < pitch) store_split4(g + t * pitch, v, o);
+          if (in && v < pitch / 6) store_three4(g + t * pitch, v, o);
         }
       } else {
         using G = std::conditional_t<KIND == KIND_F32, float, __bf16>;
@@ -392,23 +365,18 @@ struct WriteGrad {
 // The same from logits whose k was split.
 template <int KIND>
 __global__ __launch_bounds__(256) void k_grad_slabs(const float *slabs, int splits, int64_t ld, WriteGrad<KIND> to) {
-  const int e = whole_exponent<KIND>(to.scale);
-  const float heaviest = KIND != KIND_SPLIT && to.weights ? to.scalars->heaviest : 1.0f;
   const int64_t t = blockIdx.y;
-  const bool live = counted(to.labels, t, to.all);
-  const int64_t y = to.labels[t] - to.first;
-  const float z = live ? to.lse[t] : 0.0f;
-  const float w = KIND == KIND_SPLIT ? (float)(1 << kGradExponent) : to.weights && live ? to.weights[t] / heaviest : 1.0f;
+  const typename WriteGrad<KIND>::Row r = to.row(t, true, to.heaviest());
   char *row = to.g + t * to.pitch;
-  const int64_t wide = KIND == KIND_BF16 ? to.pitch / 2 : to.pitch / 4;
+  const int64_t wide = to.pitch / (KIND == KIND_BF16 ? 2 : KIND == KIND_SPLIT ? 6 : 4);
   for (int64_t v = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; v < wide; v += (int64_t)gridDim.x * 1024) {
     f32x4 l = {0.0f, 0.0f, 0.0f, 0.0f};
     if (v < ld)
 #pragma unroll 4
       for (int s = 0; s < splits; ++s) l += *(const f32x4 *)(slabs + (s * to.rows + t) * ld + v);
-    const f32x4 o = to.gradient(l, v, y, live, z, w, e);
+    const f32x4 o = to.gradient(l, v, r);
     if constexpr (KIND == KIND_SPLIT)
-      store_split4(row, v, o);
+      store_three4(row, v, o);
     else if constexpr (KIND == KIND_F32)
       store4((float *)row + v, o, 4, true);
     else
@@ -416,47 +384,27 @@ __global__ __launch_bounds__(256) void k_grad_slabs(const float *slabs, int spli
   }
 }
 
-// What a product's sums are multiplied by: the mean and the split operands' powers of two (found once a wave), and
-// the row's weight. A sum of zero stays zero whatever the weight: rows without a label.
-struct OutScale {
-  const float *rows;
-  const float *mean;  // or another common factor
-  const float *top;  // of the operand that was split (nullptr: none)
-  struct Found {
-    float mean;
-    int e;
-  };
-  __device__ __forceinline__ Found find() const { return {mean ? *mean : 1.0f, top ? -kGradExponent - split_exponent(top_of(top)) : 0}; }
-  __device__ __forceinline__ float weight(int64_t row) const { return rows ? rows[row] : 1.0f; }
-  __device__ __forceinline__ f32x4 apply(Found f, float weight, f32x4 v) const {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = v[k] == 0.0f ? 0.0f : ldexpf(v[k], f.e) * f.mean * weight;
-    return v;
-  }
-};
-
 template <class T>
 struct Store {
   T *out;
   int64_t ld, rows, cols;
   bool vec;
-  OutScale scale;
+  const float *factor = nullptr;  // what the sums are multiplied by: the mean's, or the heaviest weight
   const float *before = nullptr;  // sums of the pieces before
   int64_t ld_before = 0;
   template <class B>
   __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
     const int i16 = threadIdx.x & 15;
-    const OutScale::Found found = scale.find();
+    const float by = factor ? *factor : 1.0f;
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t r = row0 + 16 * i + i16;
       const bool in = r < rows;
-      const float w = in ? scale.weight(r) : 0.0f;
       store_row<T, B::kTN>(out + r * ld, col0, cols, vec, in, [&](int j) {
         f32x4 v = block.acc[i][j];
         const int64_t c = col0 + 16 * j + 4 * ((threadIdx.x & 63) >> 4);
         if (before && in && c < ld_before) v += *(const f32x4 *)(before + r * ld_before + c);
-        return scale.apply(found, w, v);
+        return v * by;
       });
     }
   }
@@ -468,7 +416,7 @@ __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int split
   constexpr int kItems = 256 / GROUPS;
   __shared__ f32x4 shared[GROUPS][kItems];
   const int64_t per = ld_slab / 4, total = to.rows * per;
-  const OutScale::Found found = to.scale.find();
+  const float by = to.factor ? *to.factor : 1.0f;
   const int group = threadIdx.x / kItems, item = threadIdx.x % kItems;
   for (int64_t i0 = (int64_t)blockIdx.x * kItems; i0 < total; i0 += (int64_t)gridDim.x * kItems) {
     const int64_t i = i0 + item, r = i / per, c = (i - r * per) * 4;
@@ -483,7 +431,7 @@ __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int split
       if (group == 0)
         for (int g = 1; g < GROUPS; ++g) v += shared[g][item];
     }
-    if (group == 0 && i < total && c < to.cols) store4(to.out + r * to.ld + c, to.scale.apply(found, to.scale.weight(r), v), (int)(to.cols - c < 4 ? to.cols - c : 4), to.vec);
+    if (group == 0 && i < total && c < to.cols) store4(to.out + r * to.ld + c, v * by, (int)(to.cols - c < 4 ? to.cols - c : 4), to.vec);
   }
 }
 
@@ -511,6 +459,8 @@ struct Sizes {
   int64_t per_slab() const { return dtype == SDNN_BF16 ? 64 : 32; }
   int64_t groups() const { return ceil_div(features, 32); }
   int64_t pitch_values() const { return ceil_div(features, 8) * 8; }  // rows that had to be copied
+  size_t three(int64_t n) const { return (size_t)(n * three_pitch()); }
+  int64_t three_pitch() const { return ceil_div(features, 64) * tile::kGroup3; }
   size_t packed(int64_t n) const { return kind() == KIND_SPLIT ? (size_t)(n * groups() * 128) : (size_t)(n * pitch_values() * dtype_bytes(dtype)); }
   // fp32 operands go to the fp32 matrix instructions as they are up to kPlain rows or classes: the other matrix is
   // then the larger one, and writing it in two parts costs more than products that are three times as fast save
@@ -521,15 +471,16 @@ struct Sizes {
     const int64_t p = std::max<int64_t>(256, std::min(kPieceClasses, kPieceValues / std::max<int64_t>(rows, 1)) / 256 * 256);
     return std::min(p, classes);
   }
-  int64_t g_pitch() const { return ceil_div(piece(), per_slab()) * 128; }
+  int64_t g_pitch() const { return kind() == KIND_SPLIT ? ceil_div(piece(), 64) * tile::kGroup3 : ceil_div(piece(), per_slab()) * 128; }
   // The logits' k may be split where they are few: their slabs are joined by a row's workgroup (5 x 5000 x 1000 fp32: loss
   // 21 us, 102 unsplit; gradient 42 and 127; 2100 x 2100 x 8192 bf16: 83 and 283, unsplit 125 and 331;
   // 500 x 12000 x 4096 bf16: 72 us either way).
   int logit_splits(int64_t n) const { return rows * n <= kSplitLogits && rows <= 65535 ? kMaxSplits : 1; }
   Plan logits(int64_t n) const { return plan(kind(), rows, n, features, logit_splits(n), kAlong); }
   size_t logit_slabs(const Plan &p, int64_t n) const { return p.splits > 1 ? (size_t)(p.splits * rows * (ceil_div(n, 4) * 4)) : 0; }
-  Plan dx() const { return plan(kind(), rows, features, piece(), kMaxSplits); }
-  Plan dw(int64_t n) const { return plan(kind(), n, features, rows, kMaxSplits); }
+  int product_kind() const { return kind() == KIND_SPLIT ? KIND_THREE : kind(); }
+  Plan dx() const { return plan(product_kind(), rows, features, piece(), kMaxSplits); }
+  Plan dw(int64_t n) const { return plan(product_kind(), n, features, rows, kMaxSplits); }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
   few::Fit fit(bool rows_held) const { return rows_held ? few::fit_of(rows, classes, features, dtype) : few::fit_of(classes, rows, features, dtype); }
   // Few rows are held rather than few classes.
@@ -566,7 +517,8 @@ struct LossSpace {
 
 struct GradSpace {
   Plan logits[2], dx_plan, dw_plan[2];  // of a whole piece and of the last one
-  char *x, *w, *xg, *g;
+  char *x, *w, *x3, *w3, *g;
+  int *ex, *ew;
   Scalars *scalars;
   float *dx, *dw, *few, *slabs;
   GradSpace(Carver &c, const Sizes &s) {
@@ -578,7 +530,11 @@ struct GradSpace {
     }
     x = c.take<char>(s.packed(s.rows));
     w = c.take<char>(s.packed(s.classes));
-    xg = c.take<char>(s.kind() == KIND_SPLIT ? s.packed(s.rows) : 0);
+    const bool split = s.kind() == KIND_SPLIT;
+    x3 = c.take<char>(split ? s.three(s.rows) : 0);
+    w3 = c.take<char>(split ? s.three(s.classes) : 0);
+    ex = c.take<int>(split ? s.rows : 0);
+    ew = c.take<int>(split ? s.classes : 0);
     g = c.take<char>((size_t)(s.rows * s.g_pitch()));
     const int64_t piece = s.piece(), rest = s.classes % piece;
     dx_plan = s.dx();
@@ -613,10 +569,12 @@ Matrix plain_rows(const T *data, int64_t ld, int64_t rows, const Sizes &s, const
 
 Matrix split_matrix(const Rows &r, const Sizes &s) { return {r.out, s.groups() * 128, r.rows, s.groups() * 128, 0}; }
 
-// x, w and, with xg.rows, the weighted x in the split form.
-void split_rows(const Rows &x, const Rows &w, const Rows &xg, const Sizes &s, hipStream_t stream) {
-  const unsigned a = row_grid(x.rows), b = row_grid(w.rows), c = xg.rows ? row_grid(xg.rows) : 0;
-  hipLaunchKernelGGL(k_split_rows, dim3(a + b + c), dim3(256), 0, stream, x, w, xg, (int)a, (int)b, s.features, s.groups(), s.classes);
+Matrix three_matrix(const Rows &r, const Sizes &s) { return {r.three, s.three_pitch(), r.rows, ceil_div(s.features, 8) * 16, 0}; }
+
+// x and w in their parts; with `scalars` the rows that have a label are counted too.
+void split_rows(const Rows &x, const Rows &w, const Sizes &s, const int64_t *labels, Scalars *scalars, hipStream_t stream) {
+  const unsigned a = row_grid(x.rows), b = row_grid(w.rows);
+  hipLaunchKernelGGL(k_split_rows, dim3(a + b + (scalars ? 1 : 0)), dim3(256), 0, stream, x, w, (int)a, s.features, s.groups(), labels, s.classes, scalars);
 }
 
 template <class T>
@@ -664,14 +622,14 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     a = plain_rows(x, ldx, s.rows, s, nullptr, nullptr, nullptr, sp.x, stream);
     b = plain_rows(w, ldw, s.classes, s, nullptr, nullptr, nullptr, sp.w, stream);
   } else {
-    const Rows rx{x, ldx, s.rows, nullptr, nullptr, nullptr, sp.ex, sp.x, aligned16(x, ldx, 4)};
-    const Rows rw{w, ldw, s.classes, nullptr, nullptr, nullptr, sp.ew, sp.w, aligned16(w, ldw, 4)};
-    split_rows(rx, rw, Rows{}, s, stream);
+    const Rows rx{x, ldx, s.rows, nullptr, sp.ex, sp.x, nullptr, aligned16(x, ldx, 4)};
+    const Rows rw{w, ldw, s.classes, nullptr, sp.ew, sp.w, nullptr, aligned16(w, ldw, 4)};
+    split_rows(rx, rw, s, labels, nullptr, stream);
     a = split_matrix(rx, s);
     b = split_matrix(rw, s);
   }
   if ((st = launched("rows")) != SDNN_OK) return st;
-  const LogitScale scale{sp.ex, sp.ew, nullptr, nullptr};
+  const LogitScale scale{sp.ex, sp.ew};
   if (sp.loss.splits > 1) {
     const int64_t ld = ceil_div(s.classes, 4) * 4;
     st = run_shape<KIND, false, false>(sp.loss, a, b, s.rows, s.classes, s.features, Accumulate{sp.slabs, ld, s.rows, s.classes, false}, stream, "loss");
@@ -728,46 +686,37 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     if (!held && !weights) hipLaunchKernelGGL(k_count, dim3(1), dim3(256), 0, stream, labels, s.rows, s.classes, sp.scalars);
     st = held ? few::launch<true, true>(s.few(), p, stream, "gradient") : few::launch<false, true>(s.few(), p, stream, "gradient");
     if (st != SDNN_OK || !d_held) return st;
-    const Store<T> to{d_held, ld_d_held, p.held_rows, s.features, vector_rows(d_held, ld_d_held), {nullptr, nullptr, nullptr}};
+    const Store<T> to{d_held, ld_d_held, p.held_rows, s.features, vector_rows(d_held, ld_d_held)};
     return sum_slabs(sp.few, (int)few::grid_of(s.few(), p.stream_rows, true), s.ld_slab(), to, stream, "gradient");
   }
-  Matrix a, b, ag;  // ag: dw's other operand: the rows, in fp32 times their weights
-  float *top_x = nullptr, *top_w = nullptr, *top_g = nullptr;
+  constexpr int kProduct = KIND == KIND_SPLIT ? KIND_THREE : KIND;
+  Matrix a, b, ag, bg;  // ag, bg: the rows of x and w as dw's and dx's products take them
   if constexpr (KIND != KIND_SPLIT) {
     ag = a = plain_rows(x, ldx, s.rows, s, labels, weights, sp.scalars, sp.x, stream);
-    b = plain_rows(w, ldw, s.classes, s, nullptr, nullptr, nullptr, sp.w, stream);
+    bg = b = plain_rows(w, ldw, s.classes, s, nullptr, nullptr, nullptr, sp.w, stream);
   } else {
-    const bool weighted = weights && dw;
-    top_x = sp.scalars->top[0];
-    top_w = sp.scalars->top[1];
-    top_g = weighted ? sp.scalars->top[2] : top_x;
-    const Rows rx{x, ldx, s.rows, labels, nullptr, top_x, nullptr, sp.x, aligned16(x, ldx, 4)};
-    const Rows rw{w, ldw, s.classes, nullptr, nullptr, top_w, nullptr, sp.w, aligned16(w, ldw, 4)};
-    Rows rg = rx;
-    rg.rows = weighted ? s.rows : 0;
-    rg.weights = weights;
-    rg.top = top_g;
-    rg.out = sp.xg;
-    hipLaunchKernelGGL(k_survey, dim3(1 + kTopBlocks * (weighted ? 3 : 2)), dim3(256), 0, stream, rx, rw, rg, s.features, labels, s.classes, sp.scalars);
-    split_rows(rx, rw, rg, s, stream);
+    const Rows rx{x, ldx, s.rows, labels, sp.ex, sp.x, dw ? sp.x3 : nullptr, aligned16(x, ldx, 4)};
+    const Rows rw{w, ldw, s.classes, nullptr, sp.ew, sp.w, dx ? sp.w3 : nullptr, aligned16(w, ldw, 4)};
+    split_rows(rx, rw, s, labels, sp.scalars, stream);
     a = split_matrix(rx, s);
     b = split_matrix(rw, s);
-    ag = weighted ? split_matrix(rg, s) : a;
+    ag = three_matrix(rx, s);
+    bg = three_matrix(rw, s);
   }
   st = launched("gradient");
-  // what the products are multiplied by in the end: the mean's factor, or the weights
-  const float *mean = !weights ? &sp.scalars->mean : KIND != KIND_SPLIT ? &sp.scalars->heaviest : nullptr;
-  const float *row_weights = KIND == KIND_SPLIT ? weights : nullptr;
+  // what the products are multiplied by in the end: the mean's factor, or the weights'
+  const float *factor = !weights ? &sp.scalars->mean : KIND != KIND_SPLIT ? &sp.scalars->heaviest : nullptr;
   const Plan &px = sp.dx_plan;
   const int64_t piece = s.piece();
   const bool through_x = px.splits > 1 || piece < s.classes;
   for (int64_t v0 = 0; v0 < s.classes && st == SDNN_OK; v0 += piece) {
     const int64_t n = std::min(piece, s.classes - v0);
     const bool last = v0 + n == s.classes;
-    Matrix wp = b;
+    Matrix wp = b, wg = bg;  // the piece's classes
     wp.data += v0 * b.pitch;
-    wp.rows = n;
-    const WriteGrad<KIND> e{{nullptr, nullptr, top_x, top_w}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
+    wg.data += v0 * bg.pitch;
+    wp.rows = wg.rows = n;
+    const WriteGrad<KIND> e{{sp.ex, sp.ew + v0}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
     const Plan &pl = sp.logits[n < piece];
     if (pl.splits > 1) {
       const int64_t ld = ceil_div(n, 4) * 4;
@@ -779,17 +728,17 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
       st = run_shape<KIND, false, false>(pl, a, wp, s.rows, n, s.features, e, stream, "gradient");
     }
     if (st != SDNN_OK) return st;
-    const int64_t wide = KIND == KIND_SPLIT ? ceil_div(n, 32) * 128 : ceil_div(n * (int64_t)sizeof(T), 16) * 16;  // bytes of a row of G
+    const int64_t wide = ceil_div(n * (int64_t)(kProduct == KIND_THREE ? 2 : sizeof(T)), 16) * 16;  // bytes of a row of G (of one part)
     if (dx) {
-      const Store<T> to{dx, lddx, s.rows, s.features, vector_rows(dx, lddx), {row_weights, mean, top_w}, v0 > 0 && px.splits == 1 ? sp.dx : nullptr, s.ld_slab()};
+      const Store<T> to{dx, lddx, s.rows, s.features, vector_rows(dx, lddx), factor, v0 > 0 && px.splits == 1 ? sp.dx : nullptr, s.ld_slab()};
       const bool direct = !through_x || (last && px.splits == 1);
-      st = product<KIND, false>(px, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, wp, n, sp.dx, s.ld_slab(), !direct, v0 > 0, last, to, stream, "gradient of the rows");
+      st = product<kProduct, false>(px, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, wg, n, sp.dx, s.ld_slab(), !direct, v0 > 0, last, to, stream, "gradient of the rows");
       if (st != SDNN_OK) return st;
     }
     if (dw) {
       const Plan &pw = sp.dw_plan[n < piece];
-      const Store<T> to{dw + v0 * lddw, lddw, n, s.features, vector_rows(dw + v0 * lddw, lddw), {nullptr, mean, top_g}};
-      st = product<KIND, true>(pw, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, ag, s.rows, sp.dw, s.ld_slab(), pw.splits > 1, false, true, to, stream, "gradient of the weights");
+      const Store<T> to{dw + v0 * lddw, lddw, n, s.features, vector_rows(dw + v0 * lddw, lddw), factor};
+      st = product<kProduct, true>(pw, Matrix{sp.g, s.g_pitch(), s.rows, wide, 0}, ag, s.rows, sp.dw, s.ld_slab(), pw.splits > 1, false, true, to, stream, "gradient of the weights");
     }
   }
   return st;

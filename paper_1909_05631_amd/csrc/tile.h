@@ -1,7 +1,7 @@
 // Matrix-core tile product shared by the readout's kernels: acc[m][n] = sum_k A[m][k] B[n][k] for a block of
 // BM x BN outputs.
 //
-// Three kinds of operands share one geometry, a slab of 128 bytes of every row of A and B at a time:
+// Five kinds of operands share one geometry, a slab of 128 bytes of every row of A and B at a time:
 //   KIND_BF16   64 bf16 values a slab.
 //   KIND_SPLIT  32 fp32 values a slab, each held as two fp16 numbers whose sum it is to 22 bits or more: 64 bytes
 //               of high parts, then 64 bytes of low parts. Three products (low*high, high*low, high*high) into one
@@ -9,6 +9,10 @@
 //               operands give it, at a third of the fp16 matrix rate (the fp32 matrix instructions run at a
 //               sixteenth of it).
 //   KIND_MX     256 4-bit values a slab with one power-of-two scale per 32 (see mx.hip).
+//   KIND_THREE  64 fp32 values a group, each held as three bf16 numbers whose sum it is exactly (24 bits, at any
+//               size down to 2^-110: no scale): 128 bytes of high, of middle and of low parts. A group is six slabs, one
+//               for each product of parts that reaches 2^-24 of a term, each a slab of KIND_BF16; for products whose terms
+//               differ so much in size that no common power of two keeps two fp16 parts of all of them.
 //   KIND_F32    32 fp32 values a slab as they are, on the fp32 matrix instructions: exact products at a sixteenth of
 //               the bf16 rate, for products that memory bounds and whose operands are not worth writing in two parts.
 //
@@ -28,7 +32,7 @@
 
 namespace tile {
 
-enum Kind { KIND_BF16 = 0, KIND_SPLIT = 1, KIND_MX = 2, KIND_F32 = 3 };
+enum Kind { KIND_BF16 = 0, KIND_SPLIT = 1, KIND_MX = 2, KIND_F32 = 3, KIND_THREE = 4 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -47,18 +51,28 @@ constexpr uint32_t kOut = 0x7fffff00;  // an offset past every operand: reads ze
 // and an along extent.
 // 256 pitches stay under 2^31 (checked on the host).
 // KIND_MX: `scales` is the first row's scale bytes, pitch / 16 of them a row.
+// KIND_THREE: `extent` counts the bytes of one part; across, `base` is the group that holds the first column, `start`
+// that column's bytes within it.
 struct Operand {
   const char *base;
   int pitch, rows, extent;
   const char *scales = nullptr;
+  int start = 0;
+  int end = 0, parts = 0;  // KIND_THREE, set by Block: the first slab that is left out, the part of each of a group's slabs
 };
 
-// Values per slab, bytes per value of an across operand.
+// Values of k that kSlabs slabs take, bytes per value of an across operand.
 template <int KIND>
 struct Geometry {
-  static constexpr int kPerSlab = KIND == KIND_BF16 ? 64 : KIND == KIND_MX ? 256 : 32;
-  static constexpr int kBytes = KIND == KIND_BF16 ? 2 : 4;
+  static constexpr int kPerSlab = KIND == KIND_BF16 || KIND == KIND_THREE ? 64 : KIND == KIND_MX ? 256 : 32;
+  static constexpr int kSlabs = KIND == KIND_THREE ? 6 : 1;
+  static constexpr int kBytes = KIND == KIND_BF16 || KIND == KIND_THREE ? 2 : 4;
 };
+
+// KIND_THREE: where byte `b` of a row's high parts lies, a group's bytes, and the parts of A and of B (0 high, 1 middle, 2
+// low; two bits a slab) in the order of the slabs: the smallest products first.
+constexpr int kGroup3 = 3 * kSlab, kPartsA = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10, kPartsB = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+__host__ __device__ constexpr int place3(int b) { return b / kSlab * kGroup3 + b % kSlab; }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -109,8 +123,9 @@ struct Loader {
     row = t / (kRowBytes / 16);
     const int c = t % (kRowBytes / 16);
     chunk = ACROSS ? c ^ ((row << 1) & kTurn) : c ^ (row & 7);
-    offset = row * op.pitch + chunk * 16;
-    if ((ACROSS && chunk * 16 >= op.extent) || row * kRowBytes >= kData) offset = kOut;
+    const int from = op.start + chunk * 16;  // (start is 0 but for KIND_THREE)
+    offset = row * op.pitch + (ACROSS && KIND == KIND_THREE ? place3(from) : from);
+    if ((ACROSS && from >= op.extent) || row * kRowBytes >= kData) offset = kOut;
   }
 
   // A slab's loads, issued one at a time. Past the operand's k they read zeros: every slab has kRounds of them, which the
@@ -125,15 +140,21 @@ struct Loader {
     uint32_t off = offset;
     int wide, rows;
     uint64_t origin = (uint64_t)op.base;
+    const int unit = s / Geometry<KIND>::kSlabs;  // of k
     if (ACROSS) {
-      wide = min(op.extent, kRowBytes);
-      rows = min(op.rows - s * kSlabRows, kSlabRows);
-      origin += (uint64_t)(uint32_t)s * (uint32_t)(kSlabRows * op.pitch);
+      wide = min(op.extent, op.start + kRowBytes);
+      if (KIND == KIND_THREE) wide = place3(wide - 1) + 1;
+      rows = min(op.rows - unit * kSlabRows, kSlabRows);
+      origin += (uint64_t)(uint32_t)unit * (uint32_t)(kSlabRows * op.pitch);
     } else {
-      wide = min(op.extent - s * kSlab, kSlab);
+      wide = min(op.extent - unit * kSlab, kSlab);
       rows = wide > 0 ? min(op.rows, ROWS) : 0;
-      origin += (uint64_t)(uint32_t)s * kSlab;
+      origin += (uint64_t)(uint32_t)unit * (KIND == KIND_THREE ? kGroup3 : kSlab);
       if (chunk * 16 >= wide) off = kOut;
+    }
+    if constexpr (KIND == KIND_THREE) {
+      origin += (op.parts >> 2 * (s - unit * 6) & 3) * kSlab;
+      if (s >= op.end) rows = 0;
     }
     const int size = max(rows, 0) * op.pitch - op.pitch + wide;
     return {{uniform((int)origin), uniform((int)(origin >> 32)), uniform(rows > 0 ? size : 0), 0x00027000}, off, kRowsPerRound * op.pitch, lds};
@@ -256,7 +277,7 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
     return c;
-  } else if constexpr (KIND == KIND_BF16)
+  } else if constexpr (KIND == KIND_BF16 || KIND == KIND_THREE)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -265,7 +286,7 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 // The product of one block. WM x WN waves share it, each BM / WM x BN / WN outputs in subtiles of 16 x 16.
 // acc[i][j]: rows 16 i + lane % 16 of the wave's part, columns 16 j + 4 (lane / 16) + 0..3.
 //
-// STAGES buffers in LDS. A slab is multiplied in passes: its two halves (bf16, 4-bit), or high*high, high*low, low*high
+// STAGES buffers in LDS. A slab is multiplied in passes: its two halves (bf16, three parts, 4-bit), or high*high, high*low, low*high
 // (KIND_SPLIT). A pass goes down the subtiles of A, and each one's registers take the next pass's fragment as soon as
 // its products are issued, so that LDS reads run between products and one set of A fragments is enough. A little
 // into a slab's last pass, when its last fragments have been read, the waves meet, and the slab's buffer takes
@@ -287,6 +308,7 @@ struct Block {
   using ScaleA = ScaleLoader<BM, kGroup>;
   using ScaleB = ScaleLoader<BN, kGroup>;
   static constexpr bool kMx = KIND == KIND_MX;
+  static constexpr bool kRagged = KIND == KIND_BF16 || KIND == KIND_F32;  // rows that are read in place may end within a chunk
   static constexpr int kValuesA = LoadA::kBytes, kValues = kValuesA + LoadB::kBytes;
   static constexpr int kPart = kValues + (kMx ? ScaleA::kBytes + ScaleB::kBytes : 0);  // a group's slab
   static constexpr int kStage = GROUPS * kPart;
@@ -324,9 +346,14 @@ struct Block {
   }
   // Nothing of the operand past slab s1.
   __device__ __forceinline__ static void clip(Operand &op, bool across, int slab_rows, int s1) {
-    int &k = across ? op.rows : op.extent;
-    const int64_t end = (int64_t)s1 * (across ? slab_rows : kSlab);
-    if (end < k) k = (int)end;
+    if constexpr (KIND == KIND_THREE) {
+      op.end = uniform(s1);
+      op.start = uniform(op.start);
+    } else {
+      int &k = across ? op.rows : op.extent;
+      const int64_t end = (int64_t)s1 * (across ? slab_rows : kSlab);
+      if (end < k) k = (int)end;
+    }
     op.pitch = uniform(op.pitch);
     op.rows = uniform(op.rows);
     op.extent = uniform(op.extent);
@@ -354,6 +381,8 @@ struct Block {
   __device__ __forceinline__ void run(Operand a, Operand b, int s0, int s1, char *lds) {
     clip(a, ACROSS_A, LoadA::kSlabRows, s1);
     clip(b, ACROSS_B, LoadB::kSlabRows, s1);
+    a.parts = kPartsA;
+    b.parts = kPartsB;
     LoadA la;
     LoadB lb;
     ScaleA lsa;
@@ -401,7 +430,7 @@ struct Block {
       if (now_b && s_b == s) trim<BN, kGroup>(stage + kValuesA, b.extent);
       if (now_a || now_b) meet();
     };
-    if constexpr (KIND != KIND_SPLIT && !kMx) trim_last(s0, lds);
+    if constexpr (kRagged) trim_last(s0, lds);
     constexpr int kAcross = KIND == KIND_F32 ? 4 : 2;                      // LDS reads of a fragment across
     constexpr int kEach = kMx ? 2 : ACROSS_A ? kAcross : 1;                // with a subtile of A
     constexpr int kAll = kTN * (kMx ? 2 : ACROSS_B ? kAcross : 1);         // with all of B
@@ -445,7 +474,7 @@ struct Block {
       // slab s + 1 has arrived; all fragments of slab s are in registers
       wait_loads<(STAGES - 2) * kLoads>();
       meet();
-      if constexpr (KIND != KIND_SPLIT && !kMx) trim_last(s + GROUPS, lds + at * kStage);
+      if constexpr (kRagged) trim_last(s + GROUPS, lds + at * kStage);
       constexpr bool kSpread = kTM >= 8 && GROUPS == 1;  // a small block has no time to spread its loads over
       if constexpr (kSpread)
         load_scales(s + STAGES, used);

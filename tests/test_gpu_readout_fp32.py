@@ -1,0 +1,120 @@
+"""The readout's fp32 gradient where rows, classes, features or weights differ by many powers of two, at more than 128 rows
+and classes (the form whose operands are held in parts), against 64 bits.
+
+Bounds. u = 2^-24. The logits are products of operands in two fp16 parts under a power of two of each row: off by at most
+d = (6 k / 32 + 40) u + 4 * 2^-22 of a logit's sum of magnitudes plus 2^-38 k of its two rows' largest magnitudes. A
+softmax of logits off by up to d lies between those of l - d and l + d; lse rounds by 2 u (1 + |lse|) beyond that, and exp's
+argument and result by (|l - lse| + 8) 2^-22. G is those probabilities less one at the label, rounded twice (the subtraction,
+the weight). dx and dw are sums of G in three bf16 parts (exact; products below 2^-24 of a term are left out), so each
+value's error goes by its own sum of magnitudes, without a common floor: (6 k / 32 + 40) u + 4 u of it, what G's error
+makes of it, and two roundings of the result."""
+import pytest
+
+from tests.gpu_util import log, torch_cuda
+from tests.test_gpu_readout import Case
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TINY = 2.0 ** -100  # what parts below the normal numbers lose
+
+
+def sums(k):
+    return (6 * k / 32 + 40) * U
+
+
+def check(c, g, certain=()):
+    """`certain`: rows whose answer is certain and right; their part of G is zero to the bit."""
+    t = c.torch
+    live = (c.y >= 0) & (c.y < c.w.shape[0])
+    x, w = t.where(live[:, None], c.x.double(), 0.0), c.w.double()
+    l, k = x @ w.t(), x.shape[1]
+    d = (sums(k) + 4 * 2.0 ** -22) * (x.abs() @ w.abs().t()) + 2.0 ** -38 * k * x.abs().amax(1)[:, None] * w.abs().amax(1)
+    lse = t.logsumexp(l, 1)
+    e = t.maximum(t.logsumexp(l + d, 1) - lse, lse - t.logsumexp(l - d, 1)) + 2 * U * (1 + lse.abs())
+    p = t.exp(l - lse[:, None])
+    ep = t.exp(l - lse[:, None] + d + e[:, None] + ((l - lse[:, None]).abs() + 8) * 2.0 ** -22) - p
+    G = p.scatter_add(1, c.y.clamp(0, w.shape[0] - 1)[:, None], -t.ones_like(p[:, :1]))
+    weight = t.where(live, t.full_like(lse, 1.0 / max(1, int(live.sum()))) if g is None else g.double(), 0.0)[:, None]
+    for r in certain:
+        G[r] = ep[r] = 0
+        assert not c.dx[r].any(), f"row {r} is certain"
+    G, eG = G * weight, (ep + 2 * U * G.abs()) * weight.abs()
+    for name, got, a, ea, b in (("dx", c.dx, G, eG, w.t().contiguous()), ("dw", c.dw, G.t().contiguous(), eG.t().contiguous(), x.t().contiguous())):
+        want, size = a @ b.t(), a.abs() @ b.abs().t()
+        bound = (sums(a.shape[1]) + 4 * U) * size + 1.01 * (ea @ b.abs().t()) + 4 * U * want.abs() + TINY * float(b.abs().max())
+        assert bool(got.isfinite().all()), f"{name} is not finite"
+        over = ((got.double() - want).abs() / bound).amax()
+        assert float(over) <= 1.0, f"{name} is {float(over):.3g} times its bound off"
+
+
+SIZES = [(200, 300, 64), (257, 1000, 129), (700, 131, 33)]
+
+
+def weights(c, which):
+    if which == "mean":
+        return None
+    gen = c.torch.Generator("cuda").manual_seed(7)
+    return c.torch.randn(len(c.y), generator=gen, device="cuda") * c.torch.exp2(-(c.torch.arange(len(c.y), device="cuda") % 40.0))
+
+
+@pytest.mark.parametrize("which", ["mean", "weights"])
+@pytest.mark.parametrize("size", [1.0, 1e4, 1e8, 1e12, 1e20])
+@pytest.mark.parametrize("rows,classes,features", SIZES)
+def test_one_row_far_larger(rows, classes, features, size, which):
+    """A labelled row `size` times the others, whose answer is certain and right: the others' gradients are theirs."""
+    log(f"readout fp32 one row {size:g} times {rows} x {classes} x {features} {which}")
+    c = Case(rows, classes, features, "float32", seed=3)
+    certain = ()
+    if size > 1:
+        c.x[3] *= size
+        l = c.x[3].double() @ c.w.double().t()
+        c.y[3] = l.argmax()
+        if size >= 1e8:  # (at 1e4 the next class may be near)
+            certain = (3,)
+    if size == 1e4:
+        c.y[3] = -1
+    g = weights(c, which)
+    c.run(g)
+    check(c, g, certain)
+
+
+@pytest.mark.parametrize("which", ["mean", "weights"])
+@pytest.mark.parametrize("size", [1e4, 1e8, 1e12, 1e20])
+@pytest.mark.parametrize("rows,classes,features", SIZES)
+def test_one_class_far_larger(rows, classes, features, size, which):
+    """A class's weights `size` times the others' and negative against rows that are not: no row answers it."""
+    log(f"readout fp32 one class {size:g} times {rows} x {classes} x {features} {which}")
+    c = Case(rows, classes, features, "float32", seed=4)
+    c.w[5] = -size * c.w[5].abs()
+    c.y[c.y == 5] = 6
+    g = weights(c, which)
+    c.run(g)
+    check(c, g)
+
+
+@pytest.mark.parametrize("rows,classes,features", SIZES)
+def test_features_of_many_sizes(rows, classes, features):
+    """Features 30 binary orders apart: the gradient of the smallest is as good as that of the largest."""
+    log(f"readout fp32 features {rows} x {classes} x {features}")
+    c = Case(rows, classes, features, "float32", seed=5)
+    c.x *= c.torch.exp2(-(c.torch.arange(features, device="cuda") % 31.0))
+    c.run()
+    check(c, None)
+
+
+def test_values_at_the_ends_of_fp32():
+    """Rows and weights near fp32's largest and smallest: nothing turns infinite on the way, the small ones count."""
+    log("readout fp32 ends")
+    c = Case(150, 140, 40, "float32", seed=6)
+    c.x[2], c.x[4] = 3.4e38 * (c.x[2] > 0), 1e-30 * c.x[4]
+    c.w *= 1e-38  # logits up to about 1
+    c.w[7] = 1e-37
+    c.run()
+    assert bool(c.loss.isfinite().all()) and bool(c.dx.isfinite().all()) and bool(c.dw.isfinite().all())
+    l = c.x.double() @ c.w.double().t()
+    G = c.torch.softmax(l, 1)
+    G[c.torch.arange(150), c.y] -= 1
+    want = G.t() @ c.x.double() / 150
+    size = (G.t().abs() @ c.x.double().abs()) / 150
+    # (logits within 2^-20 of their magnitudes, at most 40 * 4 of them a row)
+    assert float(((c.dw.double() - want).abs() - 160 * 2.0 ** -20 * size).max()) <= 0
