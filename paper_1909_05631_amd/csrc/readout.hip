@@ -516,7 +516,7 @@ struct LossSpace {
 };
 
 struct GradSpace {
-  Plan logits[2], dx_plan, dw_plan[2];  // of a whole piece and of the last one
+  Plan logits, dx_plan, dw_plan[2];  // dw: of a whole piece and of the last one
   char *x, *w, *x3, *w3, *g;
   int *ex, *ew;
   Scalars *scalars;
@@ -539,16 +539,18 @@ struct GradSpace {
     const int64_t piece = s.piece(), rest = s.classes % piece;
     dx_plan = s.dx();
     dx = c.take<float>(dx_plan.splits > 1 || piece < s.classes ? (size_t)(dx_plan.splits * s.rows * s.ld_slab()) : 0);
+    // the loss's blocks and parts of k, whatever the piece: the logits are those that lse was taken of, to the bit. With
+    // sums in another order a logit of 1e6 would be off by a sixteenth against its own lse, and a certain answer not certain.
+    logits = s.logits(s.classes);
     size_t most = 0;
     for (int i = 0; i < 2; ++i) {
       const int64_t n = i == 0 ? piece : rest;
       if (n == 0) continue;
-      logits[i] = s.logits(n);
       dw_plan[i] = s.dw(n);
       if (dw_plan[i].splits > 1) most = std::max(most, (size_t)(dw_plan[i].splits * n * s.ld_slab()));
     }
     dw = c.take<float>(most);
-    slabs = c.take<float>(std::max(s.logit_slabs(logits[0], piece), rest ? s.logit_slabs(logits[1], rest) : 0));
+    slabs = c.take<float>(s.logit_slabs(logits, piece));
   }
 };
 
@@ -717,7 +719,7 @@ sdnn_status grad_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     wg.data += v0 * bg.pitch;
     wp.rows = wg.rows = n;
     const WriteGrad<KIND> e{{sp.ex, sp.ew + v0}, labels, lse, weights, sp.scalars, s.rows, s.classes, v0, n, sp.g, s.g_pitch()};
-    const Plan &pl = sp.logits[n < piece];
+    const Plan &pl = sp.logits;
     if (pl.splits > 1) {
       const int64_t ld = ceil_div(n, 4) * 4;
       st = run_shape<KIND, false, false>(pl, a, wp, s.rows, n, s.features, Accumulate{sp.slabs, ld, s.rows, n, false}, stream, "gradient");
