@@ -208,7 +208,8 @@ typedef enum {
 
 /* Bytes of workspace for sdnn_readout_loss (gradient = 0) or for both calls (gradient = 1). It grows with
  * n_rows * n_features and n_features * n_classes (fp32 operands are held in 16-bit parts, unaligned ones are
- * copied), not with n_rows * n_classes past 2^26 of them. 0 for sizes that the calls refuse: n_rows in [0, 2^24],
+ * copied); what it holds for each row and class together stays under 256 MB for the loss, and for the gradient under
+ * 6 bytes times the larger of 2^26 and 256 n_rows, however many there are of both. 0 for sizes that the calls refuse: n_rows in [0, 2^24],
  * n_classes in [1, 2^24], n_features in [1, 2^20]. */
 size_t sdnn_readout_workspace_bytes(int64_t n_rows, int64_t n_classes, int64_t n_features, int32_t dtype,
                                     int32_t gradient);

@@ -8,14 +8,15 @@
 // whatever it holds.
 //
 // Loss: one pass over w. A block of up to 256 rows by as many classes has its logits in registers; the epilogue takes
-// the maximum and the sum of exponentials of its columns per row (fp32), k_loss joins them. Nothing of size
-// n_rows x n_classes is written. Where there are few logits (at most 2^24) and blocks for only a part of the
+// the maximum and the sum of exponentials of its columns per row (fp32), k_loss joins them: 8 bytes are written for 32 to
+// 64 logits. Past 2^30 logits rows and classes are gone over in panels of that many, a row's softmax so far is carried
+// from one panel of its classes to the next, and what is written grows no more. Where there are few logits (at most 2^24) and blocks for only a part of the
 // CUs, the features are split instead, and a workgroup a row joins the slabs and takes the softmax.
 // Gradient: piece by piece, the logits are computed again (2 of 8 T V D operations, against a logit matrix in memory),
 // the epilogue writes the piece's G (bf16; fp32 inputs: three bf16 parts), and two products read it, dx +=
 // G w (over the piece's classes) and dw = G^T x (over the rows), both through the transposing LDS reads, so neither
-// w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G: it stays in the Infinity Cache
-// between the products.
+// w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G (or 256 classes of all rows): in bf16
+// it stays in the Infinity Cache between the products.
 //
 // What bounds it, measured on this card (a copy runs at 4.8 TB/s, the library's bf16 product at 1570-1650 TFLOP/s):
 //   8192 x 4096 x 32768, bf16: 6.5 ms, matrix instructions: loss 1.60-1.63 ms (1350-1376 TFLOP/s), each of four pieces
@@ -47,6 +48,7 @@ namespace {
 
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
+constexpr int64_t kPanel = 1 << 30, kPanelClasses = 1 << 16;  // of logits at a time in the loss, of classes where rows go in panels too
 constexpr int64_t kPlain = 128;            // fp32 rows or classes for the plain fp32 products: see Sizes::kind
 constexpr int64_t kSplitLogits = 1 << 24;  // logits whose features may be split: past that there is a 256 x 256 block for every CU
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -184,7 +186,7 @@ template <int KIND>
 struct LossParts {
   LogitScale scale;
   const int64_t *labels;
-  int64_t rows, classes;
+  int64_t rows, first, classes;  // of the panel; its first class
   float2 *parts;   // [rows][count]
   int64_t count;   // parts of a row
   float *picked;   // the label's logit
@@ -197,7 +199,7 @@ struct LossParts {
       const int64_t t = row0 + 16 * i + i16;
       const bool in = t < rows;
       const int er = KIND == KIND_SPLIT && in ? scale.row[t] : 0;
-      const int64_t y = in ? labels[t] : -1;
+      const int64_t y = in ? labels[t] - first : -1;
       float l[4 * B::kTN], m = -__builtin_inff();
 #pragma unroll
       for (int j = 0; j < B::kTN; ++j)
@@ -223,7 +225,7 @@ struct LossParts {
   }
 };
 
-// Joins the parts of a row: one wave a row, or a workgroup where there are many. A NaN logit makes NaN of its row's
+// Joins the parts of a row, and what is carried of the panels before: one wave a row, or a workgroup where there are many. A NaN logit makes NaN of its row's
 // sum (the maximum passes it over).
 struct Softmax {
   float top, sum;
@@ -233,12 +235,21 @@ struct Softmax {
     top = n;
   }
 };
+// The rows of a panel and what their softmax comes to.
+struct Losses {
+  const float *picked;
+  const int64_t *labels;
+  int64_t rows, classes;  // all classes
+  float *loss, *lse;
+  float2 *carried;   // nullptr: all classes are in one panel
+  bool first, last;  // of the panels of these rows' classes
+};
 template <int WAVES>
-__global__ __launch_bounds__(256) void k_loss(const float2 *parts, int64_t count, const float *picked, const int64_t *labels, int64_t rows, int64_t classes, float *loss, float *lse) {
+__global__ __launch_bounds__(256) void k_loss(const float2 *parts, int64_t count, Losses to) {
   __shared__ float2 shared[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t t = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-  if (WAVES == 1 && t >= rows) return;
+  if (WAVES == 1 && t >= to.rows) return;
   Softmax a{-__builtin_inff(), 0.0f};
 #pragma unroll 4
   for (int64_t p = threadIdx.x & (64 * WAVES - 1); p < count; p += 64 * WAVES) {
@@ -256,9 +267,14 @@ __global__ __launch_bounds__(256) void k_loss(const float2 *parts, int64_t count
     for (int w = 1; w < 4; ++w) a.join(shared[w].x, shared[w].y);
   }
   if (lane == 0 && (WAVES == 1 || wave == 0)) {
+    if (!to.first) a.join(to.carried[t].x, to.carried[t].y);
+    if (!to.last) {
+      to.carried[t] = float2{a.top, a.sum};
+      return;
+    }
     const float s = a.top + logf(a.sum);
-    if (lse) lse[t] = s;
-    loss[t] = counted(labels, t, classes) ? s - picked[t] : 0.0f;
+    if (to.lse) to.lse[t] = s;
+    to.loss[t] = counted(to.labels, t, to.classes) ? s - to.picked[t] : 0.0f;
   }
 }
 
@@ -293,11 +309,11 @@ __global__ __launch_bounds__(256) void k_loss_slabs(const float *slabs, int spli
   }
 }
 
-sdnn_status join_parts(const float2 *parts, int64_t count, const float *picked, const int64_t *labels, int64_t rows, int64_t classes, float *loss, float *lse, hipStream_t stream) {
-  if (count > 256 && rows < 8 * kCus)
-    hipLaunchKernelGGL((k_loss<4>), dim3((unsigned)rows), dim3(256), 0, stream, parts, count, picked, labels, rows, classes, loss, lse);
+sdnn_status join_parts(const float2 *parts, int64_t count, const Losses &to, hipStream_t stream) {
+  if (count > 256 && to.rows < 8 * kCus)
+    hipLaunchKernelGGL((k_loss<4>), dim3((unsigned)to.rows), dim3(256), 0, stream, parts, count, to);
   else
-    hipLaunchKernelGGL((k_loss<1>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, stream, parts, count, picked, labels, rows, classes, loss, lse);
+    hipLaunchKernelGGL((k_loss<1>), dim3((unsigned)ceil_div(to.rows, 4)), dim3(256), 0, stream, parts, count, to);
   return launched("loss");
 }
 
@@ -466,6 +482,12 @@ struct Sizes {
   // then the larger one, and writing it in two parts costs more than products that are three times as fast save
   // (loss and gradient of 128 x 1024 x 65536 613 us; of 129 rows, in two parts, 748; of 16 rows 289 and 609).
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, classes) <= kPlain ? KIND_F32 : KIND_SPLIT; }
+  // The loss's panels: all of it, or whole blocks of 256 rows and of 256 or 192 classes.
+  int64_t panel_classes() const {
+    if (rows * classes <= kPanel) return classes;
+    return std::min(classes, std::max(kPanelClasses, kPanel / rows) / 768 * 768);
+  }
+  int64_t panel_rows() const { return rows * panel_classes() <= kPanel ? rows : std::min(rows, std::max<int64_t>(256, kPanel / panel_classes() / 256 * 256)); }
   // Classes of a piece: 2^26 values of G, whole blocks of 256 classes.
   int64_t piece() const {
     const int64_t p = std::max<int64_t>(256, std::min(kPieceClasses, kPieceValues / std::max<int64_t>(rows, 1)) / 256 * 256);
@@ -498,7 +520,7 @@ struct LossSpace {
   Plan loss{};
   char *x, *w;
   int *ex, *ew;
-  float2 *parts;
+  float2 *parts, *carried;
   float *picked, *slabs;
   int64_t count;
   LossSpace(Carver &c, const Sizes &s) {
@@ -508,8 +530,9 @@ struct LossSpace {
     w = c.take<char>(packed ? s.packed(s.classes) : 0);
     ex = c.take<int>(s.rows);
     ew = c.take<int>(s.classes);
-    count = !packed ? (s.rows_held() ? (int64_t)few::grid_of(s.few(), s.classes, false) * few::batch_of(s.few()) : 0) : ceil_div(s.classes, kWaveCols[loss.shape]);
-    parts = c.take<float2>(s.rows * count);
+    count = !packed ? (s.rows_held() ? (int64_t)few::grid_of(s.few(), s.classes, false) * few::batch_of(s.few()) : 0) : ceil_div(s.panel_classes(), kWaveCols[loss.shape]);
+    parts = c.take<float2>((packed ? s.panel_rows() : s.rows) * count);
+    carried = c.take<float2>(packed && s.panel_classes() < s.classes ? s.panel_rows() : 0);
     picked = c.take<float>(s.rows);
     slabs = c.take<float>(packed ? s.logit_slabs(loss, s.classes) : 0);
   }
@@ -617,7 +640,7 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     p.picked = sp.picked;
     if (!s.rows_held()) return few::launch<false, false>(s.few(), p, stream, "loss");
     st = few::launch<true, false>(s.few(), p, stream, "loss");
-    return st != SDNN_OK ? st : join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
+    return st != SDNN_OK ? st : join_parts(sp.parts, sp.count, Losses{sp.picked, labels, s.rows, s.classes, loss, lse, nullptr, true, true}, stream);
   }
   Matrix a, b;
   if constexpr (KIND != KIND_SPLIT) {
@@ -639,10 +662,24 @@ sdnn_status loss_of(const Sizes &s, const T *x, int64_t ldx, const T *w, int64_t
     hipLaunchKernelGGL((k_loss_slabs<KIND>), dim3((unsigned)s.rows), dim3(256), 0, stream, sp.slabs, sp.loss.splits, ld, scale, labels, s.rows, s.classes, loss, lse);
     return launched("loss");
   }
-  const LossParts<KIND> e{scale, labels, s.rows, s.classes, sp.parts, sp.count, sp.picked};
-  st = run_shape<KIND, false, false>(sp.loss, a, b, s.rows, s.classes, s.features, e, stream, "loss");
-  if (st != SDNN_OK) return st;
-  return join_parts(sp.parts, sp.count, sp.picked, labels, s.rows, s.classes, loss, lse, stream);
+  const int64_t panel = s.panel_rows(), piece = s.panel_classes();
+  for (int64_t t0 = 0; t0 < s.rows; t0 += panel)
+    for (int64_t v0 = 0; v0 < s.classes; v0 += piece) {
+      const int64_t m = std::min(panel, s.rows - t0), n = std::min(piece, s.classes - v0);
+      Matrix ap = a, bp = b;
+      ap.data += t0 * a.pitch;
+      bp.data += v0 * b.pitch;
+      ap.rows = m;
+      bp.rows = n;
+      const int64_t count = ceil_div(n, kWaveCols[sp.loss.shape]);
+      const LossParts<KIND> e{{sp.ex + t0, sp.ew + v0}, labels + t0, m, v0, n, sp.parts, count, sp.picked + t0};
+      st = run_shape<KIND, false, false>(sp.loss, ap, bp, m, n, s.features, e, stream, "loss");
+      if (st != SDNN_OK) return st;
+      const Losses to{sp.picked + t0, labels + t0, m, s.classes, loss + t0, lse ? lse + t0 : nullptr, sp.carried, v0 == 0, v0 + n == s.classes};
+      st = join_parts(sp.parts, count, to, stream);
+      if (st != SDNN_OK) return st;
+    }
+  return SDNN_OK;
 }
 
 // C = A B^T over k, into `to` directly or through fp32 slabs.

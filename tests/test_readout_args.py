@@ -128,3 +128,15 @@ def test_binding_refuses_tensors_off_the_gpu():
             call()
     with pytest.raises(ValueError, match="float16"):
         readout.workspace_bytes(1, 1, 1, torch.float16)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("rows,classes", [(60000, 65536), (60000, 131072), (1 << 20, 65536), (1 << 22, 1 << 18), (1000, 1 << 24), (1 << 24, 1 << 15)])
+def test_workspace_does_not_grow_with_rows_times_classes(lib, rows, classes, dtype):
+    """Past what grows with the rows (at most 8 bytes a value of x, and 40 a row) and with the classes (the same), the loss takes at
+    most 256 MB and 1 MB of rounding; the gradient, with sums of dx and parts of 6 bytes a value too, 6 bytes times its
+    values of G."""
+    f, d = lib.sdnn_readout_workspace_bytes, 64
+    assert f(rows, classes, d, dtype, 0) <= (rows + classes) * (8 * d + 40) + (257 << 20)
+    splits = 64  # parts of k whose sums may be kept
+    assert f(rows, classes, d, dtype, 1) <= (rows + classes) * ((14 + 4) * d + 40) + splits * 4 * d * min(rows, classes) + 6 * max(1 << 26, 256 * rows) + (257 << 20)
