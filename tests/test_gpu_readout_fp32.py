@@ -118,3 +118,111 @@ def test_values_at_the_ends_of_fp32():
     size = (G.t().abs() @ c.x.double().abs()) / 150
     # (logits within 2^-20 of their magnitudes, at most 40 * 4 of them a row)
     assert float(((c.dw.double() - want).abs() - 160 * 2.0 ** -20 * size).max()) <= 0
+
+
+def case(**kw):
+    """Sizes on which both operands go in parts."""
+    c = Case(**{**dict(rows=171, classes=300, features=97, dtype="float32", seed=9), **kw})
+    assert min(c.x.shape[0], c.w.shape[0]) > 128
+    return c
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 0), (0, 1), (1, 0), (8, 0), (3, 5), (24, 8)])
+@pytest.mark.parametrize("features", [33, 64, 96, 97, 129])
+def test_strides_and_alignment(features, pad, offset):
+    """Rows apart from each other, bases on any value, NaN all around: nothing outside a matrix is used or written."""
+    log(f"readout fp32 strides {features} {pad} {offset}")
+    c = case(features=features, pad=pad, offset=offset)
+    around = [t.as_strided((t.untyped_storage().nbytes() // t.element_size(),), (1,), 0) for t in (c.dx, c.dw)]
+    before = [a.isnan().sum() for a in around]
+    for which in ("mean", "weights"):
+        g = weights(c, which)
+        c.run(g)
+        check(c, g)
+    assert [a.isnan().sum() for a in around] == before
+
+
+def test_rows_without_a_label():
+    """They hold NaN, infinities and huge values, and so do their weights; labels are below, at and past the ends."""
+    log("readout fp32 masked rows")
+    c = case()
+    t = c.torch
+    out = t.tensor([0, 3, 64, 65, 100, 170], device="cuda")
+    c.y[out] = t.tensor([-1, 300, -100, 1 << 40, -(1 << 62), 301], device="cuda")
+    c.x[0], c.x[3, 5], c.x[64], c.x[65, 0], c.x[100] = float("nan"), float("inf"), -float("inf"), 3e38, 1e30
+    g = t.rand(171, device="cuda")
+    g[out] = float("nan")
+    for w in (None, g):
+        c.run(w)
+        check(c, None if w is None else t.where(w.isnan(), 0.0, w))
+        assert not c.loss[out].any() and not c.dx[out].any()
+
+
+def test_no_row_has_a_label():
+    log("readout fp32 all masked")
+    c = case()
+    c.y.fill_(-1)
+    c.x.fill_(float("nan"))
+    c.run()
+    assert not c.loss.any() and not c.dx.any() and not c.dw.any()
+
+
+@pytest.mark.parametrize("what", ["dx", "dw"])
+def test_one_gradient_alone(what):
+    log(f"readout fp32 {what} alone")
+    c = case()
+    c.run()
+    want = getattr(c, what).clone()
+    getattr(c, what).fill_(5)
+    c.ws.fill_(255)
+    c.r.gradient(c.x, c.w, c.y, c.lse, c.dx if what == "dx" else None, c.dw if what == "dw" else None, c.ws)
+    assert c.torch.equal(getattr(c, what), want)
+
+
+def test_labelled_rows_of_infinities_and_nan():
+    """Such a row has a NaN in its loss and its dx, and makes NaN of dw; the other rows' dx are what they are without it."""
+    log("readout fp32 infinities")
+    c = case()
+    c.run()
+    dx, lse = c.dx.clone(), c.lse.clone()
+    c.x[0, 1], c.x[2, 0], c.x[4, 96] = float("inf"), -float("inf"), float("nan")
+    c.run()
+    bad = c.torch.zeros(171, dtype=c.torch.bool, device="cuda")
+    bad[[0, 2, 4]] = True
+    assert c.torch.equal(c.dx.isnan().any(1), bad) and c.torch.equal(c.dx[~bad], dx[~bad]) and c.torch.equal(c.lse[~bad], lse[~bad])
+    assert bool(c.loss[bad].isnan().all()) and bool(c.dw.isnan().any())
+
+
+def test_gradient_against_differences():
+    """Directional derivatives of the loss as the library computes it: the loss's error is at most 1e-5 a row, that of the
+    quotient at h^2 / 6 times the third derivative, at most the cube of twice the logits' largest change along the direction."""
+    log("readout fp32 differences")
+    c = case(features=64)
+    t = c.torch
+    c.run()
+    h = 0.02
+    gen = t.Generator("cuda").manual_seed(4)
+    for name, grad in (("x", c.dx), ("w", c.dw)):
+        base = getattr(c, name).clone()
+        d = t.randn(base.shape, generator=gen, device="cuda")
+        d /= d.norm(dim=1, keepdim=True)
+        total = []
+        for sign in (1, -1):
+            getattr(c, name).copy_(base + sign * h * d)
+            c.r.loss(c.x, c.w, c.y, c.loss, None, c.ws)
+            total.append(float(c.loss.double().mean()))
+        getattr(c, name).copy_(base)
+        along = (d.double() @ c.w.double().t() if name == "x" else c.x.double() @ d.double().t()).abs().max()
+        want = float((grad.double() * d.double()).sum())
+        assert abs((total[0] - total[1]) / (2 * h) - want) <= 1e-5 / h + h * h / 6 * float(2 * along) ** 3
+
+
+def test_several_pieces():
+    """More classes than a piece of G holds, the last one ragged; a row and a class far larger than the others."""
+    log("readout fp32 pieces")
+    c = Case(2100, 33000, 40, "float32", seed=15)
+    c.y[::7] = -1
+    c.x[3] *= 1e8
+    c.y[3] = (c.x[3].double() @ c.w.double().t()).argmax()
+    c.run()
+    check(c, None, (3,))
