@@ -123,6 +123,10 @@ def _matrices(name: str, t, like=None) -> tuple[int, int, int]:
 def orthogonalize(g, out, workspace, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
                   stream=None) -> None:
     """out = g (a matrix, or a batch of them) orthogonalised by `steps` Newton-Schulz products; out may be g itself."""
+    try:
+        a, b, c = (float(v) for v in coefficients)
+    except (TypeError, ValueError) as e:
+        raise ValueError(f"coefficients {coefficients!r} are not three numbers") from e
     _on_gpu("g", g)
     dt = _dtype(g.dtype)
     pg, ldg, batch_g = _matrices("g", g)
@@ -130,7 +134,7 @@ def orthogonalize(g, out, workspace, steps: int = 5, coefficients=(3.4445, -4.77
         raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(g.shape)} of {g.dtype}")
     po, ldo, batch_o = _matrices("out", out, g)
     batch, (rows, cols) = g.shape[0] if g.dim() == 3 else 1, g.shape[-2:]
-    coef = (ctypes.c_float * 3)(*coefficients)
+    coef = (ctypes.c_float * 3)(a, b, c)
     _call(g, "sdnn_orthogonalize", pg, ldg, batch_g, po, ldo, batch_o, dt, batch, rows, cols, steps, coef, eps,
           *_workspace(workspace, g), _stream_handle(stream))
 

@@ -140,3 +140,10 @@ def test_workspace_does_not_grow_with_rows_times_classes(lib, rows, classes, dty
     assert f(rows, classes, d, dtype, 0) <= (rows + classes) * (8 * d + 40) + (257 << 20)
     splits = 64  # parts of k whose sums may be kept
     assert f(rows, classes, d, dtype, 1) <= (rows + classes) * ((14 + 4) * d + 40) + splits * 4 * d * min(rows, classes) + 6 * max(1 << 26, 256 * rows) + (257 << 20)
+
+
+@pytest.mark.parametrize("coefficients", [(), (1.5, -0.5), (1.0, 1.0, 1.0, 1.0), 3.0, ("a", 1, 1)])
+def test_binding_refuses_coefficients_that_are_not_three_numbers(coefficients):
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="coefficients"):
+        readout.orthogonalize(x, x, x, coefficients=coefficients)
