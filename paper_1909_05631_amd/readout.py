@@ -114,8 +114,10 @@ def _matrices(name: str, t, like=None) -> tuple[int, int, int]:
     _on_gpu(name, t, like)
     if t.dim() not in (2, 3):
         raise ValueError(f"{name} is neither a matrix nor a batch of them")
-    if t.numel() == 0:
-        raise ValueError(f"{name} is empty")
+    if 0 in t.shape[-2:]:
+        raise ValueError(f"the matrices of {name} are empty")
+    if t.numel() == 0:  # a batch of none
+        return t.data_ptr(), t.shape[2], 0
     p, ld = _rows(name, t if t.dim() == 2 else t[0], None, None, t.dtype)
     return p, ld, t.stride(0) if t.dim() == 3 else 0
 
