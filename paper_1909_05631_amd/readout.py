@@ -132,6 +132,7 @@ def orthogonalize(g, out, workspace, steps: int = 5, coefficients=(3.4445, -4.77
     _on_gpu("g", g)
     dt = _dtype(g.dtype)
     pg, ldg, batch_g = _matrices("g", g)
+    _on_gpu("out", out, g)
     if tuple(out.shape) != tuple(g.shape) or out.dtype != g.dtype:
         raise ValueError(f"out is {tuple(out.shape)} of {out.dtype}, not {tuple(g.shape)} of {g.dtype}")
     po, ldo, batch_o = _matrices("out", out, g)

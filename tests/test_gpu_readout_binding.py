@@ -19,6 +19,17 @@ def test_no_matrices_are_no_error(shape):
         readout.orthogonalize(g[:, :0], g[:, :0], ws)  # matrices without rows
 
 
+def test_orthogonalize_refuses_what_is_no_tensor():
+    from paper_1909_05631_amd import readout
+    torch = torch_cuda()
+    log("no tensor")
+    g = torch.zeros(2, 4, 5, device="cuda")
+    ws = torch.empty(readout.orthogonalize_workspace_bytes(2, 4, 5), dtype=torch.uint8, device="cuda")
+    for out in (None, 3, g.tolist(), g.cpu(), g[0]):
+        with pytest.raises(ValueError):
+            readout.orthogonalize(g, out, ws)
+
+
 @pytest.mark.parametrize("rows,outputs", [(0, 5), (5, 0)])
 def test_no_rows_or_outputs_of_4_bits(rows, outputs):
     from paper_1909_05631_amd import readout
