@@ -468,6 +468,9 @@ sdnn_status sum_slabs(const float *slabs, int splits, int64_t ld_slab, const Sto
 
 constexpr int kWaveCols[kShapes] = {64, 48, 48, 64, 64, 32, 32, 32, 32};  // columns of a wave: the parts of a row of logits
 
+// The size of equal parts of `all`, of at most about `most` each and whole units but for the last.
+int64_t part_of(int64_t all, int64_t most, int64_t unit) { return std::min(all, ceil_div(ceil_div(all, ceil_div(all, most)), unit) * unit); }
+
 // Sizes of one call.
 struct Sizes {
   int64_t rows, classes, features;
@@ -482,12 +485,11 @@ struct Sizes {
   // then the larger one, and writing it in two parts costs more than products that are three times as fast save
   // (loss and gradient of 128 x 1024 x 65536 613 us; of 129 rows, in two parts, 748; of 16 rows 289 and 609).
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, classes) <= kPlain ? KIND_F32 : KIND_SPLIT; }
-  // The loss's panels: all of it, or whole blocks of 256 rows and of 256 or 192 classes.
-  int64_t panel_classes() const {
-    if (rows * classes <= kPanel) return classes;
-    return std::min(classes, std::max(kPanelClasses, kPanel / rows) / 768 * 768);
-  }
-  int64_t panel_rows() const { return rows * panel_classes() <= kPanel ? rows : std::min(rows, std::max<int64_t>(256, kPanel / panel_classes() / 256 * 256)); }
+  // The loss's panels: all of it, or equal parts of whole blocks (256 rows, 256 or 192 classes): a last one of a few
+  // classes would be a launch that fills few CUs (60000 x 1024 x 65536 bf16: 7.5 ms, 7.8 with last panels of 256 classes; 7.3
+  // in one launch, whose parts take twice the memory).
+  int64_t panel_classes() const { return rows * classes <= kPanel ? classes : part_of(classes, std::max(kPanelClasses, kPanel / rows), 768); }
+  int64_t panel_rows() const { return rows * classes <= kPanel ? rows : part_of(rows, std::max<int64_t>(256, kPanel / panel_classes() / 256 * 256), 256); }
   // Classes of a piece: 2^26 values of G, whole blocks of 256 classes.
   int64_t piece() const {
     const int64_t p = std::max<int64_t>(256, std::min(kPieceClasses, kPieceValues / std::max<int64_t>(rows, 1)) / 256 * 256);
