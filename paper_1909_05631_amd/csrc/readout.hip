@@ -31,7 +31,7 @@
 // rows and columns take back. The gradient's products cannot: their sums run over the rows of x or the classes, whose
 // sizes may lie any number of powers of two apart, and one row of x or of w far larger than the others would leave
 // these no bits. So G, w and x go there as three bf16 parts, which need no common scale. Where rows or classes are at
-// most 128, all go to the fp32 matrix instructions as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts). One to four rows or classes
+// most 192, all go to the fp32 matrix instructions as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts). One to four rows or classes
 // (few.h) mostly have no use for tiles: one kernel with fp32 arithmetic streams the other matrix past them, once.
 #include "dense.h"
 #include "few.h"
@@ -49,7 +49,7 @@ namespace {
 constexpr int64_t kPieceValues = 1 << 26;  // of G at a time
 constexpr int64_t kPieceClasses = 1 << 19;
 constexpr int64_t kPanel = 1 << 30, kPanelClasses = 1 << 16;  // of logits at a time in the loss, of classes where rows go in panels too
-constexpr int64_t kPlain = 128;            // fp32 rows or classes for the plain fp32 products: see Sizes::kind
+constexpr int64_t kPlain = 192;            // fp32 rows or classes for the plain fp32 products: see Sizes::kind
 constexpr int64_t kSplitLogits = 1 << 24;  // logits whose features may be split: past that there is a 256 x 256 block for every CU
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -482,8 +482,10 @@ struct Sizes {
   int64_t three_pitch() const { return ceil_div(features, 64) * tile::kGroup3; }
   size_t packed(int64_t n) const { return kind() == KIND_SPLIT ? (size_t)(n * groups() * 128) : (size_t)(n * pitch_values() * dtype_bytes(dtype)); }
   // fp32 operands go to the fp32 matrix instructions as they are up to kPlain rows or classes: the other matrix is
-  // then the larger one, and writing it in two parts costs more than products that are three times as fast save
-  // (loss and gradient of 128 x 1024 x 65536 613 us; of 129 rows, in two parts, 748; of 16 rows 289 and 609).
+  // then the larger one, and writing it in parts costs more than faster products save. Loss and gradient, us, as they are
+  // and in parts: 64 x 1024 x 65536 374 and 794; 160 rows 833 and 972; 192 rows 856 and 984; 256 rows 1160 and 1045; 512
+  // rows 2259 and 1524; 192 x 1000 x 10007 173 both, 256 rows 223 and 196; 60000 x 1024 x 130 classes 928 and 949, 200
+  // classes 1211 and 1019. (Small products gain by it past that, 512 x 512 x 512 66 and 70, 5000 x 200 x 256 65 and 81.)
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, classes) <= kPlain ? KIND_F32 : KIND_SPLIT; }
   // The loss's panels: all of it, or equal parts of whole blocks (256 rows, 256 or 192 classes): a last one of a few
   // classes would be a launch that fills few CUs (60000 x 1024 x 65536 bf16: 7.5 ms, 7.8 with last panels of 256 classes; 7.3

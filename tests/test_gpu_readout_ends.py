@@ -9,7 +9,7 @@ LONG = 1 << 20
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("rows,classes,features,pad", [(3, 5, LONG, 0), (200, 150, LONG, 0), (130, 131, LONG - 1, 2), (70, 9, LONG, 500000)])
+@pytest.mark.parametrize("rows,classes,features,pad", [(3, 5, LONG, 0), (200, 250, LONG, 0), (200, 150, LONG, 0), (200, 201, LONG - 1, 2), (70, 9, LONG, 500000)])
 def test_long_rows(rows, classes, features, pad, dtype):
     log(f"readout long rows {rows} x {classes} x {features} + {pad} {dtype}")
     c = Case(rows, classes, features, dtype, seed=1, pad=pad)
