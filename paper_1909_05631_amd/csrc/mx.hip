@@ -8,7 +8,7 @@
 //
 // The product runs on the scaled 4-bit matrix instructions (16 x 16 x 128, fp32 sums of exact products): 64 bytes
 // of a row are 4 lane groups' 16-byte blocks, and each lane hands the instruction its block's scale byte. 4096 x 16384
-// x 16384: 542 us with its quantisation, 4.0 PFLOP/s.
+// x 16384: 535 us with its quantisation once the card's clock has settled, 4.1 PFLOP/s (up to 680 in the first passes).
 #include "dense.h"
 
 using namespace dense;
@@ -153,14 +153,19 @@ sdnn_status product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8
 
 // Few rows: one launch that quantises x into LDS, every workgroup for itself, and streams w from memory to the matrix
 // instructions, each byte once and without LDS. A workgroup takes 16 outputs at a time and its four waves share k, 1024
-// values of a wave on their way at once; their sums meet in LDS. Bound by w's bytes: 65536 x 4096 (143 MB) takes 28 us
-// for one row, 5.2 TB/s. Every workgroup's own quantisation is what limits it: four rows of that take 32 us, 26 in
-// tiles. So it takes up to 4096 values, or up to 65536 where the outputs make no more workgroups than there are
-// CUs (1000 x 1024: 4 us; in tiles k would be one long chain: 4096 x 65536 takes 106 us there).
+// values of a wave on their way at once; their sums meet in LDS. Bound by w's bytes: 65536 x 4096 (143 MB) takes 28.6 us
+// for one row, 5.0 TB/s. Every workgroup's own quantisation is what limits it, by the row: 16 rows of 4096 cost 10 us
+// more than one. Measured against the tiles with their quantisation (us here / there, w not in the caches):
+//   up to 4 rows, whatever their length: 1 x 65536 to 4096 outputs 46/107, 4 x 16384 27/32; 1 x 8192 to 65536 outputs 54/65,
+//     4 x 8192 63/66, 4 x 16384 120/115 (the worst: 4 x 1024 to 65536 outputs 15/13);
+//   more rows, few values: 16 x 256 to 65536 outputs 9/12 (but 6 x 1024 15/13);
+//   more rows, few outputs, where the tiles would be a few long chains of k: 8 x 4096 to 4096 outputs 11.7/12.6, 16 x 2048
+//     11.4/11.8, but 12 x 4096 15/12, and 8 x 4096 to 20000 outputs 21/18.
 constexpr int kFewRows = 16, kFewValues = 65536;
 inline bool is_few(int64_t rows, int64_t outputs, int64_t n) {
   const int64_t values = rows * ceil_div(n, 256) * 256;
-  return rows <= kFewRows && (values <= 4096 || (values <= kFewValues && outputs <= 16 * kCus));
+  if (rows > kFewRows || values > kFewValues) return false;
+  return rows <= 4 || values <= 4096 || (values <= 32768 && outputs <= 32 * kCus);
 }
 
 template <class T>
