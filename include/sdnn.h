@@ -192,7 +192,7 @@ int32_t sdnn_kernel_path(const sdnn_net *net);
 
 /* ---------------------------------------------------------------------------------------------------------------
  * The dense readout: a layer of n_classes outputs on rows of n_features values, such as a network's final rows
- * (sdnn_final_rows) on the device. These calls need no handle. All matrices are row-major in device memory; a
+ * (sdnn_final_rows leaves them on the host; they are uploaded for these calls). These calls need no handle. All matrices are row-major in device memory; a
  * stride is the distance of two rows in values and at least the row's length. Everything is enqueued on
  * hip_stream (NULL = default stream), of the current device, on which all pointers must be usable; no call
  * waits, allocates or keeps anything, so each can be captured into a graph. A workspace is the caller's, 256-byte
@@ -208,8 +208,9 @@ typedef enum {
 
 /* Bytes of workspace for sdnn_readout_loss (gradient = 0) or for both calls (gradient = 1). It grows with
  * n_rows * n_features and n_features * n_classes (fp32 operands are held in 16-bit parts, unaligned ones are
- * copied); what it holds for each row and class together stays under 256 MB for the loss, and for the gradient under
- * 6 bytes times the larger of 2^26 and 256 n_rows, however many there are of both. 0 for sizes that the calls refuse: n_rows in [0, 2^24],
+ * copied). What it holds for each row and class together is bounded however many there are of both: for the loss by 256
+ * MB (or up to 64 fp32 parts of at most 2^24 logits, where rows are long), for the gradient by 6 bytes times the larger of
+ * 2^26 and 256 n_rows as well. 0 for sizes that the calls refuse: n_rows in [0, 2^24],
  * n_classes in [1, 2^24], n_features in [1, 2^20]. */
 size_t sdnn_readout_workspace_bytes(int64_t n_rows, int64_t n_classes, int64_t n_features, int32_t dtype,
                                     int32_t gradient);
@@ -229,7 +230,8 @@ sdnn_status sdnn_readout_loss(const void *x, int64_t ldx, const void *w, int64_t
 
 /* The gradient of sum_t row_grad_t loss_t, or, with row_grad == NULL, of the mean loss over the rows with a label:
  *   G_tv = row_grad_t (exp(l_tv - lse_t) - [v = label_t]),  dx = G w,  dw = G^T x.
- *   lse: as sdnn_readout_loss left it. row_grad: n_rows fp32 or NULL.
+ *   lse: as sdnn_readout_loss left it for these x and w, of whose logits exp(l - lse) takes the same bits. row_grad:
+ *   n_rows fp32 or NULL.
  *   dx: n_rows x n_features, dw: n_classes x n_features, of `dtype`, row strides lddx and lddw; overwritten. Either
  *   may be NULL: not computed. Neither may overlap an input.
  * Rows without a label add nothing to dw and have a dx of zeros, whatever x, lse and row_grad hold there. For bf16 G is
@@ -250,7 +252,9 @@ size_t sdnn_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t c
  * two sizes (for rows > cols the same X is found from X^T X).
  *   g, out: device, of `dtype`, row strides ldg and ldo, batch strides (values; ignored for one matrix). out may be
  *   g itself (same strides), and may not overlap it otherwise.
- * Every product is of factors held in two fp16 parts, with fp32 sums; the result is rounded to `dtype` once. A
+ * Every product is of factors held in two fp16 parts under one power of two for a matrix (2^-38 of a bound of its entries
+ * is the smallest part), with fp32 sums: errors are fp32's against the matrix's norm, a row far smaller than the others
+ * keeps fewer bits. The result is rounded to `dtype` once. A
  * matrix of zeros gives zeros (eps > 0); one with an infinity or a NaN gives NaN where those reach.
  * steps in [0, 32]; eps >= 0; |coefficients| <= 1e6. */
 sdnn_status sdnn_orthogonalize(const void *g, int64_t ldg, int64_t batch_stride_g, void *out, int64_t ldo,
@@ -283,7 +287,8 @@ sdnn_status sdnn_mx_product(const uint8_t *x_codes, const uint8_t *x_scales, con
                             int64_t ldo, int32_t dtype, void *hip_stream);
 
 /* The same for rows x of `dtype` (row stride ldx) that are quantised on the way: a readout's answer with its weights held
- * in 4 bits. The result is that of sdnn_mx_quantize and sdnn_mx_product. */
+ * in 4 bits. The products are those of sdnn_mx_quantize and sdnn_mx_product; for few rows their fp32 sums may be taken
+ * in another order. */
 size_t sdnn_mx_linear_workspace_bytes(int64_t n_rows, int64_t n_values);
 sdnn_status sdnn_mx_linear(const void *x, int64_t ldx, int32_t dtype, const uint8_t *w_codes, const uint8_t *w_scales,
                            int64_t n_rows, int64_t n_outputs, int64_t n_values, void *out, int64_t ldo, void *workspace,

@@ -10,9 +10,9 @@
 // blocks for few CUs (a small side against a long one) its k is split and a fourth launch joins the sums. Small
 // matrices are one launch in all (k_small).
 //
-// Measured (five steps): 4096 x 4096 fp32 3.4 ms, 404 TFLOP/s of fp32 in the products that are computed, bound by the
-// matrix instructions: A and A A 0.18-0.20 ms each (253 blocks of 192 x 192, one to a CU), X's update 0.30-0.32 ms.
-// 2000 x 1021 bf16 0.29 ms: 22, 14 and 23 us a step; the two squares have 136 blocks of 64 x 64 for 256 CUs, each
+// Measured (five steps): 4096 x 4096 fp32 3.3 ms, 411 TFLOP/s of fp32 in the products that are computed, bound by the
+// matrix instructions: A and A A 0.17-0.18 ms each (253 blocks of 192 x 192, one to a CU), X's update 0.29-0.31 ms.
+// 2000 x 1021 bf16 0.29 ms: 21, 14 and 22 us a step; the two squares have 136 blocks of 64 x 64 for 256 CUs, each
 // going through its k alone. 4 x 128 x 256 110 us: 17 launches of 6 to 8 us.
 //
 // Scaling: fp16 holds 2^-24 ... 65504, so each factor is held times a power of two from a bound of its

@@ -10,29 +10,32 @@
 // Loss: one pass over w. A block of up to 256 rows by as many classes has its logits in registers; the epilogue takes
 // the maximum and the sum of exponentials of its columns per row (fp32), k_loss joins them: 8 bytes are written for 32 to
 // 64 logits. Past 2^30 logits rows and classes are gone over in panels of that many, a row's softmax so far is carried
-// from one panel of its classes to the next, and what is written grows no more. Where there are few logits (at most 2^24) and blocks for only a part of the
-// CUs, the features are split instead, and a workgroup a row joins the slabs and takes the softmax.
+// from one panel of its classes to the next, and what is written grows no more. Where there are few logits (at most
+// 2^24) and blocks for only a part of the CUs, the features are split instead, and a workgroup a row joins the slabs
+// and takes the softmax.
 // Gradient: piece by piece, the logits are computed again (2 of 8 T V D operations, against a logit matrix in memory),
 // the epilogue writes the piece's G (bf16; fp32 inputs: three bf16 parts), and two products read it, dx +=
 // G w (over the piece's classes) and dw = G^T x (over the rows), both through the transposing LDS reads, so neither
 // w, x nor G is ever transposed in memory. A piece holds at most 2^26 values of G (or 256 classes of all rows): in bf16
 // it stays in the Infinity Cache between the products.
 //
-// What bounds it, measured on this card (a copy runs at 4.8 TB/s, the library's bf16 product at 1570-1650 TFLOP/s):
-//   8192 x 4096 x 32768, bf16: 6.5 ms, matrix instructions: loss 1.60-1.63 ms (1350-1376 TFLOP/s), each of four pieces
-//     0.42-0.44 ms logits and G, 0.39-0.44 ms dx, 0.37-0.38 ms dw (1480).
-//   64 x 1024 x 65536, bf16: 140 us, memory: w three times (23-25 us each, 5.8 TB/s), dw once (41 us, 3.3 TB/s).
-//   1021 x 1000 x 10007, fp32: 315 us: four products of 65-74 us, 280-310 TFLOP/s of fp32 against 477 of the largest (212
-//     blocks for 256 CUs in the logits, 256 in dx, 160 in dw), 38 us for writing x and w in two parts twice, 12 us
-//     for their largest values.
-//   2000 x 1024 x 10, fp32: 45 us, eight launches of 4 to 9 us.
+// What bounds it, measured on this card (a copy runs at 4.8 TB/s, the library's bf16 product at 1650 TFLOP/s once the
+// clock has settled under load, 1290 in its first passes; fp16 1555):
+//   8192 x 4096 x 32768, bf16: 6.5 ms, matrix instructions: loss 1.59 ms (1386 TFLOP/s), each of four pieces
+//     0.42-0.43 ms logits and G, 0.40-0.42 ms dx, 0.36-0.37 ms dw (1470-1520).
+//   64 x 1024 x 65536, bf16: 136 us, memory: w three times (23-25 us each, 5.4-5.8 TB/s), dw once (35 us, 3.8 TB/s).
+//   1021 x 1000 x 10007, fp32: 451 us: logits 62 us in the loss (333 TFLOP/s of fp32 in two fp16 parts, of 518) and 85 us
+//     with G's three parts stored; dx 98 us, dw 133 us (209 and 154 TFLOP/s in three bf16 parts, of 275; dw has
+//     160 blocks for 256 CUs); 64 us for writing x and w in parts, once a call.
+//   2000 x 1024 x 10, fp32: 45 us, eight launches of 5 to 8 us.
 //
 // fp32 inputs go to the logits as two fp16 parts under a power of two per row of x and of w, which the logits' own
 // rows and columns take back. The gradient's products cannot: their sums run over the rows of x or the classes, whose
 // sizes may lie any number of powers of two apart, and one row of x or of w far larger than the others would leave
 // these no bits. So G, w and x go there as three bf16 parts, which need no common scale. Where rows or classes are at
-// most 192, all go to the fp32 matrix instructions as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts). One to four rows or classes
-// (few.h) mostly have no use for tiles: one kernel with fp32 arithmetic streams the other matrix past them, once.
+// most 192, all go to the fp32 matrix instructions as they are (16 x 1024 x 65536: loss 55 us, 224 with w in two parts).
+// One to four rows or classes (few.h) mostly have no use for tiles: one kernel with fp32 arithmetic streams the other
+// matrix past them, once.
 #include "dense.h"
 #include "few.h"
 
