@@ -192,14 +192,14 @@ int32_t sdnn_kernel_path(const sdnn_net *net);
 
 /* ---------------------------------------------------------------------------------------------------------------
  * The dense readout: a layer of n_classes outputs on rows of n_features values, such as a network's final rows
- * (sdnn_final_rows leaves them on the host; they are uploaded for these calls). These calls need no handle. All matrices are row-major in device memory; a
- * stride is the distance of two rows in values and at least the row's length. Everything is enqueued on
- * hip_stream (NULL = default stream), of the current device, on which all pointers must be usable; no call
- * waits, allocates or keeps anything, so each can be captured into a graph. A workspace is the caller's, 256-byte
- * aligned, overwritten, and must stay untouched until the call's work completes on the stream; SDNN_ERANGE
- * where it is too small. Malformed arguments are SDNN_EINVAL and enqueue nothing. SDNN_EDEVICE: a launch failed
- * (some of the call's work may have been enqueued). Results do not depend on what else runs: the same
- * inputs give the same bits. */
+ * (sdnn_final_rows leaves them on the host; they are uploaded for these calls). These calls need no handle. All
+ * matrices are row-major in device memory; a stride is the distance of two rows in values and at least the row's
+ * length. Everything is enqueued on hip_stream (NULL = default stream), of the current device, on which all pointers
+ * must be usable; no call waits, allocates or keeps anything, so each can be captured into a graph. A workspace is the
+ * caller's, 256-byte aligned, overwritten, and must stay untouched until the call's work completes on the stream;
+ * SDNN_ERANGE where it is too small. Malformed arguments are SDNN_EINVAL and enqueue nothing. SDNN_EDEVICE: a launch
+ * failed (some of the call's work may have been enqueued). Results do not depend on what else runs: the same inputs
+ * give the same bits. */
 
 typedef enum {
   SDNN_FP32 = 0,
