@@ -294,6 +294,45 @@ sdnn_status sdnn_mx_linear(const void *x, int64_t ldx, int32_t dtype, const uint
                            int64_t n_rows, int64_t n_outputs, int64_t n_values, void *out, int64_t ldo, void *workspace,
                            size_t workspace_bytes, void *hip_stream);
 
+/* A gated hidden layer, such as one under a readout: h = act(g) * u with g = x w_gate^T and u = x w_up^T. The conventions
+ * are the readout's. */
+typedef enum {
+  SDNN_SILU = 0, /* g / (1 + exp(-g)) */
+  SDNN_GELU = 1, /* g times the normal distribution's integral up to g (by the error function) */
+  SDNN_RELU = 2  /* max(g, 0); its slope at 0 is 0 */
+} sdnn_activation;
+
+/* Bytes of workspace for sdnn_gated (gradient = 0), for both calls where the gradient gets gate and up (1), or where
+ * it computes them again (2). 0 for sizes that the calls refuse: n_rows in [0, 2^24], n_hidden in [1, 2^19], n_features in
+ * [1, 2^20]. For the gradient it grows with n_rows * n_hidden. */
+size_t sdnn_gated_workspace_bytes(int64_t n_rows, int64_t n_hidden, int64_t n_features, int32_t dtype, int32_t gradient);
+
+/* The layer.
+ *   x: n_rows x n_features, w_gate, w_up: n_hidden x n_features, all of `dtype`, with their row strides.
+ *   h: n_rows x n_hidden of `dtype`, written.  gate, up: the same size, or NULL: g and u, rounded to `dtype`, for
+ *   sdnn_gated_grad. None of the three may overlap an input or another.
+ * g and u are fp32 sums, of exact products for bf16 inputs; fp32 inputs are multiplied as they are or as two fp16 parts
+ * each (22 bits or more of each value down to 2^-17 of its row's largest). h is taken from these sums, whether they are kept or
+ * not, and rounded once. Infinities and NaN give what the formula gives of them, in the rows and outputs that they
+ * reach. */
+sdnn_status sdnn_gated(const void *x, int64_t ldx, const void *w_gate, int64_t ldw_gate, const void *w_up, int64_t ldw_up,
+                       int32_t dtype, int32_t activation, int64_t n_rows, int64_t n_hidden, int64_t n_features, void *h,
+                       int64_t ldh, void *gate, int64_t ldgate, void *up, int64_t ldup, void *workspace,
+                       size_t workspace_bytes, void *hip_stream);
+
+/* Its gradient: with dg = dh * u * act'(g) and du = dh * act(g),
+ *   dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x.
+ *   gate, up: as sdnn_gated kept them, or both NULL: they are computed again, with the same results.
+ *   dh: n_rows x n_hidden.  dx: n_rows x n_features, dw_gate, dw_up: n_hidden x n_features; overwritten. Each may be
+ *   NULL: not computed. None may overlap an input or another. All are of `dtype`.
+ * For bf16 dg and du are rounded to bf16 once, between fp32 arithmetic and fp32 sums. fp32 values are multiplied as they
+ * are or as three bf16 parts each (all 24 bits of a value down to 2^-110). With no rows dw_gate and dw_up are zeros. */
+sdnn_status sdnn_gated_grad(const void *x, int64_t ldx, const void *w_gate, int64_t ldw_gate, const void *w_up,
+                            int64_t ldw_up, int32_t dtype, int32_t activation, const void *gate, int64_t ldgate,
+                            const void *up, int64_t ldup, const void *dh, int64_t lddh, int64_t n_rows, int64_t n_hidden,
+                            int64_t n_features, void *dx, int64_t lddx, void *dw_gate, int64_t lddw_gate, void *dw_up,
+                            int64_t lddw_up, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -235,8 +235,26 @@ struct Matrix {
   int64_t extent;  // bytes in a row: of k (along), of columns (across); KIND_THREE: of one part
   int64_t batch;   // bytes from one matrix of a batch (blockIdx.y) to the next
   const uint8_t *scales = nullptr;  // KIND_MX: pitch / 16 bytes a row
-  template <int KIND, int SIZE, bool ACROSS>
+  // An operand of two matrices of `rows` rows each (tile::Operand). across: the first's rows of k are padded to `units` slabs
+  const char *second = nullptr;
+  int64_t pitch_second = 0;
+  int units = 0;
+  template <int KIND, int SIZE, bool ACROSS, bool TWO = false>
   __device__ __forceinline__ tile::Operand at(int block) const {
+    if constexpr (TWO) {
+      constexpr int kRows = tile::Geometry<KIND>::kPerSlab;  // of k in a slab across
+      tile::Operand o = at<KIND, ACROSS ? SIZE : SIZE / 2, ACROSS>(block);
+      const int64_t first = (int64_t)block * (SIZE / 2);  // along: of each
+      const int64_t skip = ACROSS ? o.base - data : first * pitch_second;
+      o.second = second + skip;
+      o.pitch_second = (int)pitch_second;
+      if (ACROSS) {
+        o.units = units;
+        o.first_rows = (int)rows;
+        o.rows = (int)(units * kRows + rows);
+      }
+      return o;
+    }
     const int64_t first = (int64_t)block * SIZE;
     const char *here = data + blockIdx.y * batch;
     if (ACROSS && KIND == tile::KIND_THREE) {
@@ -251,7 +269,7 @@ struct Matrix {
   }
 };
 
-template <class B, int KIND, int BM, int BN, bool ACROSS_A, bool ACROSS_B, class Epilogue>
+template <class B, int KIND, int BM, int BN, bool ACROSS_A, bool ACROSS_B, bool TWO_B, class Epilogue>
 __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blocks blocks, Epilogue epilogue) {
   __shared__ __attribute__((aligned(1024))) char lds[B::kLds];
   int r, c, split;
@@ -262,15 +280,15 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
   blocks.range(split, s0, s1);
   const int64_t row0 = (int64_t)r * BM + B::row0(), col0 = (int64_t)c * BN + B::col0();
   B block;
-  block.run(a.template at<KIND, BM, ACROSS_A>(r), b.template at<KIND, BN, ACROSS_B>(c), s0, s1, lds);
+  block.run(a.template at<KIND, BM, ACROSS_A>(r), b.template at<KIND, BN, ACROSS_B, TWO_B>(c), s0, s1, lds);
   if (B::holds()) epilogue(block, row0, col0, split, r != c);
 }
 
 // Launches the blocks of one shape. What the sizes need of it is the caller's rule.
-template <int KIND, int BM, int BN, int WM, int WN, int STAGES, int GROUPS, bool ACROSS_A, bool ACROSS_B, class Epilogue>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES, int GROUPS, bool ACROSS_A, bool ACROSS_B, bool TWO_B = false, class Epilogue>
 sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const Epilogue &e, hipStream_t stream, const char *what, bool symmetric,
                    int batch) {
-  using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES, GROUPS>;
+  using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES, GROUPS, TWO_B>;
   Blocks blocks;
   blocks.slabs = (int)ceil_div(k, tile::Geometry<KIND>::kPerSlab) * tile::Geometry<KIND>::kSlabs;
   blocks.per = (int)ceil_div(blocks.slabs, splits);
@@ -278,10 +296,10 @@ sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols,
   const int64_t r = ceil_div(rows, BM), c = ceil_div(cols, BN);
   const int64_t n = symmetric ? c * (c + 1) / 2 : r * c * splits;
   blocks.symmetric = symmetric;
-  if (n * B::kThreads > 0xffffffffll || a.pitch > kMaxPitch || b.pitch > kMaxPitch) return fail(SDNN_EINVAL, "%s: %lld x %lld outputs are too many for one launch", what, (long long)rows, (long long)cols);
+  if (n * B::kThreads > 0xffffffffll || a.pitch > kMaxPitch || b.pitch > kMaxPitch || b.pitch_second > kMaxPitch) return fail(SDNN_EINVAL, "%s: %lld x %lld outputs are too many for one launch", what, (long long)rows, (long long)cols);
   blocks.rows = (int)r;
   blocks.cols = (int)c;
-  hipLaunchKernelGGL((k_product<B, KIND, BM, BN, ACROSS_A, ACROSS_B, Epilogue>), dim3((unsigned)n, (unsigned)batch), dim3(B::kThreads), 0, stream, a, b, blocks, e);
+  hipLaunchKernelGGL((k_product<B, KIND, BM, BN, ACROSS_A, ACROSS_B, TWO_B, Epilogue>), dim3((unsigned)n, (unsigned)batch), dim3(B::kThreads), 0, stream, a, b, blocks, e);
   return launched(what);
 }
 
@@ -326,29 +344,30 @@ inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_split
   return best;
 }
 
-template <int KIND, bool AA, bool AB, class E>
+// TWO: b is of two matrices (blocks of 192 columns do not split into wave parts of whole pairs).
+template <int KIND, bool AA, bool AB, bool TWO = false, class E>
 sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
   constexpr int kPair = KIND == tile::KIND_MX ? 1 : 2;  // (its scales need LDS too: two blocks a CU instead)
   if constexpr (KIND == tile::KIND_F32) {
     switch (p.shape) {
-      case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-      case kFlat: return launch<KIND, 32, 128, 1, 4, 3, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-      case kTall: return launch<KIND, 128, 32, 4, 1, 3, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-      default: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      case kFlat: return launch<KIND, 32, 128, 1, 4, 3, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      case kTall: return launch<KIND, 128, 32, 4, 1, 3, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      default: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     }
   } else {
   switch (p.shape) {
-    case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kBroad:
-      if constexpr (!AA && !AB) return launch<KIND, 256, 192, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      if constexpr (!AA && !AB && !TWO) return launch<KIND, 256, 192, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
     case kMiddle:
-      if constexpr (!AA && !AB) return launch<KIND, 192, 192, 2, 4, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kPaired: return launch<KIND, 128, 128, 2, 2, 2, 2, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kStream: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    default: return launch<KIND, 128, 32, 4, 1, 3, kPair, AA, AB>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      if constexpr (!AA && !AB && !TWO) return launch<KIND, 192, 192, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kPaired: return launch<KIND, 128, 128, 2, 2, 2, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kStream: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    default: return launch<KIND, 128, 32, 4, 1, 3, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
   }
   }
 }

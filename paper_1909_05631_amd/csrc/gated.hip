@@ -1,0 +1,614 @@
+// A gated hidden layer on rows of features, h = act(g) * u with g = x wg^T and u = x wu^T, and its gradient:
+//
+//   dg = dh * u * act'(g),  du = dh * act(g)
+//   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x
+//
+// Layer: one product. A block's columns are 16 rows of wg and 16 of wu in turn, read where they are, so that a wave
+// holds g and u of the same outputs in neighbouring subtiles and the epilogue takes the activation and the product from
+// fp32 sums; g and u are written only where the caller keeps them for the gradient. Where there are few outputs and blocks for
+// only a part of the CUs, the features are split and a second kernel joins the parts.
+// Gradient: one pass over g, u and dh writes dg and du side by side, a row of 2 H values (each half padded to whole
+// slabs of k with zeros). Then two products read them: dx = [dg du] [wg; wu], whose k goes through both halves into one
+// sum, and [dwg; dwu] = [dg du]^T x. Nothing is transposed or concatenated in memory.
+//
+// fp32: the layer's sums run along rows of x and w, which take a power of two each and go in two fp16 parts; the gradient's run
+// across rows of any size, so dg, du, w and x go there in three bf16 parts, which need no scale. Few rows or outputs go to
+// the fp32 matrix instructions as they are.
+#include "dense.h"
+#include "few.h"
+#include "sums.h"
+
+using namespace dense;
+using namespace sums;
+using tile::KIND_BF16;
+using tile::KIND_F32;
+using tile::KIND_SPLIT;
+using tile::KIND_THREE;
+
+namespace {
+
+constexpr int64_t kMaxHidden = 1 << 19;    // a row of dg and du in three parts is then the longest that the tiles take
+constexpr int64_t kSplitValues = 1 << 24;  // values of g and u whose features may be split
+constexpr int64_t kPlain = 192;            // fp32 rows or outputs for the plain fp32 products
+
+// act(g) and, for the gradient, act'(g).
+struct Activated {
+  float value, slope;
+};
+template <bool SLOPE>
+__device__ __forceinline__ Activated activated(int activation, float g) {
+  Activated a;
+  a.slope = 0.0f;
+  if (activation == SDNN_SILU) {
+    // g p with p = 1 / (1 + exp(-g)); the exponential may be infinite: p is then 0
+    const float p = 1.0f / (1.0f + few::exp_of(-g));
+    a.value = g * p;
+    if (SLOPE) a.slope = fmaf(a.value, 1.0f - p, p);
+  } else if (activation == SDNN_GELU) {
+    // g P with P the normal distribution, by erfc, which keeps its relative precision in the lower tail
+    const float p = 0.5f * erfcf(g * -0.70710678118654752440f);
+    a.value = g * p;
+    if (SLOPE) a.slope = fmaf(g * 0.39894228040143267794f, few::exp_of(-0.5f * g * g), p);
+  } else {
+    a.value = g <= 0.0f ? 0.0f : g;
+    if (SLOPE) a.slope = g > 0.0f ? 1.0f : 0.0f;
+  }
+  return a;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Operands that are written anew
+
+// A matrix and where its rows go: fp32 in two fp16 parts under a power of two a row, in three bf16 parts, or as they are on
+// aligned rows.
+struct Source {
+  const void *data;
+  int64_t ld, rows;
+  char *out;
+  int *exponents;  // of two parts
+  bool vec;
+};
+struct Sources {
+  Source of[3];
+  int64_t cols;
+};
+
+// The source that row r of all of them is of, and its row there.
+__device__ __forceinline__ const Source &source_of(const Sources &s, int64_t &r) {
+  int i = 0;
+  while (i < 2 && r >= s.of[i].rows) r -= s.of[i++].rows;
+  return s.of[i];
+}
+
+// Two parts, zeros past the columns, a workgroup a row.
+__global__ __launch_bounds__(256) void k_two_parts(Sources s, int64_t rows) {
+  __shared__ float part[4];
+  const int64_t groups = ceil_div(s.cols, 32);
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+    int64_t r = i;
+    const Source &m = source_of(s, r);
+    const float *row = (const float *)m.data + r * m.ld;
+    float top = 0.0f;
+    for (int64_t k = threadIdx.x * 4; k < s.cols; k += 1024) {
+      const f32x4 v = few::load4(row, (int)k, (int)s.cols, m.vec);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a = fabsf(v[e]);
+        top = fmaxf(top, a < __builtin_inff() ? a : 0.0f);  // infinities and NaN have no say
+      }
+    }
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
+    __syncthreads();
+    const int e = split_exponent(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
+    if (threadIdx.x == 0) m.exponents[r] = e;
+    char *to = m.out + r * groups * 128;
+    for (int64_t k = threadIdx.x * 4; k < groups * 32; k += 1024) {
+      f32x4 v = few::load4(row, (int)k, (int)s.cols, m.vec);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = ldexpf(v[c], e);
+      store_split4(to, k, v);
+    }
+  }
+}
+
+// Three parts, zeros past the columns.
+__global__ __launch_bounds__(256) void k_three_parts(Sources s, int64_t rows) {
+  const int64_t groups = ceil_div(s.cols, 64);
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+    int64_t r = i;
+    const Source &m = source_of(s, r);
+    const float *row = (const float *)m.data + r * m.ld;
+    char *to = m.out + r * groups * tile::kGroup3;
+    for (int64_t k = threadIdx.x * 4; k < groups * 64; k += 1024) store_three4(to, k, few::load4(row, (int)k, (int)s.cols, m.vec));
+  }
+}
+
+// On rows of whole 16 bytes, zeros past the columns.
+template <class T>
+__global__ __launch_bounds__(256) void k_aligned(Sources s, int64_t rows) {
+  const int64_t pitch = ceil_div(s.cols, 8) * 8;
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+    int64_t r = i;
+    const Source &m = source_of(s, r);
+    const T *row = (const T *)m.data + r * m.ld;
+    T *to = (T *)m.out + r * pitch;
+    for (int64_t k = threadIdx.x * 4; k < pitch; k += 1024) store4(to + k, few::load4(row, (int)k, (int)s.cols, m.vec), 4, true);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// The layer's results
+
+template <int KIND, class T>
+struct Layer {
+  const int *ex, *eg, *eu;  // exponents of the rows of x, wg and wu (KIND_SPLIT)
+  int activation;
+  int64_t rows, hidden;
+  T *h, *gate, *up;  // gate and up: nullptr where they are not kept; h: nullptr where they alone are wanted
+  int64_t ldh, ldg, ldu;
+  bool vec_h, vec_g, vec_u;
+  // Four neighbours' sums from output c on, of row t with exponent e.
+  __device__ __forceinline__ f32x4 scaled(f32x4 s, int e, const int *exponents, int64_t c) const {
+    if constexpr (KIND == KIND_SPLIT) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = ldexpf(s[i], -e - (c + i < hidden ? exponents[c + i] : 0));
+    }
+    return s;
+  }
+  __device__ __forceinline__ f32x4 product(f32x4 g, f32x4 u) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g[i] = activated<false>(activation, g[i]).value * u[i];
+    return g;
+  }
+  template <class B>
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
+    constexpr int N = B::kTN / 2;  // pairs of subtiles: g and u
+    static_assert(B::kTN % 2 == 0, "whole pairs");
+    const int i16 = threadIdx.x & 15, j4 = (threadIdx.x & 63) >> 4;
+    const int64_t first = col0 / 2;
+#pragma unroll
+    for (int i = 0; i < B::kTM; ++i) {
+      const int64_t t = row0 + 16 * i + i16;
+      const bool in = t < rows;
+      const int e = KIND == KIND_SPLIT && in ? ex[t] : 0;
+      const auto g = [&](int j) { return scaled(block.acc[i][2 * j], e, eg, first + 16 * j + 4 * j4); };
+      const auto u = [&](int j) { return scaled(block.acc[i][2 * j + 1], e, eu, first + 16 * j + 4 * j4); };
+      if (gate) store_row<T, N>(gate + t * ldg, first, hidden, vec_g, in, g);
+      if (up) store_row<T, N>(up + t * ldu, first, hidden, vec_u, in, u);
+      if (h) store_row<T, N>(h + t * ldh, first, hidden, vec_h, in, [&](int j) { return product(g(j), u(j)); });
+    }
+  }
+};
+
+// The same from sums whose k was split: slabs of 16 columns of g and 16 of u in turn, `ld` a row.
+template <int KIND, class T>
+__global__ __launch_bounds__(256) void k_layer_slabs(const float *slabs, int splits, int64_t ld, Layer<KIND, T> to) {
+  const int64_t t = blockIdx.y;
+  const int e = KIND == KIND_SPLIT ? to.ex[t] : 0;
+  for (int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; c < to.hidden; c += (int64_t)gridDim.x * 1024) {
+    const float *from = slabs + t * ld + c / 16 * 32 + c % 16;
+    f32x4 g = {0.0f, 0.0f, 0.0f, 0.0f}, u = g;
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      g += *(const f32x4 *)(from + s * to.rows * ld);
+      u += *(const f32x4 *)(from + s * to.rows * ld + 16);
+    }
+    g = to.scaled(g, e, to.eg, c);
+    u = to.scaled(u, e, to.eu, c);
+    const int n = to.hidden - c < 4 ? (int)(to.hidden - c) : 4;
+    if (to.gate) store4(to.gate + t * to.ldg + c, g, n, to.vec_g);
+    if (to.up) store4(to.up + t * to.ldu + c, u, n, to.vec_u);
+    if (to.h) store4(to.h + t * to.ldh + c, to.product(g, u), n, to.vec_h);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// The gradient's dg and du
+
+template <class T>
+struct Slopes {
+  const T *gate, *up, *dh;
+  int64_t ldg, ldu, ldd;
+  bool vec;  // the three's rows are aligned for 16 bytes
+  int activation;
+  int64_t rows, hidden, half;  // half: values of dg with its zeros
+  char *out;
+  int64_t pitch;  // bytes
+};
+
+template <class T, int N>
+__device__ __forceinline__ void load_some(const T *row, int64_t c, int64_t n, bool vec, float (&v)[N]) {
+  typedef T Chunk __attribute__((ext_vector_type(N)));
+  if (vec && c + N <= n) {
+    const Chunk x = *(const Chunk *)(row + c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (float)x[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = c + i < n ? (float)row[c + i] : 0.0f;
+  }
+}
+
+// Where four values of a row's half go in the form of KIND.
+template <int KIND>
+__device__ __forceinline__ void store_slopes(char *row, int64_t c, const float *v) {
+  const f32x4 x = {v[0], v[1], v[2], v[3]};
+  if constexpr (KIND == KIND_THREE)
+    store_three4(row, c, x);
+  else if constexpr (KIND == KIND_F32)
+    store4((float *)row + c, x, 4, true);
+  else
+    store4((__bf16 *)row + c, x, 4, true);
+}
+
+// 16 bytes of each input a lane. dg and du are rounded to bf16 once, between fp32 arithmetic and fp32 sums (bf16).
+template <int KIND, class T>
+__global__ __launch_bounds__(256) void k_slopes(Slopes<T> p) {
+  constexpr int N = 16 / sizeof(T);
+  for (int64_t t = blockIdx.y; t < p.rows; t += gridDim.y)
+    for (int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * N; c < p.half; c += (int64_t)gridDim.x * 256 * N) {
+      float g[N], u[N], d[N];
+      load_some(p.gate + t * p.ldg, c, p.hidden, p.vec, g);
+      load_some(p.up + t * p.ldu, c, p.hidden, p.vec, u);
+      load_some(p.dh + t * p.ldd, c, p.hidden, p.vec, d);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const Activated a = activated<true>(p.activation, g[i]);
+        g[i] = c + i < p.hidden ? d[i] * u[i] * a.slope : 0.0f;
+        u[i] = c + i < p.hidden ? d[i] * a.value : 0.0f;
+      }
+      char *row = p.out + t * p.pitch;
+      if constexpr (KIND == KIND_BF16) {
+        typedef __bf16 Chunk __attribute__((ext_vector_type(N)));
+        Chunk a, b;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          a[i] = (__bf16)g[i];
+          b[i] = (__bf16)u[i];
+        }
+        *(Chunk *)((__bf16 *)row + c) = a;
+        *(Chunk *)((__bf16 *)row + p.half + c) = b;
+      } else {
+        store_slopes<KIND>(row, c, g);
+        store_slopes<KIND>(row, p.half + c, u);
+      }
+    }
+}
+
+// The two weights' gradients: rows [0, hidden) of the product are dwg's, those from `half` on dwu's.
+template <class T>
+struct TwoStores {
+  using Value = T;
+  T *gate, *up;  // either may be nullptr
+  int64_t ldg, ldu, hidden, half;
+  int64_t rows, cols;  // of the product: half + hidden
+  bool vec;
+  const float *factor = nullptr;
+  __device__ __forceinline__ T *row(int64_t r) const {
+    if (r < hidden) return gate ? gate + r * ldg : nullptr;
+    return r >= half && r < rows && up ? up + (r - half) * ldu : nullptr;
+  }
+  template <class B>
+  __device__ __forceinline__ void operator()(const B &block, int64_t row0, int64_t col0, int, bool) const {
+#pragma unroll
+    for (int i = 0; i < B::kTM; ++i) {
+      T *to = row(row0 + 16 * i + (threadIdx.x & 15));
+      store_row<T, B::kTN>(to, col0, cols, vec, to != nullptr, [&](int j) { return block.acc[i][j]; });
+    }
+  }
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void k_zero(T *out, int64_t ld, int64_t rows, int64_t cols) {
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int64_t c = threadIdx.x; c < cols; c += 256) out[r * ld + c] = (T)0.0f;
+}
+
+// ------------------------------------------------------------------------------------------------
+// Host
+
+struct Sizes {
+  int64_t rows, hidden, features;
+  int32_t dtype;
+  int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, hidden) <= kPlain ? KIND_F32 : KIND_SPLIT; }
+  int product_kind() const { return kind() == KIND_SPLIT ? KIND_THREE : kind(); }
+  int bytes() const { return dtype_bytes(dtype); }
+  // Bytes of a row of features written anew, as the layer and as the gradient take it.
+  int64_t pitch(int kind) const {
+    return kind == KIND_SPLIT ? ceil_div(features, 32) * 128 : kind == KIND_THREE ? ceil_div(features, 64) * tile::kGroup3 : ceil_div(features, 8) * 8 * bytes();
+  }
+  int64_t paired() const { return ceil_div(hidden, 16) * 32; }  // columns of the layer's product
+  int64_t half() const { return ceil_div(hidden, 64) * 64; }    // values of dg in a row, whole slabs of any kind
+  int64_t slopes_pitch() const { return product_kind() == KIND_THREE ? half() / 64 * 2 * tile::kGroup3 : half() * 2 * bytes(); }
+  Plan layer() const { return plan(kind(), rows, paired(), features, rows * paired() <= kSplitValues && rows <= 65535 ? kMaxSplits : 1); }
+  Plan dx() const { return plan(product_kind(), rows, features, 2 * half(), kMaxSplits); }
+  Plan dw() const { return plan(product_kind(), half() + hidden, features, rows, kMaxSplits); }
+  int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
+};
+
+// x, wg and wu written anew. Room for all three is always taken: whether rows can be read in place is a matter of their
+// addresses, which the workspace's size does not know.
+struct Copies {
+  char *x, *wg, *wu;
+  int *ex, *eg, *eu;
+  Copies(Carver &c, const Sizes &s, int kind) {
+    x = c.take<char>((size_t)(s.rows * s.pitch(kind)));
+    wg = c.take<char>((size_t)(s.hidden * s.pitch(kind)));
+    wu = c.take<char>((size_t)(s.hidden * s.pitch(kind)));
+    ex = c.take<int>(kind == KIND_SPLIT ? s.rows : 0);
+    eg = c.take<int>(kind == KIND_SPLIT ? s.hidden : 0);
+    eu = c.take<int>(kind == KIND_SPLIT ? s.hidden : 0);
+  }
+};
+
+struct LayerSpace {
+  Plan layer;
+  Copies copies;
+  float *slabs;
+  LayerSpace(Carver &c, const Sizes &s) : layer(s.layer()), copies(c, s, s.kind()), slabs(c.take<float>(layer.splits > 1 ? (size_t)(layer.splits * s.rows * s.paired()) : 0)) {}
+};
+
+struct GradSpace {
+  Plan dx, dw;
+  Copies copies;
+  char *slopes;
+  float *dx_slabs, *dw_slabs;
+  GradSpace(Carver &c, const Sizes &s) : dx(s.dx()), dw(s.dw()), copies(c, s, s.product_kind()) {
+    slopes = c.take<char>((size_t)(s.rows * s.slopes_pitch()));
+    dx_slabs = c.take<float>(dx.splits > 1 ? (size_t)(dx.splits * s.rows * s.ld_slab()) : 0);
+    dw_slabs = c.take<float>(dw.splits > 1 ? (size_t)(dw.splits * (s.half() + s.hidden) * s.ld_slab()) : 0);
+  }
+};
+
+template <class T>
+struct Inputs {
+  const T *x, *wg, *wu;
+  int64_t ldx, ldg, ldu;
+};
+
+// x and the weights as operands of KIND, written anew where they have to be; nullptr space: not wanted.
+struct Operands {
+  Matrix x, w;  // w: two matrices
+};
+template <int KIND, class T>
+sdnn_status operands(const Sizes &s, const Inputs<T> &in, const Copies &to, bool want_x, bool want_w, bool across, Operands &o, hipStream_t stream) {
+  const T *data[3] = {in.x, in.wg, in.wu};
+  const int64_t ld[3] = {in.ldx, in.ldg, in.ldu}, rows[3] = {s.rows, s.hidden, s.hidden};
+  char *space[3] = {to.x, to.wg, to.wu};
+  int *exponents[3] = {to.ex, to.eg, to.eu};
+  const bool want[3] = {want_x, want_w, want_w};
+  const char *base[3];
+  int64_t pitch[3], extent = KIND == KIND_SPLIT ? s.pitch(KIND) : KIND == KIND_THREE ? ceil_div(s.features, 8) * 16 : s.features * (int64_t)sizeof(T);
+  constexpr bool kParts = KIND == KIND_SPLIT || KIND == KIND_THREE;
+  // both weights are read in place, or neither: they share one extent
+  bool in_place[3];
+  for (int i = 0; i < 3; ++i) in_place[i] = !kParts && usable_in_place(data[i], ld[i], s.features, sizeof(T));
+  if (s.features * sizeof(T) % 4) extent = s.pitch(KIND);  // no row is usable in place then
+  Sources src{};
+  src.cols = s.features;
+  int64_t all = 0;
+  for (int i = 0; i < 3; ++i) {
+    const bool write = want[i] && !in_place[i];
+    src.of[i] = {data[i], ld[i], write ? rows[i] : 0, space[i], exponents[i], aligned16(data[i], ld[i], sizeof(T))};
+    all += src.of[i].rows;
+    base[i] = in_place[i] ? (const char *)data[i] : space[i];
+    pitch[i] = in_place[i] ? ld[i] * (int64_t)sizeof(T) : s.pitch(KIND);
+  }
+  if (all > 0) {
+    const dim3 grid((unsigned)std::min<int64_t>(all, 4096));
+    if constexpr (KIND == KIND_SPLIT)
+      hipLaunchKernelGGL(k_two_parts, grid, dim3(256), 0, stream, src, all);
+    else if constexpr (KIND == KIND_THREE)
+      hipLaunchKernelGGL(k_three_parts, grid, dim3(256), 0, stream, src, all);
+    else
+      hipLaunchKernelGGL((k_aligned<T>), grid, dim3(256), 0, stream, src, all);
+    const sdnn_status st = launched("rows");
+    if (st != SDNN_OK) return st;
+  }
+  o.x = {base[0], pitch[0], s.rows, extent, 0};
+  o.w = {base[1], pitch[1], s.hidden, extent, 0};
+  o.w.second = base[2];
+  o.w.pitch_second = pitch[2];
+  if (across) o.w.units = (int)(s.half() / tile::Geometry<KIND>::kPerSlab);
+  return SDNN_OK;
+}
+
+template <class T>
+struct Kept {
+  T *gate, *up;
+  int64_t ldg, ldu;
+};
+
+template <int KIND, class T>
+sdnn_status layer_of(const Sizes &s, const Inputs<T> &in, int activation, T *h, int64_t ldh, const Kept<T> &kept, Carver &carver, hipStream_t stream) {
+  const LayerSpace sp(carver, s);
+  Operands o;
+  sdnn_status st = operands<KIND>(s, in, sp.copies, true, true, false, o, stream);
+  if (st != SDNN_OK) return st;
+  const Layer<KIND, T> e{sp.copies.ex, sp.copies.eg, sp.copies.eu, activation, s.rows, s.hidden, h, kept.gate, kept.up, ldh, kept.ldg, kept.ldu,
+                         vector_rows(h, ldh), vector_rows(kept.gate, kept.ldg), vector_rows(kept.up, kept.ldu)};
+  if (sp.layer.splits == 1) return run_shape<KIND, false, false, true>(sp.layer, o.x, o.w, s.rows, s.paired(), s.features, e, stream, "gated layer");
+  const int64_t ld = s.paired();
+  st = run_shape<KIND, false, false, true>(sp.layer, o.x, o.w, s.rows, ld, s.features, Accumulate{sp.slabs, ld, s.rows, ld, false}, stream, "gated layer");
+  if (st != SDNN_OK) return st;
+  hipLaunchKernelGGL((k_layer_slabs<KIND, T>), dim3((unsigned)std::min<int64_t>(ceil_div(s.hidden, 1024), 256), (unsigned)s.rows), dim3(256), 0, stream, sp.slabs, sp.layer.splits, ld, e);
+  return launched("gated layer");
+}
+
+// Workgroups along a row of `items` lanes, and down the rows.
+dim3 grid_of(int64_t rows, int64_t items) {
+  const int64_t x = ceil_div(items, 256);
+  return dim3((unsigned)x, (unsigned)std::max<int64_t>(1, std::min<int64_t>({rows, 65535, ceil_div(kCus * 32, x)})));
+}
+
+template <class T>
+struct Gradients {
+  T *dx, *dwg, *dwu;
+  int64_t lddx, lddg, lddu;
+};
+
+template <int KIND, class T>
+sdnn_status grad_of(const Sizes &s, const Inputs<T> &in, int activation, const Kept<T> &kept, const T *dh, int64_t lddh, const Gradients<T> &to, Carver &carver, hipStream_t stream) {
+  constexpr int kProduct = KIND == KIND_SPLIT ? KIND_THREE : KIND;
+  const GradSpace sp(carver, s);
+  const bool weights = to.dwg || to.dwu;
+  const Slopes<T> p{kept.gate, kept.up, dh, kept.ldg, kept.ldu, lddh, vector_rows(kept.gate, kept.ldg) && vector_rows(kept.up, kept.ldu) && vector_rows(dh, lddh), activation,
+                    s.rows, s.hidden, s.half(), sp.slopes, s.slopes_pitch()};
+  hipLaunchKernelGGL((k_slopes<kProduct, T>), grid_of(s.rows, ceil_div(s.half(), 16 / (int)sizeof(T))), dim3(256), 0, stream, p);
+  sdnn_status st = launched("gated gradient");
+  if (st != SDNN_OK) return st;
+  Operands o;
+  st = operands<kProduct>(s, in, sp.copies, weights, to.dx != nullptr, true, o, stream);
+  if (st != SDNN_OK) return st;
+  const int64_t per_value = kProduct == KIND_THREE ? 2 : (int64_t)sizeof(T), ld = s.ld_slab();
+  const Matrix d{sp.slopes, s.slopes_pitch(), s.rows, 2 * s.half() * per_value, 0};
+  if (to.dx) {
+    const Store<T> e{to.dx, to.lddx, s.rows, s.features, vector_rows(to.dx, to.lddx)};
+    if (sp.dx.splits == 1) {
+      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), e, stream, "gated gradient of the rows");
+    } else {
+      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), Accumulate{sp.dx_slabs, ld, s.rows, s.features, false}, stream, "gated gradient of the rows");
+      if (st == SDNN_OK) st = sum_slabs(sp.dx_slabs, sp.dx.splits, ld, e, stream, "gated gradient of the rows");
+    }
+    if (st != SDNN_OK) return st;
+  }
+  if (weights) {
+    const int64_t rows = s.half() + s.hidden;
+    const TwoStores<T> e{to.dwg, to.dwu, to.lddg, to.lddu, s.hidden, s.half(), rows, s.features,
+                         (!to.dwg || vector_rows(to.dwg, to.lddg)) && (!to.dwu || vector_rows(to.dwu, to.lddu))};
+    if (sp.dw.splits == 1) {
+      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, e, stream, "gated gradient of the weights");
+    } else {
+      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, Accumulate{sp.dw_slabs, ld, rows, s.features, false}, stream, "gated gradient of the weights");
+      if (st == SDNN_OK) st = sum_slabs(sp.dw_slabs, sp.dw.splits, ld, e, stream, "gated gradient of the weights");
+    }
+  }
+  return st;
+}
+
+sdnn_status check_sizes(int64_t n_rows, int64_t n_hidden, int64_t n_features, int32_t dtype) {
+  if (n_rows < 0 || n_rows > kMaxRows) return fail(SDNN_EINVAL, "n_rows %lld is outside [0, %lld]", (long long)n_rows, (long long)kMaxRows);
+  if (n_hidden < 1 || n_hidden > kMaxHidden) return fail(SDNN_EINVAL, "n_hidden %lld is outside [1, %lld]", (long long)n_hidden, (long long)kMaxHidden);
+  if (n_features < 1 || n_features > kMaxFeatures) return fail(SDNN_EINVAL, "n_features %lld is outside [1, %lld]", (long long)n_features, (long long)kMaxFeatures);
+  if (!good_dtype(dtype)) return fail(SDNN_EINVAL, "dtype %d is neither SDNN_FP32 nor SDNN_BF16", dtype);
+  return SDNN_OK;
+}
+
+sdnn_status check_activation(int32_t activation) {
+  if (activation < SDNN_SILU || activation > SDNN_RELU) return fail(SDNN_EINVAL, "activation %d is none of SDNN_SILU, SDNN_GELU and SDNN_RELU", activation);
+  return SDNN_OK;
+}
+
+enum Gradient { kLayerOnly = 0, kFromKept = 1, kAgain = 2 };
+
+// The parts of a gradient call's workspace: g and u where they are computed again (and what the layer needs for it), then
+// the gradient's own over the same room.
+template <class T>
+Kept<T> again_space(Carver &c, const Sizes &s) {
+  const int64_t ld = ceil_div(s.hidden, 8) * 8;
+  T *gate = c.take<T>((size_t)(s.rows * ld)), *up = c.take<T>((size_t)(s.rows * ld));
+  return {gate, up, ld, ld};
+}
+
+size_t workspace_of(const Sizes &s, int gradient) {
+  Carver layer{nullptr};
+  if (gradient == kAgain) {
+    if (s.dtype == SDNN_BF16)
+      again_space<__bf16>(layer, s);
+    else
+      again_space<float>(layer, s);
+  }
+  Carver grad = layer;
+  LayerSpace a(layer, s);
+  if (gradient == kLayerOnly) return layer.used;
+  GradSpace b(grad, s);
+  return std::max(layer.used, grad.used);
+}
+
+template <int KIND, class T>
+sdnn_status layer_call(const Sizes &s, const void *x, int64_t ldx, const void *wg, int64_t ldg, const void *wu, int64_t ldu, int32_t activation, void *h, int64_t ldh, void *gate, int64_t ldgate, void *up,
+                       int64_t ldup, void *workspace, hipStream_t stream) {
+  Carver c{(char *)workspace};
+  return layer_of<KIND, T>(s, {(const T *)x, (const T *)wg, (const T *)wu, ldx, ldg, ldu}, activation, (T *)h, ldh, {(T *)gate, (T *)up, ldgate, ldup}, c, stream);
+}
+
+template <int KIND, class T>
+sdnn_status grad_call(const Sizes &s, const void *x, int64_t ldx, const void *wg, int64_t ldg, const void *wu, int64_t ldu, int32_t activation, const void *gate, int64_t ldgate, const void *up, int64_t ldup,
+                      const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dwg, int64_t lddg, void *dwu, int64_t lddu, void *workspace, hipStream_t stream) {
+  const Inputs<T> in{(const T *)x, (const T *)wg, (const T *)wu, ldx, ldg, ldu};
+  Carver c{(char *)workspace};
+  Kept<T> kept{(T *)gate, (T *)up, ldgate, ldup};
+  if (!gate) {
+    kept = again_space<T>(c, s);
+    Carver over = c;
+    const sdnn_status st = layer_of<KIND, T>(s, in, activation, nullptr, 0, kept, over, stream);
+    if (st != SDNN_OK) return st;
+  }
+  return grad_of<KIND, T>(s, in, activation, kept, (const T *)dh, lddh, {(T *)dx, (T *)dwg, (T *)dwu, lddx, lddg, lddu}, c, stream);
+}
+
+template <class T>
+void zero(void *p, int64_t ld, const Sizes &s, hipStream_t stream) {
+  if (p) hipLaunchKernelGGL((k_zero<T>), dim3(row_grid(s.hidden)), dim3(256), 0, stream, (T *)p, ld, s.hidden, s.features);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdnn_gated_workspace_bytes(int64_t n_rows, int64_t n_hidden, int64_t n_features, int32_t dtype, int32_t gradient) {
+  if (check_sizes(n_rows, n_hidden, n_features, dtype) != SDNN_OK || gradient < kLayerOnly || gradient > kAgain) return 0;
+  return workspace_of({n_rows, n_hidden, n_features, dtype}, gradient);
+}
+
+sdnn_status sdnn_gated(const void *x, int64_t ldx, const void *w_gate, int64_t ldw_gate, const void *w_up, int64_t ldw_up, int32_t dtype, int32_t activation, int64_t n_rows, int64_t n_hidden,
+                       int64_t n_features, void *h, int64_t ldh, void *gate, int64_t ldgate, void *up, int64_t ldup, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  sdnn_status st = check_sizes(n_rows, n_hidden, n_features, dtype);
+  if (st == SDNN_OK) st = check_activation(activation);
+  if (st != SDNN_OK || n_rows == 0) return st;
+  if ((st = check_matrix("x", x, ldx, n_features, dtype)) != SDNN_OK) return st;
+  if ((st = check_matrix("w_gate", w_gate, ldw_gate, n_features, dtype)) != SDNN_OK) return st;
+  if ((st = check_matrix("w_up", w_up, ldw_up, n_features, dtype)) != SDNN_OK) return st;
+  if ((st = check_matrix("h", h, ldh, n_hidden, dtype)) != SDNN_OK) return st;
+  if (gate && (st = check_matrix("gate", gate, ldgate, n_hidden, dtype)) != SDNN_OK) return st;
+  if (up && (st = check_matrix("up", up, ldup, n_hidden, dtype)) != SDNN_OK) return st;
+  const Sizes s{n_rows, n_hidden, n_features, dtype};
+  if ((st = check_workspace(workspace, workspace_bytes, workspace_of(s, kLayerOnly))) != SDNN_OK) return st;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const auto call = s.kind() == KIND_BF16 ? layer_call<KIND_BF16, __bf16> : s.kind() == KIND_F32 ? layer_call<KIND_F32, float> : layer_call<KIND_SPLIT, float>;
+  return call(s, x, ldx, w_gate, ldw_gate, w_up, ldw_up, activation, h, ldh, gate, ldgate, up, ldup, workspace, stream);
+}
+
+sdnn_status sdnn_gated_grad(const void *x, int64_t ldx, const void *w_gate, int64_t ldw_gate, const void *w_up, int64_t ldw_up, int32_t dtype, int32_t activation, const void *gate, int64_t ldgate,
+                            const void *up, int64_t ldup, const void *dh, int64_t lddh, int64_t n_rows, int64_t n_hidden, int64_t n_features, void *dx, int64_t lddx, void *dw_gate, int64_t lddw_gate,
+                            void *dw_up, int64_t lddw_up, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  sdnn_status st = check_sizes(n_rows, n_hidden, n_features, dtype);
+  if (st == SDNN_OK) st = check_activation(activation);
+  if (st != SDNN_OK) return st;
+  if (n_rows > 0) {
+    if ((st = check_matrix("x", x, ldx, n_features, dtype)) != SDNN_OK) return st;
+    if ((st = check_matrix("w_gate", w_gate, ldw_gate, n_features, dtype)) != SDNN_OK) return st;
+    if ((st = check_matrix("w_up", w_up, ldw_up, n_features, dtype)) != SDNN_OK) return st;
+    if ((st = check_matrix("dh", dh, lddh, n_hidden, dtype)) != SDNN_OK) return st;
+    if (!gate != !up) return fail(SDNN_EINVAL, "gate and up are kept together or not at all");
+    if (gate && (st = check_matrix("gate", gate, ldgate, n_hidden, dtype)) != SDNN_OK) return st;
+    if (up && (st = check_matrix("up", up, ldup, n_hidden, dtype)) != SDNN_OK) return st;
+    if (dx && (st = check_matrix("dx", dx, lddx, n_features, dtype)) != SDNN_OK) return st;
+  }
+  if (dw_gate && (st = check_matrix("dw_gate", dw_gate, lddw_gate, n_features, dtype)) != SDNN_OK) return st;
+  if (dw_up && (st = check_matrix("dw_up", dw_up, lddw_up, n_features, dtype)) != SDNN_OK) return st;
+  if ((!dx || n_rows == 0) && !dw_gate && !dw_up) return SDNN_OK;
+  const Sizes s{n_rows, n_hidden, n_features, dtype};
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  if (n_rows == 0) {
+    for (const auto &[p, ld] : {std::pair<void *, int64_t>{dw_gate, lddw_gate}, std::pair<void *, int64_t>{dw_up, lddw_up}}) dtype == SDNN_BF16 ? zero<__bf16>(p, ld, s, stream) : zero<float>(p, ld, s, stream);
+    return launched("gated gradient");
+  }
+  if ((st = check_workspace(workspace, workspace_bytes, workspace_of(s, gate ? kFromKept : kAgain))) != SDNN_OK) return st;
+  const auto call = s.kind() == KIND_BF16 ? grad_call<KIND_BF16, __bf16> : s.kind() == KIND_F32 ? grad_call<KIND_F32, float> : grad_call<KIND_SPLIT, float>;
+  return call(s, x, ldx, w_gate, ldw_gate, w_up, ldw_up, activation, gate, ldgate, up, ldup, dh, lddh, dx, lddx, dw_gate, lddw_gate, dw_up, lddw_up, workspace, stream);
+}
+
+}  // extern "C"

@@ -59,6 +59,11 @@ struct Operand {
   const char *scales = nullptr;
   int start = 0;
   int end = 0, parts = 0;  // KIND_THREE, set by Block: the first slab that is left out, the part of each of a group's slabs
+  // An operand of two matrices (Loader's TWO). along: the block's rows are 16 of the first and 16 of the second in turn, `rows`
+  // those of each. across: `units` slabs' rows of k are the first's, `first_rows` of them there, what follows the second's;
+  // `rows` counts both with the first's padded to whole slabs.
+  const char *second = nullptr;
+  int pitch_second = 0, units = 0, first_rows = 0;
 };
 
 // Values of k that kSlabs slabs take, bytes per value of an across operand.
@@ -98,8 +103,10 @@ __device__ __forceinline__ void meet() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// Moves slab `s` of one operand to LDS. ROWS: the block's rows (along) or columns (across) of this operand.
-template <int KIND, int ROWS, bool ACROSS, int THREADS>
+// Moves slab `s` of one operand to LDS. ROWS: the block's rows (along) or columns (across) of this operand. TWO: they
+// are two matrices' (see Operand). along, a wave loads 8 rows at once, the same of every 32 in each of its rounds, and so reads one
+// of the two; across, a slab is of one.
+template <int KIND, int ROWS, bool ACROSS, int THREADS, bool TWO = false>
 struct Loader {
   static constexpr int kData = ROWS * kSlab;
   static constexpr int kRound = THREADS * 16;  // bytes that the workgroup moves at once
@@ -114,7 +121,11 @@ struct Loader {
   // chunk bits that an across row's number permutes (fp32 columns are read value by value and stay)
   static constexpr int kTurn = KIND == KIND_F32 ? 0 : (kRowBytes / 16 - 1) & 6;
 
+  static constexpr bool kTurns = TWO && !ACROSS;  // rows of two matrices in turn
+  static_assert(!kTurns || (kRowsPerRound % 32 == 0 && ROWS % 32 == 0), "a wave's rows are of one matrix in every round");
+
   uint32_t offset;  // this lane's bytes from the slab's origin
+  uint32_t offset_second;
   int chunk;        // its 16-byte chunk within the row
   int row;
 
@@ -124,8 +135,11 @@ struct Loader {
     const int c = t % (kRowBytes / 16);
     chunk = ACROSS ? c ^ ((row << 1) & kTurn) : c ^ (row & 7);
     const int from = op.start + chunk * 16;  // (start is 0 but for KIND_THREE)
-    offset = row * op.pitch + (ACROSS && KIND == KIND_THREE ? place3(from) : from);
-    if ((ACROSS && from >= op.extent) || row * kRowBytes >= kData) offset = kOut;
+    const int place = ACROSS && KIND == KIND_THREE ? place3(from) : from;
+    const bool out = (ACROSS && from >= op.extent) || row * kRowBytes >= kData;
+    const int r = kTurns ? row / 32 * 16 + row % 16 : row;
+    offset = out ? kOut : r * op.pitch + place;
+    if constexpr (TWO) offset_second = out ? kOut : r * op.pitch_second + place;
   }
 
   // A slab's loads, issued one at a time. Past the operand's k they read zeros: every slab has kRounds of them, which the
@@ -138,26 +152,37 @@ struct Loader {
   };
   __device__ __forceinline__ Slab slab(const Operand &op, int s, int lds) const {
     uint32_t off = offset;
-    int wide, rows;
+    int wide, rows, pitch = op.pitch;
     uint64_t origin = (uint64_t)op.base;
-    const int unit = s / Geometry<KIND>::kSlabs;  // of k
+    int unit = s / Geometry<KIND>::kSlabs;  // of k
+    const int within = s - unit * Geometry<KIND>::kSlabs;
+    bool second = false;
+    if constexpr (TWO) {
+      second = kTurns ? uniform(row >> 4 & 1) : unit >= op.units;
+      if (second) {
+        off = offset_second;
+        pitch = op.pitch_second;
+        origin = (uint64_t)op.second;
+      }
+    }
     if (ACROSS) {
       wide = min(op.extent, op.start + kRowBytes);
       if (KIND == KIND_THREE) wide = place3(wide - 1) + 1;
-      rows = min(op.rows - unit * kSlabRows, kSlabRows);
-      origin += (uint64_t)(uint32_t)unit * (uint32_t)(kSlabRows * op.pitch);
+      rows = min(TWO && !second ? min(op.first_rows, op.rows) - unit * kSlabRows : op.rows - unit * kSlabRows, kSlabRows);
+      if (TWO && second) unit -= op.units;
+      origin += (uint64_t)(uint32_t)unit * (uint32_t)(kSlabRows * pitch);
     } else {
       wide = min(op.extent - unit * kSlab, kSlab);
-      rows = wide > 0 ? min(op.rows, ROWS) : 0;
+      rows = wide > 0 ? min(op.rows, kTurns ? ROWS / 2 : ROWS) : 0;
       origin += (uint64_t)(uint32_t)unit * (KIND == KIND_THREE ? kGroup3 : kSlab);
       if (chunk * 16 >= wide) off = kOut;
     }
     if constexpr (KIND == KIND_THREE) {
-      origin += (op.parts >> 2 * (s - unit * 6) & 3) * kSlab;
+      origin += (op.parts >> 2 * within & 3) * kSlab;
       if (s >= op.end) rows = 0;
     }
-    const int size = max(rows, 0) * op.pitch - op.pitch + wide;
-    return {{uniform((int)origin), uniform((int)(origin >> 32)), uniform(rows > 0 ? size : 0), 0x00027000}, off, kRowsPerRound * op.pitch, lds};
+    const int size = max(rows, 0) * pitch - pitch + wide;
+    return {{uniform((int)origin), uniform((int)(origin >> 32)), uniform(rows > 0 ? size : 0), 0x00027000}, off, (kTurns ? kRowsPerRound / 2 : kRowsPerRound) * pitch, lds};
   }
   __device__ __forceinline__ void load(const Operand &op, int s, int lds) const {
     const Slab part = slab(op, s, lds);
@@ -299,12 +324,14 @@ __device__ __forceinline__ f32x4 mfma(i32x4 a, i32x4 b, f32x4 c) {
 //
 // GROUPS of WM x WN waves may share the block's outputs, each loading and taking every GROUPS-th slab, with their sums joined
 // through LDS at the end: a launch of few blocks runs through k in fewer meetings.
-template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, int STAGES, int GROUPS = 1>
+//
+// TWO_B: B's rows are two matrices' (see Operand).
+template <int KIND, int BM, int BN, int WM, int WN, bool ACROSS_A, bool ACROSS_B, int STAGES, int GROUPS = 1, bool TWO_B = false>
 struct Block {
   static constexpr int kWaves = WM * WN, kGroup = 64 * kWaves, kThreads = kGroup * GROUPS;
   static constexpr int kTM = BM / WM / 16, kTN = BN / WN / 16;
   using LoadA = Loader<KIND, BM, ACROSS_A, kGroup>;
-  using LoadB = Loader<KIND, BN, ACROSS_B, kGroup>;
+  using LoadB = Loader<KIND, BN, ACROSS_B, kGroup, TWO_B>;
   using ScaleA = ScaleLoader<BM, kGroup>;
   using ScaleB = ScaleLoader<BN, kGroup>;
   static constexpr bool kMx = KIND == KIND_MX;
@@ -357,6 +384,7 @@ struct Block {
     op.pitch = uniform(op.pitch);
     op.rows = uniform(op.rows);
     op.extent = uniform(op.extent);
+    op.pitch_second = uniform(op.pitch_second);
   }
 
   // The last slab of rows that end within a 16-byte chunk holds what follows them there: zeros take its place.

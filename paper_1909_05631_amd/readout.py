@@ -1,5 +1,5 @@
-"""The dense readout of a network's rows: softmax cross entropy with its gradient, orthogonalised updates, and products
-of microscaled 4-bit floats (ctypes binding of the calls in include/sdnn.h that need no handle). Argument marshalling only: tensors are checked, nothing is computed or
+"""The dense readout of a network's rows: softmax cross entropy with its gradient, orthogonalised updates, products
+of microscaled 4-bit floats, and a gated hidden layer under it (ctypes binding of the calls in include/sdnn.h that need no handle). Argument marshalling only: tensors are checked, nothing is computed or
 allocated here. Every tensor lives on the GPU; rows may be strided, the values within a row may not.
 `stream`: a torch stream, its handle, or None for the default stream."""
 from __future__ import annotations
@@ -204,3 +204,54 @@ def mx_linear(x, w_codes, w_scales, out, workspace, stream=None) -> None:
     po, ldo = _rows("out", out, x.shape[0], outputs, x.dtype, x)
     _call(x, "sdnn_mx_linear", px, ldx, dt, pwc, pws, x.shape[0], outputs, x.shape[1], po, ldo, *_workspace(workspace, x),
           _stream_handle(stream))
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _activation(name) -> int:
+    code = ACTIVATIONS.get(name) if isinstance(name, str) else None
+    if code is None:
+        raise ValueError(f"activation {name!r} is none of {', '.join(ACTIVATIONS)}")
+    return code
+
+
+def gated_workspace_bytes(n_rows: int, n_hidden: int, n_features: int, dtype: torch.dtype, gradient: bool = True, kept: bool = True) -> int:
+    """Bytes of workspace for `gated`, or, with `gradient`, for `gated` and `gated_gradient`; kept=False: also where that
+    gets no gate and up."""
+    return int(load_library().sdnn_gated_workspace_bytes(n_rows, n_hidden, n_features, _dtype(dtype), (1 if kept else 2) if gradient else 0))
+
+
+def _layer(x, w_gate, w_up):
+    """dtype, (rows, hidden, features) and the leading arguments of a gated layer's calls."""
+    _on_gpu("x", x)
+    dt = _dtype(x.dtype)
+    px, ldx = _rows("x", x, None, None, x.dtype)
+    n, d = x.shape
+    pg, ldg = _rows("w_gate", w_gate, None, d, x.dtype, x)
+    pu, ldu = _rows("w_up", w_up, w_gate.shape[0], d, x.dtype, x)
+    return (n, w_gate.shape[0], d), (px, ldx, pg, ldg, pu, ldu, dt)
+
+
+def _optional_rows(name: str, t, rows, cols, dtype, like) -> tuple[int | None, int]:
+    return (None, 0) if t is None else _rows(name, t, rows, cols, dtype, like)
+
+
+def gated(x, w_gate, w_up, h, workspace, activation: str = "silu", gate=None, up=None, stream=None) -> None:
+    """h (rows, hidden) = act(x w_gate^T) * (x w_up^T): x (rows, features), w_gate, w_up (hidden, features), float32 or
+    bfloat16; activation "silu", "gelu" or "relu". gate, up (or None): like h, the two products, for `gated_gradient`."""
+    act = _activation(activation)
+    (n, m, d), lead = _layer(x, w_gate, w_up)
+    _call(x, "sdnn_gated", *lead, act, n, m, d, *_rows("h", h, n, m, x.dtype, x), *_optional_rows("gate", gate, n, m, x.dtype, x),
+          *_optional_rows("up", up, n, m, x.dtype, x), *_workspace(workspace, x), _stream_handle(stream))
+
+
+def gated_gradient(x, w_gate, w_up, dh, dx, dw_gate, dw_up, workspace, activation: str = "silu", gate=None, up=None, stream=None) -> None:
+    """From the gradient dh of h: dx, dw_gate and dw_up (each may be None), written in x's type; gate and up as `gated`
+    kept them (None: computed again)."""
+    act = _activation(activation)
+    (n, m, d), lead = _layer(x, w_gate, w_up)
+    _call(x, "sdnn_gated_grad", *lead, act, *_optional_rows("gate", gate, n, m, x.dtype, x), *_optional_rows("up", up, n, m, x.dtype, x),
+          *_rows("dh", dh, n, m, x.dtype, x), n, m, d, *_optional_rows("dx", dx, n, d, x.dtype, x),
+          *_optional_rows("dw_gate", dw_gate, m, d, x.dtype, x), *_optional_rows("dw_up", dw_up, m, d, x.dtype, x),
+          *_workspace(workspace, x), _stream_handle(stream))
