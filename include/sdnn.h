@@ -333,6 +333,31 @@ sdnn_status sdnn_gated_grad(const void *x, int64_t ldx, const void *w_gate, int6
                             int64_t n_features, void *dx, int64_t lddx, void *dw_gate, int64_t lddw_gate, void *dw_up,
                             int64_t lddw_up, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Gradients clipped by their common norm. A tensor is a matrix of rows x cols values of `dtype` in device memory, `ld` values
+ * from row to row (ignored for one row). */
+typedef struct {
+  void *data;
+  void *out;    /* sdnn_clip: where the scaled values go; NULL or data: to data itself */
+  int64_t rows, cols; /* either may be 0 */
+  int64_t ld, ldo;    /* ldo: of out; where out is data, the same */
+  int32_t dtype;
+} sdnn_tensor;
+
+/* Bytes of workspace for a list of n_tensors, whatever their sizes; 0 outside [0, 4096]. */
+size_t sdnn_clip_workspace_bytes(int64_t n_tensors);
+
+/* norm (device, one fp32) = the square root of the sum of squares of all values of the tensors (a host array, read
+ * during the call). Squares and their sums are fp64. */
+sdnn_status sdnn_global_norm(const sdnn_tensor *tensors, int64_t n_tensors, float *norm, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+
+/* The norm, and every value times min(1, max_norm / norm), a factor in fp32, rounded to the tensor's type once. A norm
+ * that is NaN makes NaN of all values, an infinite one zeros, and NaN of what was infinite. Tensors that are written may
+ * not overlap each other, nor an input that is not their own; a list that writes two of them to one address is refused.
+ * max_norm >= 0. */
+sdnn_status sdnn_clip(const sdnn_tensor *tensors, int64_t n_tensors, float max_norm, float *norm, void *workspace,
+                      size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,297 @@
+// The common norm of a list of tensors, n = sqrt(sum of v^2 over all of them), and the list scaled by min(1, most / n).
+//
+// The list is cut into pieces of one size, about 2048 for all of it (8 workgroups a CU, all resident at once, so that none
+// waits for another). One launch for every 64 tensors, whose descriptions travel as its arguments, leaves each piece's sum of
+// squares and its description in the workspace; one more goes over all pieces: every workgroup sums the pieces' sums for
+// itself, in the same order, and scales its piece. Neither waits for the host, and no sum depends on the order of
+// arrival: the same list gives the same bits.
+//
+// Squares and sums are taken in 64 bits: a list's norm is exact to its rounding to fp32 whatever the values' sizes (squares of
+// 1e-45 and of 3e38 are normal numbers there), and memory still bounds the pass.
+#include "dense.h"
+
+using namespace dense;
+
+namespace {
+
+constexpr int kMaxTensors = 4096, kBatch = 64, kPieces = 2048;
+constexpr int64_t kLeastPiece = 8192, kUnit = 4096;  // bytes
+constexpr int64_t kSegment = 4096;                   // bytes of a strided row that a workgroup takes by itself
+
+// A run of values [start, start + count) of a matrix of `cols` columns; contiguous ones have one row.
+struct Piece {
+  const void *in;
+  void *out;
+  int64_t start, count, cols, ld, ldo;
+  int dtype, contiguous;
+};
+
+// Tensors of one launch, and the first of each one's pieces there.
+struct Tensor {
+  const void *in;
+  void *out;
+  int64_t rows, cols, ld, ldo;
+  int first, dtype;
+};
+struct Batch {
+  Tensor of[kBatch];
+  int count, first;  // of the launch's pieces
+  int64_t bytes;     // of a piece
+};
+
+template <class T>
+using Chunk = T __attribute__((ext_vector_type(16 / sizeof(T))));
+
+// f(values) for 16 bytes of a contiguous run at a time, and for single values at its ends.
+template <class T, class F, class G>
+__device__ __forceinline__ void over_run(const T *p, int64_t n, const F &chunk, const G &single) {
+  constexpr int N = 16 / sizeof(T);
+  int64_t head = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / (int)sizeof(T);
+  if (head > n) head = n;
+  if (threadIdx.x < head) single(threadIdx.x);
+  const int64_t chunks = (n - head) / N;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < chunks; i += 256) chunk(head + i * N);
+  const int64_t tail = head + chunks * N;
+  if (threadIdx.x < n - tail) single(tail + threadIdx.x);
+}
+
+template <class T>
+__device__ __forceinline__ double squares_of(const Piece &p) {
+  double sum = 0.0;
+  const auto add = [&](float v) { sum = fma((double)v, (double)v, sum); };
+  const auto run = [&](const T *from, int64_t n) {
+    over_run(from, n, [&](int64_t i) {
+      const Chunk<T> v = *(const Chunk<T> *)(from + i);
+#pragma unroll
+      for (int e = 0; e < 16 / (int)sizeof(T); ++e) add((float)v[e]);
+    }, [&](int64_t i) { add((float)from[i]); });
+  };
+  if (p.contiguous) {
+    run((const T *)p.in + p.start, p.count);
+  } else if (p.cols * (int64_t)sizeof(T) >= kSegment) {
+    for (int64_t at = p.start, end = p.start + p.count; at < end;) {
+      const int64_t r = at / p.cols, c = at - r * p.cols, n = min(p.cols - c, end - at);
+      run((const T *)p.in + r * p.ld + c, n);
+      at += n;
+    }
+  } else {
+    for (int64_t i = threadIdx.x; i < p.count; i += 256) {
+      const int64_t r = (p.start + i) / p.cols, c = p.start + i - r * p.cols;
+      add((float)((const T *)p.in)[r * p.ld + c]);
+    }
+  }
+  return sum;
+}
+
+// Sum over a workgroup of 256, in every thread.
+__device__ __forceinline__ double sum_of_workgroup(double v) {
+  __shared__ double part[4];
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+__global__ __launch_bounds__(256) void k_squares(const Batch batch, Piece *pieces, double *sums) {
+  const int lane = threadIdx.x & 63, b = blockIdx.x;
+  // the last tensor whose pieces begin at or before this one
+  const uint64_t before = __ballot(lane < batch.count && batch.of[lane < batch.count ? lane : 0].first <= b);
+  const Tensor &t = batch.of[__popcll(before) - 1];
+  const int64_t per = batch.bytes / (t.dtype == SDNN_BF16 ? 2 : 4), start = (b - t.first) * per, all = t.rows * t.cols;
+  const Piece p{t.in, t.out, start, min(per, all - start), t.cols, t.ld, t.ldo, t.dtype, t.rows == 1 || (t.ld == t.cols && t.ldo == t.cols)};
+  const double sum = sum_of_workgroup(t.dtype == SDNN_BF16 ? squares_of<__bf16>(p) : squares_of<float>(p));
+  if (threadIdx.x == 0) {
+    pieces[batch.first + b] = p;
+    sums[batch.first + b] = sum;
+  }
+}
+
+__device__ __forceinline__ double norm_of(const double *sums, int count) {
+  double v = 0.0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < count; i += 256) v += sums[i];
+  return sqrt(sum_of_workgroup(v));
+}
+
+__global__ __launch_bounds__(256) void k_norm(const double *sums, int count, float *norm) {
+  const double n = norm_of(sums, count);
+  if (threadIdx.x == 0) *norm = (float)n;
+}
+
+template <class T>
+__device__ __forceinline__ void scale_piece(const Piece &p, float by) {
+  const auto run = [&](const T *from, T *to, int64_t n) {
+    if ((((uintptr_t)from ^ (uintptr_t)to) & 15) == 0) {
+      over_run(from, n, [&](int64_t i) {
+        Chunk<T> v = *(const Chunk<T> *)(from + i);
+#pragma unroll
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) v[e] = (T)((float)v[e] * by);
+        *(Chunk<T> *)(to + i) = v;
+      }, [&](int64_t i) { to[i] = (T)((float)from[i] * by); });
+    } else {
+#pragma unroll 4
+      for (int64_t i = threadIdx.x; i < n; i += 256) to[i] = (T)((float)from[i] * by);
+    }
+  };
+  if (p.contiguous) {
+    run((const T *)p.in + p.start, (T *)p.out + p.start, p.count);
+  } else if (p.cols * (int64_t)sizeof(T) >= kSegment) {
+    for (int64_t at = p.start, end = p.start + p.count; at < end;) {
+      const int64_t r = at / p.cols, c = at - r * p.cols, n = min(p.cols - c, end - at);
+      run((const T *)p.in + r * p.ld + c, (T *)p.out + r * p.ldo + c, n);
+      at += n;
+    }
+  } else {
+    for (int64_t i = threadIdx.x; i < p.count; i += 256) {
+      const int64_t r = (p.start + i) / p.cols, c = p.start + i - r * p.cols;
+      ((T *)p.out)[r * p.ldo + c] = (T)((float)((const T *)p.in)[r * p.ld + c] * by);
+    }
+  }
+}
+
+// A norm past `most`, or one that is NaN, scales; an infinite one leaves zeros (and NaN of what was infinite).
+__global__ __launch_bounds__(256) void k_clip(const Piece *pieces, const double *sums, int count, float most, float *norm) {
+  const double n = norm_of(sums, count);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
+  const float by = n <= (double)most ? 1.0f : (float)((double)most / n);
+  const Piece p = pieces[blockIdx.x];
+  if (by == 1.0f && p.in == p.out) return;
+  if (p.dtype == SDNN_BF16)
+    scale_piece<__bf16>(p, by);
+  else
+    scale_piece<float>(p, by);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Host
+
+struct Space {
+  Piece *pieces;
+  double *sums;
+  Space(Carver &c, int64_t n) {
+    pieces = c.take<Piece>((size_t)(kPieces + n));
+    sums = c.take<double>((size_t)(kPieces + n));
+  }
+};
+
+// Two tensors that are written to one place would be scaled twice; which of the two results stayed would be chance.
+bool all_apart(const sdnn_tensor *tensors, int n, bool clip, int *first, int *second) {
+  constexpr int kSlots = 2 * kMaxTensors;
+  uint16_t slot[kSlots];  // index + 1
+  int mask = 16;
+  while (mask < 2 * n) mask *= 2;
+  for (int i = 0; i < mask; ++i) slot[i] = 0;
+  --mask;
+  for (int i = 0; i < n; ++i) {
+    if (!clip || tensors[i].rows == 0 || tensors[i].cols == 0) continue;
+    const void *to = tensors[i].out ? tensors[i].out : tensors[i].data;
+    uint64_t at = ((uint64_t)(uintptr_t)to >> 1) * 0x9e3779b97f4a7c15ull >> 40;
+    for (;; ++at) {
+      const int j = slot[at & mask];
+      if (j == 0) break;
+      const void *other = tensors[j - 1].out ? tensors[j - 1].out : tensors[j - 1].data;
+      if (other == to) {
+        *first = j - 1;
+        *second = i;
+        return false;
+      }
+    }
+    slot[at & mask] = (uint16_t)(i + 1);
+  }
+  return true;
+}
+
+sdnn_status check_list(const sdnn_tensor *tensors, int64_t n, bool clip) {
+  if (n < 0 || n > kMaxTensors) return fail(SDNN_EINVAL, "n_tensors %lld is outside [0, %d]", (long long)n, kMaxTensors);
+  if (n && !tensors) return fail(SDNN_EINVAL, "tensors is null");
+  for (int64_t i = 0; i < n; ++i) {
+    const sdnn_tensor &t = tensors[i];
+    if (!good_dtype(t.dtype)) return fail(SDNN_EINVAL, "tensor %lld: dtype %d is neither SDNN_FP32 nor SDNN_BF16", (long long)i, t.dtype);
+    if (t.rows < 0 || t.cols < 0 || t.rows > 1ll << 40 || t.cols > 1ll << 40 || (t.cols && t.rows > (1ll << 40) / t.cols))
+      return fail(SDNN_EINVAL, "tensor %lld: %lld x %lld values are outside [0, 2^40]", (long long)i, (long long)t.rows, (long long)t.cols);
+    if (t.rows == 0 || t.cols == 0) continue;
+    if (!t.data || (uintptr_t)t.data % dtype_bytes(t.dtype)) return fail(SDNN_EINVAL, "tensor %lld: data is null or not aligned to its values", (long long)i);
+    if (t.rows > 1 && (t.ld < t.cols || t.ld > 1ll << 40)) return fail(SDNN_EINVAL, "tensor %lld: the row stride %lld is outside [%lld, 2^40]", (long long)i, (long long)t.ld, (long long)t.cols);
+    if (!clip) continue;
+    if ((uintptr_t)t.out % dtype_bytes(t.dtype)) return fail(SDNN_EINVAL, "tensor %lld: out is not aligned to its values", (long long)i);
+    if (t.out && t.rows > 1 && (t.ldo < t.cols || t.ldo > 1ll << 40)) return fail(SDNN_EINVAL, "tensor %lld: the row stride of out, %lld, is outside [%lld, 2^40]", (long long)i, (long long)t.ldo, (long long)t.cols);
+    if (t.out == t.data && t.rows > 1 && t.ldo != t.ld) return fail(SDNN_EINVAL, "tensor %lld: out is data with another row stride", (long long)i);
+  }
+  int a, b;
+  if (!all_apart(tensors, (int)n, clip, &a, &b)) return fail(SDNN_EINVAL, "tensors %d and %d are written to the same place", a, b);
+  return SDNN_OK;
+}
+
+// The pieces' sums and descriptions; `total` of them.
+sdnn_status squares(const sdnn_tensor *tensors, int64_t n, const Space &sp, int *total, hipStream_t stream) {
+  int64_t bytes = 0;
+  for (int64_t i = 0; i < n; ++i) bytes += tensors[i].rows * tensors[i].cols * dtype_bytes(tensors[i].dtype);
+  Batch batch;
+  batch.bytes = std::max(kLeastPiece, ceil_div(ceil_div(bytes, kPieces), kUnit) * kUnit);
+  batch.count = 0;
+  batch.first = 0;
+  int here = 0;  // pieces of this launch
+  for (int64_t i = 0; i < n; ++i) {
+    const sdnn_tensor &t = tensors[i];
+    const int64_t size = t.rows * t.cols * dtype_bytes(t.dtype);
+    if (size > 0) {
+      const bool flat = t.rows == 1 || (t.ld == t.cols && (!t.out || t.ldo == t.cols));
+      batch.of[batch.count++] = {t.data, t.out ? t.out : t.data, flat ? 1 : t.rows, flat ? t.rows * t.cols : t.cols, t.ld, t.out ? t.ldo : t.ld, here, t.dtype};
+      here += (int)ceil_div(size, batch.bytes);
+    }
+    if (batch.count == kBatch || (i == n - 1 && batch.count > 0)) {
+      hipLaunchKernelGGL(k_squares, dim3((unsigned)here), dim3(256), 0, stream, batch, sp.pieces, sp.sums);
+      const sdnn_status st = launched("squares");
+      if (st != SDNN_OK) return st;
+      batch.first += here;
+      batch.count = here = 0;
+    }
+  }
+  *total = batch.first;
+  return SDNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdnn_clip_workspace_bytes(int64_t n_tensors) {
+  if (n_tensors < 0 || n_tensors > kMaxTensors) return 0;
+  Carver c{nullptr};
+  Space s(c, n_tensors);
+  return c.used;
+}
+
+sdnn_status sdnn_global_norm(const sdnn_tensor *tensors, int64_t n_tensors, float *norm, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  sdnn_status st = check_list(tensors, n_tensors, false);
+  if (st != SDNN_OK) return st;
+  if (!norm || (uintptr_t)norm % 4) return fail(SDNN_EINVAL, "norm is null or not aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, sdnn_clip_workspace_bytes(n_tensors))) != SDNN_OK) return st;
+  Carver c{(char *)workspace};
+  const Space sp(c, n_tensors);
+  int total;
+  if ((st = squares(tensors, n_tensors, sp, &total, (hipStream_t)hip_stream)) != SDNN_OK) return st;
+  hipLaunchKernelGGL(k_norm, dim3(1), dim3(256), 0, (hipStream_t)hip_stream, sp.sums, total, norm);
+  return launched("norm");
+}
+
+sdnn_status sdnn_clip(const sdnn_tensor *tensors, int64_t n_tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  sdnn_status st = check_list(tensors, n_tensors, true);
+  if (st != SDNN_OK) return st;
+  if (!(max_norm >= 0.0f)) return fail(SDNN_EINVAL, "max_norm %g is not at least 0", max_norm);
+  if (!norm || (uintptr_t)norm % 4) return fail(SDNN_EINVAL, "norm is null or not aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, sdnn_clip_workspace_bytes(n_tensors))) != SDNN_OK) return st;
+  Carver c{(char *)workspace};
+  const Space sp(c, n_tensors);
+  int total;
+  if ((st = squares(tensors, n_tensors, sp, &total, (hipStream_t)hip_stream)) != SDNN_OK) return st;
+  if (total > 0)
+    hipLaunchKernelGGL(k_clip, dim3((unsigned)total), dim3(256), 0, (hipStream_t)hip_stream, sp.pieces, sp.sums, total, max_norm, norm);
+  else
+    hipLaunchKernelGGL(k_norm, dim3(1), dim3(256), 0, (hipStream_t)hip_stream, sp.sums, 0, norm);
+  return launched("clip");
+}
+
+}  // extern "C"

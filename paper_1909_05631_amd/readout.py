@@ -1,11 +1,13 @@
 """The dense readout of a network's rows: softmax cross entropy with its gradient, orthogonalised updates, products
-of microscaled 4-bit floats, and a gated hidden layer under it (ctypes binding of the calls in include/sdnn.h that need no handle). Argument marshalling only: tensors are checked, nothing is computed or
+of microscaled 4-bit floats, a gated hidden layer under it, and gradients clipped by their norm (ctypes binding of the calls in include/sdnn.h that need no handle). Argument marshalling only: tensors are checked, nothing is computed or
 allocated here. Every tensor lives on the GPU; rows may be strided, the values within a row may not.
 `stream`: a torch stream, its handle, or None for the default stream."""
 from __future__ import annotations
 
 import ctypes
+from operator import attrgetter
 
+import numpy as np
 import torch
 
 from .sdnn import SdnnError, _check, _stream_handle, load_library  # noqa: F401
@@ -255,3 +257,72 @@ def gated_gradient(x, w_gate, w_up, dh, dx, dw_gate, dw_up, workspace, activatio
           *_rows("dh", dh, n, m, x.dtype, x), n, m, d, *_optional_rows("dx", dx, n, d, x.dtype, x),
           *_optional_rows("dw_gate", dw_gate, m, d, x.dtype, x), *_optional_rows("dw_up", dw_up, m, d, x.dtype, x),
           *_workspace(workspace, x), _stream_handle(stream))
+
+
+def clip_workspace_bytes(n_tensors: int) -> int:
+    """Bytes of workspace for `global_norm` and `clip` of so many tensors, whatever their sizes."""
+    return int(load_library().sdnn_clip_workspace_bytes(n_tensors))
+
+
+def _extent(name: str, t) -> tuple[int, int, int]:
+    """Rows, columns and row stride of a tensor that is contiguous or a matrix of contiguous rows."""
+    if t.is_contiguous():
+        return 1, t.numel(), 0
+    if t.dim() != 2:
+        raise ValueError(f"{name} is neither contiguous nor a matrix of contiguous rows")
+    return *t.shape, _rows(name, t, None, None, t.dtype)[1]
+
+
+def _list(tensors, out, norm):
+    """The C ABI's description of a list of tensors (sdnn_tensor, seven words each) and its length. A list may hold
+    hundreds: what is asked of all of them is asked by map."""
+    _on_gpu("norm", norm)
+    tensors = list(tensors)
+    to = tensors if out is None else list(out)
+    if len(to) != len(tensors):
+        raise ValueError(f"out holds {len(to)} tensors, not {len(tensors)}")
+    for name, ts in (("tensors", tensors), ("out", to)):
+        for i, t in enumerate(ts):
+            if not isinstance(t, torch.Tensor):
+                raise ValueError(f"{name}[{i}] is no tensor")
+        if set(map(torch.Tensor.get_device, ts)) - {norm.get_device()}:
+            raise ValueError(f"not all of {name} are on the GPU of norm, {norm.device}")
+        if ts is to and ts is tensors:
+            break
+    dtypes = list(map(attrgetter("dtype"), tensors))
+    codes = [_dtype(d) for d in dtypes]
+    if to is not tensors:
+        for i, (a, b, d, e) in enumerate(zip(map(torch.Tensor.size, tensors), map(torch.Tensor.size, to), dtypes, map(attrgetter("dtype"), to))):
+            if a != b or d != e:
+                raise ValueError(f"out[{i}] is {tuple(b)} of {e}, not {tuple(a)} of {d}")
+    table = np.zeros((len(tensors), 7), np.int64)
+    table[:, 0] = list(map(torch.Tensor.data_ptr, tensors))
+    table[:, 1] = table[:, 0] if to is tensors else list(map(torch.Tensor.data_ptr, to))
+    table[:, 6] = codes
+    if all(map(torch.Tensor.is_contiguous, tensors)) and (to is tensors or all(map(torch.Tensor.is_contiguous, to))):
+        table[:, 2] = 1
+        table[:, 3] = list(map(torch.Tensor.numel, tensors))
+    else:
+        for i, (a, b) in enumerate(zip(tensors, to)):
+            (rows, cols, ld), (rows_out, cols_out, ldo) = _extent(f"tensors[{i}]", a), _extent(f"out[{i}]", b)
+            if rows != rows_out or cols != cols_out:  # one of them is contiguous, the other a matrix of rows
+                rows, cols = a.shape
+                ld, ldo = ld or cols, ldo or cols
+            table[i, 2:6] = rows, cols, ld, ldo
+    return table, len(tensors)
+
+
+def global_norm(tensors, norm, workspace, stream=None) -> None:
+    """norm (1 value, float32) = the square root of the sum of squares of all values of the tensors, float32 or
+    bfloat16, each contiguous or a matrix of contiguous rows."""
+    table, n = _list(tensors, None, norm)
+    _call(norm, "sdnn_global_norm", table.ctypes.data, n, _vector("norm", norm, 1, torch.float32, norm), *_workspace(workspace, norm),
+          _stream_handle(stream))
+
+
+def clip(tensors, max_norm: float, norm, workspace, out=None, stream=None) -> None:
+    """The norm, as `global_norm` has it, and every value times min(1, max_norm / norm), into the tensors of `out` (same shapes
+    and types; None: the tensors themselves)."""
+    table, n = _list(tensors, out, norm)
+    _call(norm, "sdnn_clip", table.ctypes.data, n, max_norm, _vector("norm", norm, 1, torch.float32, norm), *_workspace(workspace, norm),
+          _stream_handle(stream))

@@ -22,6 +22,7 @@ EXPORTED_SYMBOLS = [
     "sdnn_mx_blocks", "sdnn_mx_quantize", "sdnn_mx_dequantize", "sdnn_mx_product", "sdnn_mx_linear_workspace_bytes",
     "sdnn_mx_linear",
     "sdnn_gated_workspace_bytes", "sdnn_gated", "sdnn_gated_grad",
+    "sdnn_clip_workspace_bytes", "sdnn_global_norm", "sdnn_clip",
 ]
 # kernel families of sdnn_layer_info by a kernel of each (Net.layer_kernels names the kernel itself)
 KERNEL_KINDS = {0: "none", 1: "k_layer_lds", 2: "k_layer_gfm", 3: "k_layer_gfm_u8", 4: "k_layer_gfm_small",
@@ -88,12 +89,16 @@ def load_library():
         L.sdnn_gated.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
         L.sdnn_gated_grad.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp, i64, vp, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64,
                                       vp, sz, vp]
+        L.sdnn_clip_workspace_bytes.argtypes = [i64]
+        L.sdnn_clip_workspace_bytes.restype = sz
+        L.sdnn_global_norm.argtypes = [vp, i64, vp, vp, sz, vp]
+        L.sdnn_clip.argtypes = [vp, i64, ctypes.c_float, vp, vp, sz, vp]
         for name in ("sdnn_create", "sdnn_load_layers", "sdnn_infer", "sdnn_categories", "sdnn_live_counts",
                      "sdnn_final_rows", "sdnn_set_profiling", "sdnn_layer_times", "sdnn_layer_info",
                      "sdnn_enable_equal_value_kernels", "sdnn_infer_static", "sdnn_layer_kernel",
                      "sdnn_readout_loss", "sdnn_readout_grad", "sdnn_orthogonalize", "sdnn_mx_quantize",
                      "sdnn_mx_dequantize", "sdnn_mx_product", "sdnn_mx_linear",
-                     "sdnn_gated", "sdnn_gated_grad"):
+                     "sdnn_gated", "sdnn_gated_grad", "sdnn_global_norm", "sdnn_clip"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
