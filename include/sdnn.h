@@ -358,6 +358,36 @@ sdnn_status sdnn_global_norm(const sdnn_tensor *tensors, int64_t n_tensors, floa
 sdnn_status sdnn_clip(const sdnn_tensor *tensors, int64_t n_tensors, float max_norm, float *norm, void *workspace,
                       size_t workspace_bytes, void *hip_stream);
 
+/* Weights of 4 bits with a scale for each group of 32, 64 or 128 values of a row: w = scale * (code - 8), or, with offsets,
+ * scale * code + offset, code in [0, 15]. A matrix of n_rows rows of n_values values is
+ *   codes:   n_rows x groups * group / 2 bytes, 16-byte aligned, groups = sdnn_grouped_groups(n_values, group) (0 for
+ *            n_values outside [1, 2^20] and other groups); a byte holds values 2i (low half) and 2i + 1;
+ *   scales, offsets: n_rows x groups of `dtype`; offsets may be NULL.
+ * Codes past n_values may be anything. `dtype` is also that of the rows that they are multiplied with. */
+int64_t sdnn_grouped_groups(int64_t n_values, int32_t group);
+
+/* Quantise w (n_rows x n_values, row stride ldw). Without offsets a group's scale is its largest magnitude over 7; with
+ * them (max - min) / 15, and the offset is the minimum. Both are rounded to `dtype`, then codes to the nearest value that
+ * they can stand for, ties to the even code. A group with an infinity or a NaN stands for NaN. */
+sdnn_status sdnn_grouped_quantize(const void *w, int64_t ldw, int32_t dtype, int64_t n_rows, int64_t n_values,
+                                  int32_t group, uint8_t *codes, void *scales, void *offsets, void *hip_stream);
+
+/* The values that they stand for, one fp32 product and sum each, rounded to `dtype`, in out (n_rows x n_values, row stride
+ * ldo). */
+sdnn_status sdnn_grouped_dequantize(const uint8_t *codes, const void *scales, const void *offsets, int32_t dtype,
+                                    int64_t n_rows, int64_t n_values, int32_t group, void *out, int64_t ldo,
+                                    void *hip_stream);
+
+/* out (n_rows x n_outputs, row stride ldo) = x w^T for rows x (n_rows x n_values, row stride ldx) and n_outputs rows of codes.
+ * Up to 64 rows, scales and offsets are multiplied with fp32 sums over their groups, of exact products. For more rows w
+ * is rounded to `dtype` first, as sdnn_grouped_dequantize has it, and multiplied with x: exact products for bf16, fp32
+ * values as they are or as two fp16 parts (22 bits or more of each value down to 2^-17 of its row's largest). Sums are
+ * fp32, rounded to `dtype` once. */
+size_t sdnn_grouped_linear_workspace_bytes(int64_t n_rows, int64_t n_outputs, int64_t n_values, int32_t dtype);
+sdnn_status sdnn_grouped_linear(const void *x, int64_t ldx, int32_t dtype, const uint8_t *codes, const void *scales,
+                                const void *offsets, int64_t n_rows, int64_t n_outputs, int64_t n_values, int32_t group,
+                                void *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,5 +1,6 @@
 """The dense readout of a network's rows: softmax cross entropy with its gradient, orthogonalised updates, products
-of microscaled 4-bit floats, a gated hidden layer under it, and gradients clipped by their norm (ctypes binding of the calls in include/sdnn.h that need no handle). Argument marshalling only: tensors are checked, nothing is computed or
+of microscaled 4-bit floats, a gated hidden layer under it, gradients clipped by their norm, and weights of 4 bits with a
+scale a group (ctypes binding of the calls in include/sdnn.h that need no handle). Argument marshalling only: tensors are checked, nothing is computed or
 allocated here. Every tensor lives on the GPU; rows may be strided, the values within a row may not.
 `stream`: a torch stream, its handle, or None for the default stream."""
 from __future__ import annotations
@@ -326,3 +327,64 @@ def clip(tensors, max_norm: float, norm, workspace, out=None, stream=None) -> No
     table, n = _list(tensors, out, norm)
     _call(norm, "sdnn_clip", table.ctypes.data, n, max_norm, _vector("norm", norm, 1, torch.float32, norm), *_workspace(workspace, norm),
           _stream_handle(stream))
+
+
+GROUPS = (32, 64, 128)
+
+
+def grouped_groups(n_values: int, group: int = 128) -> int:
+    """Groups of a row of n_values weights: group / 2 bytes of codes and one scale each (sdnn_grouped_groups)."""
+    return -(-n_values // group) if 1 <= n_values <= 1 << 20 and group in GROUPS else 0
+
+
+def _grouped(codes, scales, offsets, n_values: int, group: int, dtype, like) -> tuple[int, int, int | None, int]:
+    """Addresses of codes, scales and offsets, and their rows."""
+    if group not in GROUPS:
+        raise ValueError(f"group {group!r} is none of {', '.join(map(str, GROUPS))}")
+    _on_gpu("codes", codes, like)
+    n = grouped_groups(n_values, group)
+    named = (("codes", codes, torch.uint8, n * group // 2), ("scales", scales, dtype, n), ("offsets", offsets, dtype, n))
+    for name, t, kind, cols in named:
+        if t is None and name == "offsets":
+            continue
+        _on_gpu(name, t, like)
+        if t.dtype != kind or not t.is_contiguous() or t.dim() != 2 or t.shape[0] != codes.shape[0] or t.shape[1] != cols:
+            raise ValueError(f"{name}, {tuple(t.shape)} of {t.dtype}, do not hold contiguous rows of {n_values} values in groups of {group}: ({codes.shape[0] if codes.dim() else 0}, {cols}) of {kind}")
+    return codes.data_ptr(), scales.data_ptr(), None if offsets is None else offsets.data_ptr(), codes.shape[0]
+
+
+def grouped_quantize(w, codes, scales, group: int = 128, offsets=None, stream=None) -> None:
+    """codes (rows, group / 2 * n), bytes, and scales (rows, n), in w's type, of w (rows, values), n = grouped_groups(values,
+    group): w = scale * (code - 8), or with offsets (rows, n) scale * code + offset."""
+    _on_gpu("w", w)
+    dt = _dtype(w.dtype)
+    pw, ldw = _rows("w", w, None, None, w.dtype)
+    pc, ps, po, rows = _grouped(codes, scales, offsets, w.shape[1], group, w.dtype, w)
+    if rows != w.shape[0]:
+        raise ValueError(f"{rows} rows of codes for {w.shape[0]} rows of w")
+    _call(w, "sdnn_grouped_quantize", pw, ldw, dt, rows, w.shape[1], group, pc, ps, po, _stream_handle(stream))
+
+
+def grouped_dequantize(codes, scales, out, group: int = 128, offsets=None, stream=None) -> None:
+    """out (rows, values) = the weights that the codes stand for, in the scales' type."""
+    _on_gpu("out", out)
+    dt = _dtype(out.dtype)
+    po, ldo = _rows("out", out, None, None, out.dtype)
+    pc, ps, pf, rows = _grouped(codes, scales, offsets, out.shape[1], group, out.dtype, out)
+    if rows != out.shape[0]:
+        raise ValueError(f"{rows} rows of codes for {out.shape[0]} rows of out")
+    _call(out, "sdnn_grouped_dequantize", pc, ps, pf, dt, rows, out.shape[1], group, po, ldo, _stream_handle(stream))
+
+
+def grouped_linear_workspace_bytes(n_rows: int, n_outputs: int, n_values: int, dtype: torch.dtype) -> int:
+    return int(load_library().sdnn_grouped_linear_workspace_bytes(n_rows, n_outputs, n_values, _dtype(dtype)))
+
+
+def grouped_linear(x, codes, scales, out, workspace, group: int = 128, offsets=None, stream=None) -> None:
+    """out (rows, outputs) = x w^T, x (rows, values), of weights held in 4 bits; scales, offsets and out have x's type."""
+    _on_gpu("x", x)
+    dt = _dtype(x.dtype)
+    px, ldx = _rows("x", x, None, None, x.dtype)
+    pc, ps, pf, outputs = _grouped(codes, scales, offsets, x.shape[1], group, x.dtype, x)
+    po, ldo = _rows("out", out, x.shape[0], outputs, x.dtype, x)
+    _call(x, "sdnn_grouped_linear", px, ldx, dt, pc, ps, pf, x.shape[0], outputs, x.shape[1], group, po, ldo, *_workspace(workspace, x), _stream_handle(stream))

@@ -23,6 +23,7 @@ EXPORTED_SYMBOLS = [
     "sdnn_mx_linear",
     "sdnn_gated_workspace_bytes", "sdnn_gated", "sdnn_gated_grad",
     "sdnn_clip_workspace_bytes", "sdnn_global_norm", "sdnn_clip",
+    "sdnn_grouped_groups", "sdnn_grouped_quantize", "sdnn_grouped_dequantize", "sdnn_grouped_linear_workspace_bytes", "sdnn_grouped_linear",
 ]
 # kernel families of sdnn_layer_info by a kernel of each (Net.layer_kernels names the kernel itself)
 KERNEL_KINDS = {0: "none", 1: "k_layer_lds", 2: "k_layer_gfm", 3: "k_layer_gfm_u8", 4: "k_layer_gfm_small",
@@ -93,12 +94,20 @@ def load_library():
         L.sdnn_clip_workspace_bytes.restype = sz
         L.sdnn_global_norm.argtypes = [vp, i64, vp, vp, sz, vp]
         L.sdnn_clip.argtypes = [vp, i64, ctypes.c_float, vp, vp, sz, vp]
+        L.sdnn_grouped_groups.argtypes = [i64, i32]
+        L.sdnn_grouped_groups.restype = i64
+        L.sdnn_grouped_quantize.argtypes = [vp, i64, i32, i64, i64, i32, vp, vp, vp, vp]
+        L.sdnn_grouped_dequantize.argtypes = [vp, vp, vp, i32, i64, i64, i32, vp, i64, vp]
+        L.sdnn_grouped_linear_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.sdnn_grouped_linear_workspace_bytes.restype = sz
+        L.sdnn_grouped_linear.argtypes = [vp, i64, i32, vp, vp, vp, i64, i64, i64, i32, vp, i64, vp, sz, vp]
         for name in ("sdnn_create", "sdnn_load_layers", "sdnn_infer", "sdnn_categories", "sdnn_live_counts",
                      "sdnn_final_rows", "sdnn_set_profiling", "sdnn_layer_times", "sdnn_layer_info",
                      "sdnn_enable_equal_value_kernels", "sdnn_infer_static", "sdnn_layer_kernel",
                      "sdnn_readout_loss", "sdnn_readout_grad", "sdnn_orthogonalize", "sdnn_mx_quantize",
                      "sdnn_mx_dequantize", "sdnn_mx_product", "sdnn_mx_linear",
-                     "sdnn_gated", "sdnn_gated_grad", "sdnn_global_norm", "sdnn_clip"):
+                     "sdnn_gated", "sdnn_gated_grad", "sdnn_global_norm", "sdnn_clip",
+                     "sdnn_grouped_quantize", "sdnn_grouped_dequantize", "sdnn_grouped_linear"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
