@@ -25,8 +25,10 @@ using tile::KIND_SPLIT;
 
 namespace {
 
-constexpr int64_t kFewRows = 64;               // rows that go to k_few, 16 at a time
-constexpr int64_t kPieceValues = 1 << 28;      // weights that are written as values at a time
+constexpr int64_t kFewRows = 64;               // rows that go to k_few
+// Weights that are written as values at a time. Fewer (2^26 bf16 values would stay in the Infinity Cache) leave the products too
+// few blocks: 64 rows to 16384 x 16384 360 us so, 336 at once, 2000 rows 1300 us and 1140.
+constexpr int64_t kPieceValues = 1 << 28;
 constexpr int64_t kPlain = 192;                // fp32 rows or outputs for the plain fp32 products
 
 __host__ __device__ inline int64_t groups_of(int64_t n, int group) { return ceil_div(n, group); }
@@ -90,206 +92,427 @@ __global__ __launch_bounds__(256) void k_quantize(const T *w, int64_t ld, int64_
   }
 }
 
-// Eight values a lane: one product and sum in fp32, rounded to the output's type. Zeros past n, where the output has room.
+// Eight values a lane of four rows: one product and sum in fp32, rounded to the output's type. Zeros past n, where the output
+// has room. `shift`: a group is 2^shift values.
 template <class T>
-__global__ __launch_bounds__(256) void k_dequantize(const uint8_t *codes, const T *scales, const T *offsets, int group, int64_t rows, int64_t n, T *out, int64_t ld, int64_t wide, bool vec) {
-  const int64_t groups = groups_of(n, group), pitch = pitch_of(n, group);
-  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
-    for (int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; c < wide; c += (int64_t)gridDim.x * 2048) {
-      const uint32_t word = c < n ? *(const uint32_t *)(codes + r * pitch + c / 2) : 0;
-      const int64_t g = r * groups + (c < n ? c / group : 0);
-      const float scale = (float)scales[g], offset = offsets ? (float)offsets[g] : 0.0f, from = offsets ? 0.0f : 8.0f;
-      f32x4 v[2];
+__global__ __launch_bounds__(256) void k_dequantize(const uint8_t *codes, const T *scales, const T *offsets, int shift, int64_t rows, int n, T *out, int64_t ld, int wide, bool vec) {
+  constexpr int kRows = 4;  // whose loads are on their way together
+  const int64_t groups = groups_of(n, 1 << shift), pitch = pitch_of(n, 1 << shift);
+  const float from = offsets ? 0.0f : 8.0f;
+  for (int64_t r0 = (int64_t)blockIdx.y * kRows; r0 < rows; r0 += (int64_t)gridDim.y * kRows)
+    for (int c = (blockIdx.x * 256 + threadIdx.x) * 8; c < wide; c += gridDim.x * 2048) {
+      const int at = c < n ? c : 0;
+      uint32_t word[kRows];
+      float scale[kRows], offset[kRows];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = c + i < n ? fmaf((float)(word >> 4 * i & 15) - from, scale, offset) : 0.0f;
+      for (int i = 0; i < kRows; ++i) {
+        const int64_t r = min(r0 + i, rows - 1), g = r * groups + (at >> shift);
+        word[i] = *(const uint32_t *)(codes + r * pitch + at / 2);
+        scale[i] = (float)scales[g];
+        offset[i] = offsets ? (float)offsets[g] : 0.0f;
+      }
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (c + 4 * h < wide) store4(out + r * ld + c + 4 * h, v[h], (int)min(wide - c - 4 * h, (int64_t)4), vec);
+      for (int i = 0; i < kRows; ++i) {
+        if (r0 + i >= rows) break;
+        f32x4 v[2];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e / 4][e % 4] = c + e < n ? fmaf((float)(word[i] >> 4 * e & 15) - from, scale[i], offset[i]) : 0.0f;
+        T *to = out + (r0 + i) * ld + c;
+        typedef T Eight __attribute__((ext_vector_type(8)));
+        if (vec && c + 8 <= wide) {
+          Eight o;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = (T)v[e / 4][e % 4];
+          *(Eight *)to = o;
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (c + 4 * h < wide) store4(to + 4 * h, v[h], min(wide - c - 4 * h, 4), vec);
+        }
+      }
     }
 }
 
 // ------------------------------------------------------------------------------------------------
 // Few rows
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves, kStep = 128;  // k of a wave's load
-constexpr int kStage = 64 * 1024;                              // bytes of LDS: two workgroups a CU
+constexpr int kStep = 128;  // k of a wave's load
+
+// Parts of a value of x as the matrix instructions take it: bf16, or, fp32, three of them.
+template <class T>
+constexpr int kPartsOf = sizeof(T) == 4 ? 3 : 1;
 
 template <class T>
 struct Few {
   const T *x;
   int64_t ldx;
   bool vec_x;
-  int rows, n;  // of x (all of them), values of a row
+  int rows, n;
   const uint8_t *codes;
   const T *scales, *offsets;
+  int groups, pitch;  // of a row of codes: groups, bytes
   int64_t outputs;
   T *out;
   int64_t ldo;
+  float *slabs;  // sums of the slices of k, [slice][row][ld_slab]; nullptr: one slice, stored in out
+  int64_t ld_slab;
+  int slice;  // steps of a slice
+  bool pairs;  // rows of scales and offsets are whole dwords
   int parts;  // waves that share an output's k
-  int chunk;  // k in LDS at a time: whole steps for every one of them
 };
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 // A 4 x 4 transposition: word r of lane group j becomes word j of lane group r.
 __device__ __forceinline__ i32x4 across_groups(i32x4 v) {
-  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
   const u32x2 a = __builtin_amdgcn_permlane16_swap((unsigned)v[0], (unsigned)v[1], false, false), b = __builtin_amdgcn_permlane16_swap((unsigned)v[2], (unsigned)v[3], false, false);
   const u32x2 c = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
   return i32x4{(int)c[0], (int)d[0], (int)c[1], (int)d[1]};
 }
 
-// Eight codes as bf16 numbers, in the order 0 2 4 6 1 3 5 7.
+// Eight codes as bf16 numbers.
 __device__ __forceinline__ bf16x8 numbers(int word) {
-  const int even = word & 0x0f0f0f0f, odd = word >> 4 & 0x0f0f0f0f;
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, true);
+  const unsigned even = word & 0x0f0f0f0f, odd = word >> 4 & 0x0f0f0f0f;
+  const unsigned low = __builtin_amdgcn_perm(odd, even, 0x05010400), high = __builtin_amdgcn_perm(odd, even, 0x07030602);  // bytes in their order
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 512.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(low, 512.0f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 512.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(high, 512.0f, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-template <class T, int GROUP, bool OFFSETS>
-__global__ __launch_bounds__(kThreads) void k_few(Few<T> p) {
-  constexpr int kParts = sizeof(T) == 4 ? 3 : 1;  // of x
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tile::uniform(tid >> 6), i16 = lane & 15, j4 = lane >> 4;
-  const int t0 = blockIdx.y * 16, rows = min(p.rows - t0, 16);
-  const int pitch_x = p.chunk * 2 * kParts + 16;  // 16 bytes on, so that the rows of a fragment lie in different banks
-  const int fours = (rows + 3) / 4;
-  f32x4 *room = (f32x4 *)lds;                                   // a wave's 16 x 16 sums
-  f32x4 *sums = room + kThreads;                                // [group][rows / 4]: sums of x, times -8 without offsets
-  char *const stage = (char *)(sums + p.chunk / GROUP * fours);  // x
-  const int64_t pitch = pitch_of(p.n, GROUP), groups = groups_of(p.n, GROUP);
-  const int part = wave % p.parts, member = wave / p.parts, tiles = kWaves / p.parts;
-  const bool once = p.chunk >= p.n;
-  const char *frag = stage + min(i16, rows - 1) * pitch_x + j4 * 16;
-  const int64_t turns = ceil_div(p.outputs, 16 * tiles);
-  for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
-    const int64_t first = (turn * tiles + member) * 16;
-    const int there = (int)max((int64_t)0, min(p.outputs - first, (int64_t)16));
-    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void *)(p.codes + first * pitch), 0, there * (int)pitch, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(p.scales + first * groups), 0, there * (int)groups * (int)sizeof(T), 0x00027000);
-    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.offsets + first * groups), 0, OFFSETS ? there * (int)groups * (int)sizeof(T) : 0, 0x00027000);
-    const auto value = [&](__amdgpu_buffer_rsrc_t r, int g) {  // of group g of this lane's output; zero past the last
-      const int at = g < (int)groups ? (i16 * (int)groups + g) * (int)sizeof(T) : (int)tile::kOut;
-      if constexpr (sizeof(T) == 4)
-        return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
-      else
-        return (float)__builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0));
-    };
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k0 = 0; k0 < p.n; k0 += p.chunk) {
-      if (!once || turn == blockIdx.x) {
-        __syncthreads();
-        const int units = p.chunk / 8;  // a multiple of 16: a group's lanes stay together
-        for (int u = tid; u < rows * units; u += kThreads) {
-          const int r = u / units, k = (u - r * units) * 8;
-          const T *row = p.x + (t0 + r) * p.ldx;
-          const f32x4 a = few::load4(row, k0 + k, p.n, p.vec_x), b = few::load4(row, k0 + k + 4, p.n, p.vec_x);
-          const float v[8] = {a[0], a[2], b[0], b[2], a[1], a[3], b[1], b[3]};
-          bf16x8 out[kParts];
-          float sum = 0.0f;
+// x in LDS: for every row, blocks of 32 values, 64 bytes for each part; rows are 16 bytes more apart, so that those of a
+// fragment lie in different banks.
+template <class T>
+__host__ __device__ inline int stage_pitch(int steps) { return steps * (kStep * 2 * kPartsOf<T>) + 16; }
+
+// Eight values at value `at` of a staged row.
+template <class T>
+__device__ __forceinline__ void store_eight(char *row, int at, const f32x4 (&v)[2]) {
+  constexpr int kParts = kPartsOf<T>;
+  bf16x8 out[kParts];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            sum += v[i];
-            if constexpr (kParts == 3) {
-              __bf16 h, m, l;
-              split3(v[i], h, m, l);
-              out[0][i] = h;
-              out[1][i] = m;
-              out[2][i] = l;
-            } else {
-              out[0][i] = (__bf16)v[i];
-            }
-          }
-          char *to = stage + r * pitch_x + k / 32 * (64 * kParts) + k % 32 * 2;
+  for (int i = 0; i < 8; ++i)
+    if constexpr (kParts == 3) {
+      __bf16 hi, mid, lo;
+      split3(v[i / 4][i % 4], hi, mid, lo);
+      out[0][i] = hi;
+      out[1][i] = mid;
+      out[2][i] = lo;
+    } else {
+      out[0][i] = (__bf16)v[i / 4][i % 4];
+    }
+  char *to = row + at / 32 * (64 * kParts) + at % 32 * 2;
 #pragma unroll
-          for (int i = 0; i < kParts; ++i) *(bf16x8 *)(to + 64 * i) = out[i];
+  for (int i = 0; i < kParts; ++i) *(bf16x8 *)(to + 64 * i) = out[i];
+}
+
+// Values [k0, k0 + 8 units) of every row, zeros past n. Rows of whole 16 bytes are loaded without branches, four eights a
+// lane at once: one at a time their latency is what this takes (64 x 1000 to 1000 outputs: 20 us so).
+template <class T>
+__device__ __forceinline__ void stage_rows(char *stage, int pitch, const T *x, int64_t ldx, int rows, int n, int k0, int units, bool vec, int threads) {
+  const int total = rows * units;
+  if (vec && n % 8 == 0) {
+    typedef T Eight __attribute__((ext_vector_type(8)));
+    for (int u0 = threadIdx.x; u0 < total; u0 += 4 * threads) {
+      Eight v[4];
+      int r[4], k[4];
 #pragma unroll
-          for (int d = 1; d < GROUP / 8; d <<= 1) sum += __shfl_xor(sum, d);
-          if (k % GROUP == 0) ((float *)sums)[k / GROUP * 4 * fours + r] = OFFSETS ? sum : -8.0f * sum;
-        }
-        __syncthreads();
+      for (int i = 0; i < 4; ++i) {
+        const int u = min(u0 + i * threads, total - 1);
+        r[i] = u / units;
+        k[i] = (u - r[i] * units) * 8;
+        v[i] = *(const Eight *)(x + r[i] * ldx + min(k0 + k[i], n - 8));
       }
-      const int steps = min(p.chunk, (int)ceil_div(p.n - k0, kStep) * kStep) / kStep;
-      const int per = (steps + p.parts - 1) / p.parts, s1 = min((part + 1) * per, steps);
-      constexpr int U = 4, G = kStep / GROUP;
-      for (int s = part * per; s < s1; s += U) {
-        i32x4 c[U];
-        float scale[U][G], offset[U][G];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int at = (k0 + (s + u) * kStep) / 2 + j4 * 16;
-          c[u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, s + u < s1 && at < (int)pitch ? i16 * (int)pitch + at : (int)tile::kOut, 0, 0));
+      for (int i = 0; i < 4; ++i) {
+        f32x4 f[2];
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const int which = s + u < s1 ? (k0 + (s + u) * kStep) / GROUP + g : (int)groups;
-            scale[u][g] = value(rs, which);
-            if constexpr (OFFSETS) offset[u][g] = value(ro, which);
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int step = min(s + u, s1 - 1);  // past the last: codes, scales and offsets of zero
-          const i32x4 words = across_groups(c[u]);
-          f32x4 sum;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int g = q * 32 / GROUP;
-            if (q * 32 % GROUP == 0) {
-              const f32x4 x = sums[(step * G + g) * fours + min(j4, fours - 1)];  // (past the rows: anything)
-              if constexpr (OFFSETS) {
-                sum = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] = fmaf(offset[u][g], x[e], acc[e]);
-              } else {
-                sum = x;
-              }
-            }
-            const bf16x8 w = numbers(words[q]);
-            const char *a = frag + (step * 4 + q) * (64 * kParts);
-#pragma unroll
-            for (int i = kParts - 1; i >= 0; --i) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)(a + 64 * i), w, sum, 0, 0, 0);
-            if ((q + 1) * 32 % GROUP == 0)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[e] = fmaf(scale[u][g], sum[e], acc[e]);
-          }
-        }
+        for (int e = 0; e < 8; ++e) f[e / 4][e % 4] = k0 + k[i] < n ? (float)v[i][e] : 0.0f;
+        store_eight<T>(stage + r[i] * pitch, k[i], f);
       }
     }
-    if (p.parts > 1) {
-      __syncthreads();
-      room[wave * 64 + lane] = acc;
-      __syncthreads();
-      if (part == 0)
-        for (int i = 1; i < p.parts; ++i) acc += room[(wave + i) * 64 + lane];
+  } else {
+    for (int u = threadIdx.x; u < total; u += threads) {
+      const int r = u / units, k = (u - r * units) * 8;
+      const T *row = x + r * ldx;
+      const f32x4 f[2] = {few::load4(row, k0 + k, n, vec), few::load4(row, k0 + k + 4, n, vec)};
+      store_eight<T>(stage + r * pitch, k, f);
     }
-    if (part == 0 && i16 < there)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (4 * j4 + e < rows) p.out[(t0 + 4 * j4 + e) * p.ldo + first + i16] = (T)acc[e];
   }
 }
 
-template <class T, int GROUP>
-sdnn_status few_of(Few<T> p, hipStream_t stream) {
-  const int parts_x = sizeof(T) == 4 ? 3 : 1, rows = std::min(p.rows, 16);
-  const int64_t tiles = ceil_div(p.outputs, 16), steps = ceil_div(p.n, kStep);
-  const int64_t fours = ceil_div(rows, 4) * 16, per_step = rows * kStep * 2 * parts_x + kStep / GROUP * fours, fixed = kThreads * 16 + rows * 16;
-  const int64_t fit = (kStage - fixed) / per_step;  // steps of k: 4 at least (16 rows in three parts, groups of 32)
-  // as many waves on one output's k as it takes to give every CU two workgroups
-  p.parts = 1;
-  while (p.parts < kWaves && tiles * p.parts < kWaves * 2 * kCus && p.parts * 2 <= std::min(steps, fit)) p.parts *= 2;
-  const int64_t unit = kStep * p.parts;
-  p.chunk = (int)std::min(fit / p.parts * unit, ceil_div(p.n, unit) * unit);
-  const size_t lds = (size_t)(fixed + p.chunk / kStep * per_step);
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(tiles * p.parts, kWaves), 2 * kCus), (unsigned)ceil_div(p.rows, 16));
-  if (p.offsets)
-    hipLaunchKernelGGL((k_few<T, GROUP, true>), grid, dim3(kThreads), lds, stream, p);
+// Scales and offsets of 16 groups of 16 outputs, a wave's in LDS (a row's are 4 values apart, which spreads the rows over the
+// banks). Memory is read 4 groups a lane at once: their rows are far apart, and a lane's value at a time would fetch
+// each of their lines again and again (16 x 16384 to 16384 outputs, groups of 64 with offsets: 59 us so).
+constexpr int kHeld = 16, kHeldPitch = kHeld + 4;
+template <class T>
+struct Four {
+  T v[4];
+};
+
+// Shapes of a workgroup: 16 rows of x in half a CU's LDS or all of it, 32 or 64 rows, whose fragments serve two tiles of
+// outputs each. A wave multiplies STEPS steps at a time, with those of the next AHEAD times on their way.
+template <int TILES, int OUTS, int STEPS, int AHEAD, int WAVES, int PER_SIMD, int ROOM>
+struct Shape {
+  static constexpr int kTiles = TILES, kOuts = OUTS, kSteps = STEPS, kAhead = AHEAD, kWaves = WAVES, kPerSimd = PER_SIMD;
+  template <class T>
+  static constexpr int kHeldBytes = OUTS * 2 * 16 * kHeldPitch * (int)sizeof(T);  // of a wave
+  template <class T>
+  static constexpr int kStage = (ROOM << 10) - WAVES * kHeldBytes<T>;  // what is left for x
+};
+using Half = Shape<1, 1, 2, 1, 8, 4, 76>;
+using Whole = Shape<1, 1, 2, 1, 16, 4, 158>;
+using Two = Shape<2, 2, 1, 1, 8, 2, 158>;
+using FourTiles = Shape<4, 2, 1, 1, 8, 2, 158>;
+
+// TILES x 16 rows (those past the last repeat it; their sums go nowhere), OUTS x 16 outputs a wave at a time. A workgroup
+// holds its slice of x in LDS and goes over the outputs; waves in teams of `parts` share an output's k.
+template <class T, int SHIFT, bool OFFSETS, class S>
+__global__ __launch_bounds__(64 * S::kWaves, S::kPerSimd) void k_few(Few<T> p) {
+  constexpr int TILES = S::kTiles, OUTS = S::kOuts, STEPS = S::kSteps, AHEAD = S::kAhead, WAVES = S::kWaves;
+  constexpr int kParts = kPartsOf<T>, kGroups = 4 >> SHIFT;  // kGroups: of a step
+  // -8 sum x starts each block of 32's sum, so that these never grow far past their result. bf16 rows that serve several
+  // tiles of outputs have it for a whole group at once, in one chain for all of them: 3 bits of fp32 less, none of bf16's.
+  constexpr bool kWhole = !OFFSETS && OUTS > 1 && kParts == 1;
+  __shared__ __attribute__((aligned(16))) char stage[S::template kStage<T>];
+  __shared__ __attribute__((aligned(16))) char wave_room[WAVES][S::template kHeldBytes<T>];
+  static_assert(S::template kHeldBytes<T> >= 1024, "a wave's sums have room there too");
+  const int lane = threadIdx.x & 63, wave = tile::uniform(threadIdx.x >> 6), i16 = lane & 15, j4 = lane >> 4;
+  const int part = wave % p.parts, member = wave / p.parts, teams = WAVES / p.parts;
+  const int blocks = (p.n + 31) / 32, first_step = blockIdx.y * p.slice, steps = min(p.slice, (p.n + kStep - 1) / kStep - first_step);
+  const int per = (steps + p.parts - 1) / p.parts, s0 = part * per, s1 = min(s0 + per, steps);
+  const int pitch_x = stage_pitch<T>(steps), units = steps * (kStep / 8);
+  stage_rows(stage, pitch_x, p.x, p.ldx, p.rows, p.n, first_step * kStep, units, p.vec_x, 64 * WAVES);
+  __syncthreads();
+  const char *from[TILES];
+#pragma unroll
+  for (int r = 0; r < TILES; ++r) from[r] = stage + min(r * 16 + i16, p.rows - 1) * pitch_x + j4 * 16;
+  T *const held = (T *)wave_room[wave];
+  bf16x8 ones;  // for the sums of x: times -8 where there are no offsets
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)(OFFSETS ? 1.0f : -8.0f);
+  const int64_t turns = ceil_div(p.outputs, 16 * OUTS * teams);
+  for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+    const int64_t first = (turn * teams + member) * (16 * OUTS);
+    const int there = (int)max((int64_t)0, min(p.outputs - first, (int64_t)(16 * OUTS)));
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void *)(p.codes + first * p.pitch), 0, there * p.pitch, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(p.scales + first * p.groups), 0, there * p.groups * (int)sizeof(T), 0x00027000);
+    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((void *)(p.offsets + first * p.groups), 0, OFFSETS ? there * p.groups * (int)sizeof(T) : 0, 0x00027000);
+    // This lane's 4 groups of the 16 from g on; zeros past the last.
+    const auto load_four = [&](__amdgpu_buffer_rsrc_t r, int o, int g) {
+      Four<T> to;
+      g += 4 * j4;
+      const int at = g < p.groups ? ((o * 16 + i16) * p.groups + g) * (int)sizeof(T) : (int)tile::kOut;
+      if constexpr (sizeof(T) == 4) {
+        to = __builtin_bit_cast(Four<T>, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+      } else if (p.pairs) {
+        to = __builtin_bit_cast(Four<T>, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to.v[i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(r, at + 2 * i, 0, 0));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to.v[i] = g + i < p.groups ? to.v[i] : (T)0.0f;
+      return to;
+    };
+    struct Codes {
+      i32x4 of[STEPS][OUTS];
+    };
+    // Of the steps from s on; past s1 and past the last block, zeros.
+    const auto load = [&](Codes &to, int s) {
+#pragma unroll
+      for (int u = 0; u < STEPS; ++u) {
+        const int block = (first_step + s + u) * 4 + j4;
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o)
+          to.of[u][o] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, s + u < s1 && block < blocks ? (o * 16 + i16) * p.pitch + block * 16 : (int)tile::kOut, 0, 0));
+      }
+    };
+    f32x4 acc[TILES][OUTS];
+#pragma unroll
+    for (int r = 0; r < TILES; ++r)
+#pragma unroll
+      for (int o = 0; o < OUTS; ++o) acc[r][o] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    Four<T> next_scales[OUTS], next_offsets[OUTS];
+    int next = (first_step + s0) * 4 >> SHIFT & -kHeld;  // the first group of those
+    const auto ask = [&] {
+#pragma unroll
+      for (int o = 0; o < OUTS; ++o) {
+        next_scales[o] = load_four(rs, o, next);
+        if constexpr (OFFSETS) next_offsets[o] = load_four(ro, o, next);
+      }
+    };
+    const auto multiply = [&](const i32x4 (&codes)[OUTS], int s) {
+      const int g0 = (first_step + s) * 4 >> SHIFT;
+      if (g0 >= next) {  // 16 more groups
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o) {
+          T *to = held + (o * 32 + i16) * kHeldPitch + 4 * j4;
+          *(Four<T> *)to = next_scales[o];
+          if constexpr (OFFSETS) *(Four<T> *)(to + 16 * kHeldPitch) = next_offsets[o];
+        }
+        next += kHeld;
+        ask();
+      }
+      float scale[kGroups][OUTS], offset[kGroups][OUTS];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o) {
+          const T *at = held + (o * 32 + i16) * kHeldPitch + g0 % kHeld + g;
+          scale[g][o] = (float)at[0];
+          if constexpr (OFFSETS) offset[g][o] = (float)at[16 * kHeldPitch];
+        }
+      bf16x8 w[4][OUTS];
+#pragma unroll
+      for (int o = 0; o < OUTS; ++o) {
+        const i32x4 words = across_groups(codes[o]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q][o] = numbers(words[q]);
+      }
+#pragma unroll
+      for (int r = 0; r < TILES; ++r)
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+          f32x4 all = zero, sum[OUTS];
+          if constexpr (kWhole) {
+#pragma unroll
+            for (int q = g << SHIFT; q < (g + 1) << SHIFT; ++q) all = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 *)(from[r] + (s * 4 + q) * 64), ones, all, 0, 0, 0);
+          }
+#pragma unroll
+          for (int o = 0; o < OUTS; ++o) sum[o] = all;
+#pragma unroll
+          for (int q = g << SHIFT; q < (g + 1) << SHIFT; ++q) {
+            bf16x8 x[kParts];
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) x[i] = *(const bf16x8 *)(from[r] + (s * 4 + q) * (64 * kParts) + i * 64);
+            if constexpr (kWhole) {
+#pragma unroll
+              for (int o = 0; o < OUTS; ++o) sum[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[0], w[q][o], sum[o], 0, 0, 0);
+              continue;
+            }
+            f32x4 &to = OFFSETS ? all : OUTS == 1 ? sum[0] : all;
+            if (!OFFSETS && OUTS > 1) all = zero;
+#pragma unroll
+            for (int i = kParts - 1; i >= 0; --i) to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], ones, to, 0, 0, 0);
+#pragma unroll
+            for (int o = 0; o < OUTS; ++o) {
+              if (!OFFSETS && OUTS > 1) sum[o] = sum[o] + all;
+#pragma unroll
+              for (int i = kParts - 1; i >= 0; --i) sum[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], w[q][o], sum[o], 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              acc[r][o][e] = fmaf(scale[g][o], sum[o][e], acc[r][o][e]);
+              if constexpr (OFFSETS) acc[r][o][e] = fmaf(offset[g][o], all[e], acc[r][o][e]);
+            }
+        }
+    };
+    if (s0 < s1) {
+      Codes codes[AHEAD + 1];
+      ask();
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) load(codes[i], s0 + i * STEPS);
+#pragma unroll 1
+      for (int s = s0; s < s1; s += STEPS) {
+        load(codes[AHEAD], s + AHEAD * STEPS);
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u)
+          if (s + u < s1) multiply(codes[0].of[u], s + u);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) codes[i] = codes[i + 1];
+      }
+    }
+    if (TILES == 1 && p.parts > 1) {
+      f32x4 *room = (f32x4 *)wave_room[wave];
+      room[lane] = acc[0][0];
+      __syncthreads();
+      if (part == 0)
+        for (int w = 1; w < p.parts; ++w) acc[0][0] += *(f32x4 *)(wave_room[wave + w] + lane * 16);
+      __syncthreads();  // before the next turn's scales take the place
+    }
+    if (part == 0)
+#pragma unroll
+      for (int r = 0; r < TILES; ++r)
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int t = r * 16 + 4 * j4 + e;
+            if (t >= p.rows || o * 16 + i16 >= there) continue;
+            const int64_t v = first + o * 16 + i16;
+            if (p.slabs)
+              p.slabs[((int64_t)blockIdx.y * p.rows + t) * p.ld_slab + v] = acc[r][o][e];
+            else
+              p.out[t * p.ldo + v] = (T)acc[r][o][e];
+          }
+  }
+}
+
+// How few rows are gone over.
+struct FewPlan {
+  int tiles, parts, slice, slices;
+  bool half;  // x takes half of a CU's LDS
+  template <class T>
+  void of(int64_t rows, int64_t outputs, int64_t n) {
+    const int64_t steps = ceil_div(n, kStep), per_step = rows * (kStep * 2 * kPartsOf<T>);
+    tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    half = tiles == 1 && rows * 16 + steps * per_step <= Half::kStage<T>;
+    const int64_t room = half ? Half::kStage<T> : tiles == 1 ? Whole::kStage<T> : Two::kStage<T>;
+    int64_t k = ceil_div(steps, (room - rows * 16) / per_step);
+    const int64_t outs = ceil_div(outputs, tiles == 1 ? 16 : 32);
+    // as many waves as a CU takes share an output's k, or, past 16 rows, slices of it
+    if (tiles > 1)
+      while (outs * k < 8 * kCus && k * 4 <= steps) k *= 2;
+    slice = (int)ceil_div(steps, k);
+    slices = (int)ceil_div(steps, slice);
+    parts = 1;
+    if (tiles == 1)
+      while (parts < (half ? Half::kWaves : Whole::kWaves) && outs * slices * parts < 16 * kCus && parts * 2 <= slice) parts *= 2;
+  }
+  FewPlan(int64_t rows, int64_t outputs, int64_t n, int32_t dtype) {
+    if (dtype == SDNN_BF16)
+      of<__bf16>(rows, outputs, n);
+    else
+      of<float>(rows, outputs, n);
+  }
+};
+static_assert(Two::kStage<float> == FourTiles::kStage<float> && Two::kStage<__bf16> == FourTiles::kStage<__bf16>, "one room in FewPlan");
+
+template <class S, class T>
+sdnn_status launch_few(const Few<T> &p, const FewPlan &plan, int group, hipStream_t stream) {
+  const int64_t turns = ceil_div(p.outputs, 16 * S::kOuts * (S::kWaves / p.parts));
+  const dim3 grid((unsigned)std::min<int64_t>(turns, std::max(1, (plan.half ? 2 : 1) * kCus / plan.slices)), (unsigned)plan.slices);
+  const auto go = [&](auto shift) {
+    if (p.offsets)
+      hipLaunchKernelGGL((k_few<T, shift(), true, S>), grid, dim3(64 * S::kWaves), 0, stream, p);
+    else
+      hipLaunchKernelGGL((k_few<T, shift(), false, S>), grid, dim3(64 * S::kWaves), 0, stream, p);
+  };
+  if (group == 32)
+    go(std::integral_constant<int, 0>{});
+  else if (group == 64)
+    go(std::integral_constant<int, 1>{});
   else
-    hipLaunchKernelGGL((k_few<T, GROUP, false>), grid, dim3(kThreads), lds, stream, p);
-  return launched("linear");
+    go(std::integral_constant<int, 2>{});
+  sdnn_status st = launched("linear");
+  if (st != SDNN_OK || plan.slices == 1) return st;
+  return sum_slabs(p.slabs, plan.slices, p.ld_slab, Store<T>{p.out, p.ldo, p.rows, p.outputs, vector_rows(p.out, p.ldo)}, stream, "linear");
+}
+
+template <class T>
+sdnn_status few_of(Few<T> p, const FewPlan &plan, int group, hipStream_t stream) {
+  p.slice = plan.slice;
+  p.parts = plan.parts;
+  p.pairs = p.groups % 2 == 0 && (uintptr_t)p.scales % 4 == 0 && (uintptr_t)p.offsets % 4 == 0;
+  if (plan.slices == 1) p.slabs = nullptr;
+  if (plan.tiles == 1) return plan.half ? launch_few<Half>(p, plan, group, stream) : launch_few<Whole>(p, plan, group, stream);
+  return plan.tiles == 2 ? launch_few<Two>(p, plan, group, stream) : launch_few<FourTiles>(p, plan, group, stream);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -325,6 +548,7 @@ struct Sizes {
   int32_t dtype;
   bool few() const { return rows <= kFewRows; }
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, outputs) <= kPlain ? KIND_F32 : KIND_SPLIT; }
+  int64_t ld_slab() const { return ceil_div(outputs, 4) * 4; }
   int64_t values() const { return ceil_div(n, 8) * 8; }  // of a row of weights written as values
   int64_t piece() const { return std::min(outputs, std::max<int64_t>(256, kPieceValues / values() / 256 * 256)); }
   int64_t pitch() const { return kind() == KIND_SPLIT ? ceil_div(n, 32) * 128 : values() * dtype_bytes(dtype); }  // of a row of x
@@ -333,10 +557,16 @@ struct Sizes {
 struct Space {
   char *w, *x, *split;
   int *ex, *ew;
+  float *slabs;
   Space(Carver &c, const Sizes &s) {
-    const bool parts = !s.few() && s.kind() == KIND_SPLIT;
-    w = c.take<char>(s.few() ? 0 : (size_t)(s.piece() * s.values() * dtype_bytes(s.dtype)));
-    x = c.take<char>(s.few() ? 0 : (size_t)(s.rows * s.pitch()));
+    if (s.few()) {
+      const FewPlan p(s.rows, s.outputs, s.n, s.dtype);
+      slabs = c.take<float>(p.slices > 1 ? (size_t)(p.slices * s.rows * s.ld_slab()) : 0);
+      return;
+    }
+    const bool parts = s.kind() == KIND_SPLIT;
+    w = c.take<char>((size_t)(s.piece() * s.values() * dtype_bytes(s.dtype)));
+    x = c.take<char>((size_t)(s.rows * s.pitch()));
     split = c.take<char>(parts ? (size_t)(s.piece() * s.pitch()) : 0);
     ex = c.take<int>(parts ? s.rows : 0);
     ew = c.take<int>(parts ? s.piece() : 0);
@@ -351,7 +581,7 @@ dim3 grid_of(int64_t rows, int64_t items) {
 
 template <class T>
 sdnn_status dequantize(const uint8_t *codes, const T *scales, const T *offsets, int group, int64_t rows, int64_t n, T *out, int64_t ld, int64_t wide, hipStream_t stream) {
-  hipLaunchKernelGGL((k_dequantize<T>), grid_of(rows, ceil_div(wide, 8)), dim3(256), 0, stream, codes, scales, offsets, group, rows, n, out, ld, wide, vector_rows(out, ld));
+  hipLaunchKernelGGL((k_dequantize<T>), grid_of(ceil_div(rows, 4), ceil_div(wide, 8)), dim3(256), 0, stream, codes, scales, offsets, __builtin_ctz(group), rows, (int)n, out, ld, (int)wide, vector_rows(out, ld));
   return launched("dequantize");
 }
 
@@ -394,12 +624,13 @@ sdnn_status many(const Sizes &s, const T *x, int64_t ldx, const uint8_t *codes, 
 
 template <class T>
 sdnn_status linear(const Sizes &s, const void *x, int64_t ldx, const uint8_t *codes, const void *scales, const void *offsets, int group, void *out, int64_t ldo, void *workspace, hipStream_t stream) {
-  if (s.few()) {
-    const Few<T> p{(const T *)x, ldx, aligned16(x, ldx, sizeof(T)), (int)s.rows, (int)s.n, codes, (const T *)scales, (const T *)offsets, s.outputs, (T *)out, ldo, 0, 0};
-    return group == 32 ? few_of<T, 32>(p, stream) : group == 64 ? few_of<T, 64>(p, stream) : few_of<T, 128>(p, stream);
-  }
   Carver c{(char *)workspace};
   const Space sp(c, s);
+  if (s.few()) {
+    const Few<T> p{(const T *)x, ldx, aligned16(x, ldx, sizeof(T)), (int)s.rows, (int)s.n, codes, (const T *)scales, (const T *)offsets, (int)groups_of(s.n, group), (int)pitch_of(s.n, group),
+                   s.outputs, (T *)out, ldo, sp.slabs, s.ld_slab(), 0, false, 1};
+    return few_of<T>(p, FewPlan(s.rows, s.outputs, s.n, s.dtype), group, stream);
+  }
   const auto call = [&](auto kind) { return many<kind(), T>(s, (const T *)x, ldx, codes, (const T *)scales, (const T *)offsets, group, (T *)out, ldo, sp, stream); };
   if constexpr (sizeof(T) == 2)
     return call(std::integral_constant<int, KIND_BF16>{});

@@ -274,35 +274,41 @@ def _extent(name: str, t) -> tuple[int, int, int]:
     return *t.shape, _rows(name, t, None, None, t.dtype)[1]
 
 
+def _asked(name: str, tensors, norm) -> tuple[list, list]:
+    """Types and addresses of a list of tensors on the GPU of `norm`. A list may hold hundreds: what is asked of all of
+    them is asked by map, which costs a tenth of a microsecond a tensor."""
+    for kind in set(map(type, tensors)):
+        if not issubclass(kind, torch.Tensor):
+            raise ValueError(f"{name} holds a {kind.__name__}, which is no tensor")
+    if set(map(torch.Tensor.get_device, tensors)) - {norm.get_device()}:
+        raise ValueError(f"not all of {name} are on the GPU of norm, {norm.device}")
+    return list(map(attrgetter("dtype"), tensors)), list(map(torch.Tensor.data_ptr, tensors))
+
+
 def _list(tensors, out, norm):
-    """The C ABI's description of a list of tensors (sdnn_tensor, seven words each) and its length. A list may hold
-    hundreds: what is asked of all of them is asked by map."""
+    """The C ABI's description of a list of tensors (sdnn_tensor, seven words each) and its length."""
     _on_gpu("norm", norm)
     tensors = list(tensors)
     to = tensors if out is None else list(out)
-    if len(to) != len(tensors):
-        raise ValueError(f"out holds {len(to)} tensors, not {len(tensors)}")
-    for name, ts in (("tensors", tensors), ("out", to)):
-        for i, t in enumerate(ts):
-            if not isinstance(t, torch.Tensor):
-                raise ValueError(f"{name}[{i}] is no tensor")
-        if set(map(torch.Tensor.get_device, ts)) - {norm.get_device()}:
-            raise ValueError(f"not all of {name} are on the GPU of norm, {norm.device}")
-        if ts is to and ts is tensors:
-            break
-    dtypes = list(map(attrgetter("dtype"), tensors))
-    codes = [_dtype(d) for d in dtypes]
-    if to is not tensors:
-        for i, (a, b, d, e) in enumerate(zip(map(torch.Tensor.size, tensors), map(torch.Tensor.size, to), dtypes, map(attrgetter("dtype"), to))):
-            if a != b or d != e:
-                raise ValueError(f"out[{i}] is {tuple(b)} of {e}, not {tuple(a)} of {d}")
-    table = np.zeros((len(tensors), 7), np.int64)
-    table[:, 0] = list(map(torch.Tensor.data_ptr, tensors))
-    table[:, 1] = table[:, 0] if to is tensors else list(map(torch.Tensor.data_ptr, to))
-    table[:, 6] = codes
-    if all(map(torch.Tensor.is_contiguous, tensors)) and (to is tensors or all(map(torch.Tensor.is_contiguous, to))):
-        table[:, 2] = 1
-        table[:, 3] = list(map(torch.Tensor.numel, tensors))
+    n = len(tensors)
+    if len(to) != n:
+        raise ValueError(f"out holds {len(to)} tensors, not {n}")
+    dtypes, addresses = _asked("tensors", tensors, norm)
+    to_dtypes, to_addresses = (dtypes, addresses) if to is tensors else _asked("out", to, norm)
+    codes = list(map(DTYPES.get, dtypes))
+    if None in codes:
+        _dtype(dtypes[codes.index(None)])
+    table = np.zeros((n, 7), np.int64)
+    table[:, 0], table[:, 1], table[:, 6] = addresses, to_addresses, codes
+    flat = all(map(torch.Tensor.is_contiguous, tensors)) and (to is tensors or all(map(torch.Tensor.is_contiguous, to)))
+    shape = torch.Tensor.numel if flat else torch.Tensor.size
+    shapes = list(map(shape, tensors))
+    if to is not tensors and (dtypes != to_dtypes or shapes != list(map(shape, to))):
+        for i, (a, b) in enumerate(zip(tensors, to)):
+            if a.dtype != b.dtype or shape(a) != shape(b):
+                raise ValueError(f"out[{i}] is {tuple(b.shape)} of {b.dtype}, not {tuple(a.shape)} of {a.dtype}")
+    if flat:
+        table[:, 2], table[:, 3] = 1, shapes
     else:
         for i, (a, b) in enumerate(zip(tensors, to)):
             (rows, cols, ld), (rows_out, cols_out, ldo) = _extent(f"tensors[{i}]", a), _extent(f"out[{i}]", b)
@@ -310,7 +316,7 @@ def _list(tensors, out, norm):
                 rows, cols = a.shape
                 ld, ldo = ld or cols, ldo or cols
             table[i, 2:6] = rows, cols, ld, ldo
-    return table, len(tensors)
+    return table, n
 
 
 def global_norm(tensors, norm, workspace, stream=None) -> None:
@@ -322,8 +328,8 @@ def global_norm(tensors, norm, workspace, stream=None) -> None:
 
 
 def clip(tensors, max_norm: float, norm, workspace, out=None, stream=None) -> None:
-    """The norm, as `global_norm` has it, and every value times min(1, max_norm / norm), into the tensors of `out` (same shapes
-    and types; None: the tensors themselves)."""
+    """The norm, as `global_norm` has it, and every value times min(1, max_norm / norm), into the tensors of `out` (of the same
+    types and shapes, contiguous ones of as many values; None: the tensors themselves)."""
     table, n = _list(tensors, out, norm)
     _call(norm, "sdnn_clip", table.ctypes.data, n, max_norm, _vector("norm", norm, 1, torch.float32, norm), *_workspace(workspace, norm),
           _stream_handle(stream))
@@ -337,20 +343,23 @@ def grouped_groups(n_values: int, group: int = 128) -> int:
     return -(-n_values // group) if 1 <= n_values <= 1 << 20 and group in GROUPS else 0
 
 
+def _whole(name: str, t, rows: int, cols: int, dtype, like) -> int:
+    """Address of a contiguous matrix."""
+    _on_gpu(name, t, like)
+    if t.dtype != dtype or t.shape != (rows, cols) or not t.is_contiguous():
+        raise ValueError(f"{name}, {tuple(t.shape)} of {t.dtype}, is not ({rows}, {cols}) contiguous values of {dtype}")
+    return t.data_ptr()
+
+
 def _grouped(codes, scales, offsets, n_values: int, group: int, dtype, like) -> tuple[int, int, int | None, int]:
     """Addresses of codes, scales and offsets, and their rows."""
     if group not in GROUPS:
         raise ValueError(f"group {group!r} is none of {', '.join(map(str, GROUPS))}")
-    _on_gpu("codes", codes, like)
     n = grouped_groups(n_values, group)
-    named = (("codes", codes, torch.uint8, n * group // 2), ("scales", scales, dtype, n), ("offsets", offsets, dtype, n))
-    for name, t, kind, cols in named:
-        if t is None and name == "offsets":
-            continue
-        _on_gpu(name, t, like)
-        if t.dtype != kind or not t.is_contiguous() or t.dim() != 2 or t.shape[0] != codes.shape[0] or t.shape[1] != cols:
-            raise ValueError(f"{name}, {tuple(t.shape)} of {t.dtype}, do not hold contiguous rows of {n_values} values in groups of {group}: ({codes.shape[0] if codes.dim() else 0}, {cols}) of {kind}")
-    return codes.data_ptr(), scales.data_ptr(), None if offsets is None else offsets.data_ptr(), codes.shape[0]
+    _on_gpu("codes", codes, like)
+    rows = codes.shape[0] if codes.dim() else 0
+    return (_whole("codes", codes, rows, n * group // 2, torch.uint8, like), _whole("scales", scales, rows, n, dtype, like),
+            None if offsets is None else _whole("offsets", offsets, rows, n, dtype, like), rows)
 
 
 def grouped_quantize(w, codes, scales, group: int = 128, offsets=None, stream=None) -> None:
