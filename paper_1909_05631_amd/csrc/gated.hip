@@ -22,6 +22,7 @@
 using namespace dense;
 using namespace copies;
 using namespace sums;
+using tile::i32x4;
 using tile::KIND_BF16;
 using tile::KIND_F32;
 using tile::KIND_SPLIT;
@@ -43,7 +44,7 @@ __device__ __forceinline__ Activated activated(int activation, float g) {
   a.slope = 0.0f;
   if (activation == SDNN_SILU) {
     // g p with p = 1 / (1 + exp(-g)); the exponential may be infinite: p is then 0
-    const float p = 1.0f / (1.0f + few::exp_of(-g));
+    const float p = __builtin_amdgcn_rcpf(1.0f + few::exp_of(-g));  // (to one unit of its last place)
     a.value = g * p;
     if (SLOPE) a.slope = fmaf(a.value, 1.0f - p, p);
   } else if (activation == SDNN_GELU) {
@@ -69,11 +70,19 @@ struct Layer {
   T *h, *gate, *up;  // gate and up: nullptr where they are not kept; h: nullptr where they alone are wanted
   int64_t ldh, ldg, ldu;
   bool vec_h, vec_g, vec_u;
-  // Four neighbours' sums from output c on, of row t with exponent e.
-  __device__ __forceinline__ f32x4 scaled(f32x4 s, int e, const int *exponents, int64_t c) const {
+  // The exponents of four neighbouring outputs, from c on, and four sums of a row with exponent e without them.
+  __device__ __forceinline__ i32x4 columns(const int *exponents, int64_t c) const {
+    i32x4 e = {0, 0, 0, 0};
     if constexpr (KIND == KIND_SPLIT) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = ldexpf(s[i], -e - (c + i < hidden ? exponents[c + i] : 0));
+      for (int i = 0; i < 4; ++i) e[i] = c + i < hidden ? exponents[c + i] : 0;
+    }
+    return e;
+  }
+  __device__ __forceinline__ f32x4 scaled(f32x4 s, int e, i32x4 columns) const {
+    if constexpr (KIND == KIND_SPLIT) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = ldexpf(s[i], -e - columns[i]);
     }
     return s;
   }
@@ -88,13 +97,21 @@ struct Layer {
     static_assert(B::kTN % 2 == 0, "whole pairs");
     const int i16 = threadIdx.x & 15, j4 = (threadIdx.x & 63) >> 4;
     const int64_t first = col0 / 2;
+    i32x4 cg[N], cu[N];  // read once for all rows
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      cg[j] = columns(eg, first + 16 * j + 4 * j4);
+      cu[j] = columns(eu, first + 16 * j + 4 * j4);
+    }
+    int rows_e[B::kTM];
+#pragma unroll
+    for (int i = 0; i < B::kTM; ++i) rows_e[i] = KIND == KIND_SPLIT && row0 + 16 * i + i16 < rows ? ex[row0 + 16 * i + i16] : 0;
 #pragma unroll
     for (int i = 0; i < B::kTM; ++i) {
       const int64_t t = row0 + 16 * i + i16;
       const bool in = t < rows;
-      const int e = KIND == KIND_SPLIT && in ? ex[t] : 0;
-      const auto g = [&](int j) { return scaled(block.acc[i][2 * j], e, eg, first + 16 * j + 4 * j4); };
-      const auto u = [&](int j) { return scaled(block.acc[i][2 * j + 1], e, eu, first + 16 * j + 4 * j4); };
+      const auto g = [&](int j) { return scaled(block.acc[i][2 * j], rows_e[i], cg[j]); };
+      const auto u = [&](int j) { return scaled(block.acc[i][2 * j + 1], rows_e[i], cu[j]); };
       if (gate) store_row<T, N>(gate + t * ldg, first, hidden, vec_g, in, g);
       if (up) store_row<T, N>(up + t * ldu, first, hidden, vec_u, in, u);
       if (h) store_row<T, N>(h + t * ldh, first, hidden, vec_h, in, [&](int j) { return product(g(j), u(j)); });
@@ -115,12 +132,158 @@ __global__ __launch_bounds__(256) void k_layer_slabs(const float *slabs, int spl
       g += *(const f32x4 *)(from + s * to.rows * ld);
       u += *(const f32x4 *)(from + s * to.rows * ld + 16);
     }
-    g = to.scaled(g, e, to.eg, c);
-    u = to.scaled(u, e, to.eu, c);
+    g = to.scaled(g, e, to.columns(to.eg, c));
+    u = to.scaled(u, e, to.columns(to.eu, c));
     const int n = to.hidden - c < 4 ? (int)(to.hidden - c) : 4;
     if (to.gate) store4(to.gate + t * to.ldg + c, g, n, to.vec_g);
     if (to.up) store4(to.up + t * to.ldu + c, u, n, to.vec_u);
     if (to.h) store4(to.h + t * to.ldh + c, to.product(g, u), n, to.vec_h);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// The layer of few rows
+
+// Up to 16 rows of x stay in LDS while the weights stream past, each byte once, from memory to registers to the matrix
+// instructions: 16 outputs of a wave at a time, their rows of wg and of wu, 128 bytes of each row a step. Waves in teams of
+// `parts` share an output's k. Bound by the weights' bytes; the tiles would go through k in a few long chains.
+constexpr int kStepBytes = 128;
+
+template <int KIND, class T>
+struct FewRows {
+  const T *x;
+  int64_t ldx;
+  bool vec_x;
+  int rows, n;
+  const char *wg, *wu;
+  int pitch_g, pitch_u;  // bytes
+  int parts;
+  Layer<KIND, T> to;
+};
+
+// Workgroups of 8 waves that have half of a CU's LDS, or of 16 that have all of it.
+template <int WAVES>
+constexpr int kRoom = WAVES == 8 ? 64 << 10 : 130 << 10;
+
+template <class T>
+__host__ __device__ constexpr int steps_of(int n) { return (n * (int)sizeof(T) + kStepBytes - 1) / kStepBytes; }
+__host__ __device__ constexpr int stage_pitch(int steps) { return steps * kStepBytes + 16; }  // 16 bytes on: rows of a fragment in different banks
+
+// x's rows, zeros up to whole steps; rows of whole 16 bytes four chunks a lane at once.
+template <class T>
+__device__ __forceinline__ void stage_rows(char *stage, int steps, const T *x, int64_t ldx, int rows, int n, bool vec, int threads) {
+  constexpr int N = 16 / sizeof(T);
+  typedef T Chunk __attribute__((ext_vector_type(N)));
+  const int units = steps * (kStepBytes / 16), total = rows * units, pitch = stage_pitch(steps);
+  if (vec && n % N == 0) {
+    for (int u0 = threadIdx.x; u0 < total; u0 += 4 * threads) {
+      Chunk v[4];
+      int at[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int u = min(u0 + i * threads, total - 1), r = u / units, c = u - r * units;
+        at[i] = r * pitch + c * 16;
+        v[i] = *(const Chunk *)(x + r * ldx + min(c * N, n - N));
+        if (c * N >= n) v[i] = Chunk{};
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *(Chunk *)(stage + at[i]) = v[i];
+    }
+  } else {
+    for (int u = threadIdx.x; u < total; u += threads) {
+      const int r = u / units, c = u - r * units;
+      Chunk v = {};
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (c * N + i < n) v[i] = x[r * ldx + c * N + i];
+      *(Chunk *)(stage + r * pitch + c * 16) = v;
+    }
+  }
+}
+
+template <int KIND, class T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 4) void k_few_rows(FewRows<KIND, T> p) {
+  constexpr int kSteps = 2;  // a batch, while the next one is on its way
+  __shared__ __attribute__((aligned(16))) char stage[kRoom<WAVES>];
+  __shared__ f32x4 room[WAVES - 1][2][64];  // of all but the first wave, which is the first of its team
+  const int lane = threadIdx.x & 63, wave = tile::uniform(threadIdx.x >> 6), i16 = lane & 15, j4 = lane >> 4;
+  const int part = wave % p.parts, member = wave / p.parts, teams = WAVES / p.parts;
+  const int wide = p.n * (int)sizeof(T), steps = steps_of<T>(p.n), per = (steps + p.parts - 1) / p.parts, s0 = part * per, s1 = min(s0 + per, steps);
+  stage_rows(stage, steps, p.x, p.ldx, p.rows, p.n, p.vec_x, 64 * WAVES);
+  __syncthreads();
+  const char *from = stage + min(i16, p.rows - 1) * stage_pitch(steps) + j4 * 16;  // rows past the last repeat it; their sums go nowhere
+  const int64_t hidden = p.to.hidden, turns = ceil_div(hidden, 16 * teams);
+  for (int64_t turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+    const int64_t first = (turn * teams + member) * 16;
+    const int there = (int)max((int64_t)0, min(hidden - first, (int64_t)16));
+    const auto rows_of = [&](const char *w, int pitch) { return __builtin_amdgcn_make_buffer_rsrc((void *)(w + first * pitch), 0, there > 0 ? (there - 1) * pitch + wide : 0, 0x00027000); };
+    const __amdgpu_buffer_rsrc_t rg = rows_of(p.wg, p.pitch_g), ru = rows_of(p.wu, p.pitch_u);
+    struct Batch {
+      i32x4 g[kSteps][2], u[kSteps][2];
+    };
+    // Steps from s on, zeros past s1. A row's last chunk may hold what follows the row: zeros take its place.
+    const auto load = [&](Batch &to, int s) {
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int at = (s + k) * kStepBytes + h * 64 + j4 * 16;
+          const bool in = s + k < s1 && at < wide;
+          to.g[k][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rg, in ? i16 * p.pitch_g + at : (int)tile::kOut, 0, 0));
+          to.u[k][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ru, in ? i16 * p.pitch_u + at : (int)tile::kOut, 0, 0));
+        }
+    };
+    const auto clip = [&](i32x4 &v, int at) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = at + 4 * e < wide ? v[e] : 0;
+    };
+    f32x4 g = {0.0f, 0.0f, 0.0f, 0.0f}, u = g;
+    if (s0 < s1) {
+      Batch now, next;
+      load(now, s0);
+#pragma unroll 1
+      for (int s = s0; s < s1; s += kSteps) {
+        load(next, s + kSteps);
+        if (wide % 16 && (s + kSteps) * kStepBytes > wide) {
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              clip(now.g[k][h], (s + k) * kStepBytes + h * 64 + j4 * 16);
+              clip(now.u[k][h], (s + k) * kStepBytes + h * 64 + j4 * 16);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const i32x4 x = *(const i32x4 *)(from + min(s + k, steps - 1) * kStepBytes + h * 64);  // (past the steps: products with zeros)
+            g = tile::mfma<KIND>(now.g[k][h], x, g);
+            u = tile::mfma<KIND>(now.u[k][h], x, u);
+          }
+        now = next;
+      }
+    }
+    if (p.parts > 1) {
+      if (part > 0) {
+        room[wave - 1][0][lane] = g;
+        room[wave - 1][1][lane] = u;
+      }
+      __syncthreads();
+      if (part == 0)
+        for (int w = 1; w < p.parts; ++w) {
+          g += room[wave + w - 1][0][lane];
+          u += room[wave + w - 1][1][lane];
+        }
+      __syncthreads();  // before the next turn's sums take the place
+    }
+    const int64_t c = first + 4 * j4;
+    if (part == 0 && i16 < p.rows && c < hidden) {
+      const int n = hidden - c < 4 ? (int)(hidden - c) : 4;
+      if (p.to.gate) store4(p.to.gate + i16 * p.to.ldg + c, g, n, p.to.vec_g);
+      if (p.to.up) store4(p.to.up + i16 * p.to.ldu + c, u, n, p.to.vec_u);
+      if (p.to.h) store4(p.to.h + i16 * p.to.ldh + c, p.to.product(g, u), n, p.to.vec_h);
+    }
   }
 }
 
@@ -341,14 +504,39 @@ struct Kept {
   int64_t ldg, ldu;
 };
 
+// Few rows whose weights are read where they are.
+template <class T>
+bool few_rows(const Sizes &s, const Inputs<T> &in) {
+  return s.rows <= 16 && s.rows * (int64_t)stage_pitch(steps_of<T>((int)s.features)) <= kRoom<16> && usable_in_place(in.wg, in.ldg, s.features, sizeof(T)) &&
+         usable_in_place(in.wu, in.ldu, s.features, sizeof(T));
+}
+
+template <int KIND, class T, int WAVES>
+sdnn_status launch_few(FewRows<KIND, T> p, hipStream_t stream) {
+  const int64_t tiles = ceil_div(p.to.hidden, 16);
+  // as many waves on an output's k as it takes to give every CU 16
+  p.parts = 1;
+  while (p.parts < WAVES && tiles * p.parts < 16 * kCus && p.parts * 2 <= steps_of<T>(p.n)) p.parts *= 2;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(tiles, WAVES / p.parts), 16 / WAVES * kCus));
+  hipLaunchKernelGGL((k_few_rows<KIND, T, WAVES>), grid, dim3(64 * WAVES), 0, stream, p);
+  return launched("gated layer");
+}
+
 template <int KIND, class T>
 sdnn_status layer_of(const Sizes &s, const Inputs<T> &in, int activation, T *h, int64_t ldh, const Kept<T> &kept, Carver &carver, hipStream_t stream) {
   const LayerSpace sp(carver, s);
+  const Layer<KIND, T> e{sp.copies.ex, sp.copies.eg, sp.copies.eu, activation, s.rows, s.hidden, h, kept.gate, kept.up, ldh, kept.ldg, kept.ldu,
+                         vector_rows(h, ldh), vector_rows(kept.gate, kept.ldg), vector_rows(kept.up, kept.ldu)};
+  if constexpr (KIND != KIND_SPLIT) {
+    if (few_rows(s, in)) {
+      const FewRows<KIND, T> p{in.x, in.ldx, aligned16(in.x, in.ldx, sizeof(T)), (int)s.rows, (int)s.features, (const char *)in.wg, (const char *)in.wu, (int)(in.ldg * (int64_t)sizeof(T)),
+                               (int)(in.ldu * (int64_t)sizeof(T)), 1, e};
+      return s.rows * stage_pitch(steps_of<T>((int)s.features)) <= kRoom<8> ? launch_few<KIND, T, 8>(p, stream) : launch_few<KIND, T, 16>(p, stream);
+    }
+  }
   Operands o;
   sdnn_status st = operands<KIND>(s, in, sp.copies, true, true, false, o, stream);
   if (st != SDNN_OK) return st;
-  const Layer<KIND, T> e{sp.copies.ex, sp.copies.eg, sp.copies.eu, activation, s.rows, s.hidden, h, kept.gate, kept.up, ldh, kept.ldg, kept.ldu,
-                         vector_rows(h, ldh), vector_rows(kept.gate, kept.ldg), vector_rows(kept.up, kept.ldu)};
   if (sp.layer.splits == 1) return run_shape<KIND, false, false, true>(sp.layer, o.x, o.w, s.rows, s.paired(), s.features, e, stream, "gated layer");
   const int64_t ld = s.paired();
   st = run_shape<KIND, false, false, true>(sp.layer, o.x, o.w, s.rows, ld, s.features, Accumulate{sp.slabs, ld, s.rows, ld, false}, stream, "gated layer");
