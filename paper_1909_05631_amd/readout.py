@@ -353,7 +353,7 @@ def _whole(name: str, t, rows: int, cols: int, dtype, like) -> int:
 
 def _grouped(codes, scales, offsets, n_values: int, group: int, dtype, like) -> tuple[int, int, int | None, int]:
     """Addresses of codes, scales and offsets, and their rows."""
-    if group not in GROUPS:
+    if not isinstance(group, int) or group not in GROUPS:
         raise ValueError(f"group {group!r} is none of {', '.join(map(str, GROUPS))}")
     n = grouped_groups(n_values, group)
     _on_gpu("codes", codes, like)
