@@ -379,14 +379,15 @@ sdnn_status sdnn_grouped_dequantize(const uint8_t *codes, const void *scales, co
                                     void *hip_stream);
 
 /* out (n_rows x n_outputs, row stride ldo) = x w^T for rows x (n_rows x n_values, row stride ldx) and n_outputs rows of codes.
- * Up to 64 rows, scales and offsets are multiplied with fp32 sums over their groups, of exact products. For more rows w
- * is rounded to `dtype` first, as sdnn_grouped_dequantize has it, and multiplied with x: exact products for bf16, fp32
- * values as they are or as two fp16 parts (22 bits or more of each value down to 2^-17 of its row's largest). Sums are
- * fp32, rounded to `dtype` once. An infinity or a NaN in a row of x leaves none of its results finite; a group that stands
+ * Few rows (up to 64; up to 128 of bf16 or 256 of fp32 values where n_outputs is 4096 or more and w holds 2^24 values or
+ * more): scales and offsets are multiplied with fp32 sums over their groups, of exact products. For more rows w is rounded
+ * to `dtype` first, as sdnn_grouped_dequantize has it, and multiplied with x: exact products for bf16, fp32 values as they
+ * are or as two fp16 parts (22 bits or more of each value down to 2^-17 of its row's largest). Sums are fp32, rounded to
+ * `dtype` once. An infinity or a NaN in a row of x leaves none of its results finite; a group that stands
  * for NaN makes NaN of its output's. out may not overlap an input.
- * The workspace is 0 bytes for up to 64 rows whose k a workgroup holds in one piece (16 rows of 4096 bf16 values, 16 rows
- * of 1152 fp32 values). Past that it holds fp32 sums of 2 or more slices of k for each row and output; for more rows, w's
- * values, up to 2^28 of them. */
+ * The workspace is 0 bytes for up to 16 rows that a workgroup holds in one piece (16 of 4352 bf16 values, 16 of 1152 fp32
+ * values, one of 70528 and 20096). For other few rows it has fp32 sums of slices of k for 64 rows and each output; for
+ * more rows, w's values, up to 2^28 of them, and x's. */
 size_t sdnn_grouped_linear_workspace_bytes(int64_t n_rows, int64_t n_outputs, int64_t n_values, int32_t dtype);
 sdnn_status sdnn_grouped_linear(const void *x, int64_t ldx, int32_t dtype, const uint8_t *codes, const void *scales,
                                 const void *offsets, int64_t n_rows, int64_t n_outputs, int64_t n_values, int32_t group,

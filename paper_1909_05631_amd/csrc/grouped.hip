@@ -4,12 +4,17 @@
 //   y = sum over groups of  s sum_k x_k q_k + o sum_k x_k      (o = -8 s where there are no offsets)
 //
 // Few rows (k_few): every byte of codes goes from memory to registers once and from there to the matrix instructions as
-// exact whole numbers; a group's scale meets its fp32 sum, not its weights. A lane loads 32 codes of one output; four
-// lane exchanges bring the four lane groups of 16 to the same group of 32; a nibble in a byte is an 8-bit float of 2^-9 times
-// its value (up to 7 as a denormal number, from 8 on by its exponent), so that one conversion with the scale 2^9 makes two of
-// them the bf16 numbers 0 to 15. x is written once into LDS in the order of the codes, in bf16, fp32 as three bf16 parts
-// (exactly), with its sums over groups, which start the groups' products at -8 sum x or are multiplied with the offsets.
-// Many rows: the weights are written as values of x's type, and the tile products do the rest.
+// exact whole numbers; a group's scale meets its fp32 sum, not its weights. A lane loads 32 codes of one output, so that 16
+// lanes of each of 4 groups read 64 bytes of a row; four lane exchanges bring the four lane groups to the same 32 codes' group.
+// A nibble in a byte is an 8-bit float of 2^-9 times its value (up to 7 as a denormal number, from 8 on by its exponent), so
+// that one conversion with the scale 2^9 makes two of them the bf16 numbers 0 to 15. x stays in a workgroup's LDS, in bf16,
+// fp32 as three bf16 parts (exactly), past its size in slices of k whose sums a second kernel joins. Its sums over groups
+// are one more product, with a row of ones, or of -8.
+// Bound by the codes' bytes for one row (1 x 4096 to 65536 outputs 28.6 us, 4.8 TB/s; 1 x 16384 to 16384 30 us). Each 16 rows
+// more are one more product, LDS read and sum for each of them, and x takes its time on the way to LDS: 16 x 16384 to 16384
+// 38 us, with groups of 64 and offsets 42; 64 rows 75.
+// Many rows: the weights are written as values of x's type, and the tile products do the rest (2000 x 4096 to 16384 outputs
+// 231 us, 30 of them for that).
 #include "dense.h"
 #include "copies.h"
 #include "few.h"
@@ -25,10 +30,12 @@ using tile::KIND_SPLIT;
 
 namespace {
 
-constexpr int64_t kFewRows = 64;               // rows that go to k_few
+constexpr int64_t kFewRows = 64;               // rows that k_few takes at once
+constexpr int64_t kManyWeights = 1 << 24, kManyOutputs = 4096;  // see Sizes::few
 // Weights that are written as values at a time. Fewer (2^26 bf16 values would stay in the Infinity Cache) leave the products too
 // few blocks: 64 rows to 16384 x 16384 360 us so, 336 at once, 2000 rows 1300 us and 1140.
 constexpr int64_t kPieceValues = 1 << 28;
+constexpr int64_t kSplitResults = 1 << 24;     // results of a product whose k may be split
 constexpr int64_t kPlain = 192;                // fp32 rows or outputs for the plain fp32 products
 
 __host__ __device__ inline int64_t groups_of(int64_t n, int group) { return ceil_div(n, group); }
@@ -546,11 +553,18 @@ struct StoreScaled {
 struct Sizes {
   int64_t rows, outputs, n;
   int32_t dtype;
-  bool few() const { return rows <= kFewRows; }
+  // Rows for k_few, 64 at a time. Up to 64 it is never behind (us, k_few / the weights written as values: 64 x 1000 to 1000
+  // outputs 12 / 12, fp32 17 / 28; 64 x 16384 to 16384 75 / 273). Past that a second pass over the codes costs less than
+  // writing the weights where these are many and go to many outputs: bf16, 128 rows: 16384 to 16384 147 / 287, 4096 to
+  // 16384 53 / 66, 4096 to 4096 29 / 34, but 16384 to 1024 40 / 24; 192 rows: 4096 to 16384 78 / 74. fp32, 256 rows: 4096 to 8192
+  // 134 / 201, 4096 to 4096 80 / 87.
+  bool few() const { return rows <= kFewRows || (outputs >= kManyOutputs && outputs * n >= kManyWeights && rows <= kFewRows * (dtype == SDNN_BF16 ? 2 : 4)); }
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, outputs) <= kPlain ? KIND_F32 : KIND_SPLIT; }
   int64_t ld_slab() const { return ceil_div(outputs, 4) * 4; }
   int64_t values() const { return ceil_div(n, 8) * 8; }  // of a row of weights written as values
   int64_t piece() const { return std::min(outputs, std::max<int64_t>(256, kPieceValues / values() / 256 * 256)); }
+  // The product's k may be split where it has few results.
+  Plan product(int64_t m) const { return plan(kind(), rows, m, n, kind() != KIND_SPLIT && rows * m <= kSplitResults ? kMaxSplits : 1, kAlong); }
   int64_t pitch() const { return kind() == KIND_SPLIT ? ceil_div(n, 32) * 128 : values() * dtype_bytes(dtype); }  // of a row of x
 };
 
@@ -560,11 +574,23 @@ struct Space {
   float *slabs;
   Space(Carver &c, const Sizes &s) {
     if (s.few()) {
-      const FewPlan p(s.rows, s.outputs, s.n, s.dtype);
-      slabs = c.take<float>(p.slices > 1 ? (size_t)(p.slices * s.rows * s.ld_slab()) : 0);
+      size_t most = 0;
+      for (const int64_t m : {std::min(s.rows, kFewRows), s.rows % kFewRows}) {
+        if (m == 0) continue;
+        const FewPlan p(m, s.outputs, s.n, s.dtype);
+        if (p.slices > 1) most = std::max(most, (size_t)(p.slices * m * s.ld_slab()));
+      }
+      slabs = c.take<float>(most);
       return;
     }
     const bool parts = s.kind() == KIND_SPLIT;
+    size_t most = 0;
+    for (const int64_t m : {s.piece(), s.outputs % s.piece()}) {
+      if (m == 0) continue;
+      const Plan p = s.product(m);
+      if (p.splits > 1) most = std::max(most, (size_t)(p.splits * s.rows * (ceil_div(m, 4) * 4)));
+    }
+    slabs = c.take<float>(most);
     w = c.take<char>((size_t)(s.piece() * s.values() * dtype_bytes(s.dtype)));
     x = c.take<char>((size_t)(s.rows * s.pitch()));
     split = c.take<char>(parts ? (size_t)(s.piece() * s.pitch()) : 0);
@@ -613,10 +639,17 @@ sdnn_status many(const Sizes &s, const T *x, int64_t ldx, const uint8_t *codes, 
       if ((st = launched("linear")) != SDNN_OK) return st;
       b = {sp.split, s.pitch(), m, s.pitch(), 0};
       const StoreScaled e{sp.ex, sp.ew, out + v0, ldo, s.rows, m, vector_rows(out + v0, ldo)};
-      st = run_shape<KIND, false, false>(plan(KIND, s.rows, m, s.n, 1, kAlong), a, b, s.rows, m, s.n, e, stream, "linear");
+      st = run_shape<KIND, false, false>(s.product(m), a, b, s.rows, m, s.n, e, stream, "linear");
     } else {
       const Store<T> e{out + v0, ldo, s.rows, m, vector_rows(out + v0, ldo)};
-      st = run_shape<KIND, false, false>(plan(KIND, s.rows, m, s.n, 1, kAlong), a, b, s.rows, m, s.n, e, stream, "linear");
+      const Plan p = s.product(m);
+      if (p.splits == 1) {
+        st = run_shape<KIND, false, false>(p, a, b, s.rows, m, s.n, e, stream, "linear");
+      } else {
+        const int64_t ld_slab = ceil_div(m, 4) * 4;
+        st = run_shape<KIND, false, false>(p, a, b, s.rows, m, s.n, Accumulate{sp.slabs, ld_slab, s.rows, m, false}, stream, "linear");
+        if (st == SDNN_OK) st = sum_slabs(sp.slabs, p.splits, ld_slab, e, stream, "linear");
+      }
     }
   }
   return st;
@@ -627,9 +660,14 @@ sdnn_status linear(const Sizes &s, const void *x, int64_t ldx, const uint8_t *co
   Carver c{(char *)workspace};
   const Space sp(c, s);
   if (s.few()) {
-    const Few<T> p{(const T *)x, ldx, aligned16(x, ldx, sizeof(T)), (int)s.rows, (int)s.n, codes, (const T *)scales, (const T *)offsets, (int)groups_of(s.n, group), (int)pitch_of(s.n, group),
-                   s.outputs, (T *)out, ldo, sp.slabs, s.ld_slab(), 0, false, 1};
-    return few_of<T>(p, FewPlan(s.rows, s.outputs, s.n, s.dtype), group, stream);
+    for (int64_t r = 0; r < s.rows; r += kFewRows) {
+      const int m = (int)std::min(s.rows - r, kFewRows);
+      const Few<T> p{(const T *)x + r * ldx, ldx, aligned16(x, ldx, sizeof(T)), m, (int)s.n, codes, (const T *)scales, (const T *)offsets, (int)groups_of(s.n, group), (int)pitch_of(s.n, group),
+                     s.outputs, (T *)out + r * ldo, ldo, sp.slabs, s.ld_slab(), 0, false, 1};
+      const sdnn_status st = few_of<T>(p, FewPlan(m, s.outputs, s.n, s.dtype), group, stream);
+      if (st != SDNN_OK) return st;
+    }
+    return SDNN_OK;
   }
   const auto call = [&](auto kind) { return many<kind(), T>(s, (const T *)x, ldx, codes, (const T *)scales, (const T *)offsets, group, (T *)out, ldo, sp, stream); };
   if constexpr (sizeof(T) == 2)

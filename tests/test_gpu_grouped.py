@@ -26,6 +26,11 @@ def parts_of(codes, scales, offsets, n, group):
     return q, s, o
 
 
+def few(rows, outputs, n, fp32):
+    """Rows whose groups' sums are scaled, by the header's rule."""
+    return rows <= 64 or (outputs >= 4096 and outputs * n >= 1 << 24 and rows <= (256 if fp32 else 128))
+
+
 def reference(x, codes, scales, offsets, group):
     n, fp32 = x.shape[1], x.element_size() == 4
     unit = U32 if fp32 else U16
@@ -35,7 +40,7 @@ def reference(x, codes, scales, offsets, group):
     value = x @ w.t()
     size = x.abs() @ (15 * s.abs() + o.abs()).t()
     e = (n / 16 + 60) * U32 * size
-    if x.shape[0] > 64:
+    if not few(*x.shape[:1], codes.shape[0], n, fp32):
         m = x.abs() @ w.abs().t()
         e = 2 * U32 * size + unit * m + (n / 4 + 40) * U32 * m
         if fp32:
@@ -56,7 +61,8 @@ class Weights:
 
 
 SHAPES = [(1, 1, 1), (1, 10, 31), (2, 17, 33), (3, 300, 1000), (4, 16, 128), (5, 33, 129), (15, 1000, 65), (16, 129, 4096), (17, 40, 300), (31, 9000, 70), (48, 100, 1024), (64, 257, 520),
-          (65, 40, 64), (100, 300, 1000), (193, 193, 97), (300, 1000, 250), (1000, 70, 513), (1, 20000, 200), (1, 40, 20001), (16, 30, 16384), (7, 50, 40000), (300, 250, 4000)]
+          (65, 40, 64), (100, 300, 1000), (193, 193, 97), (300, 1000, 250), (1000, 70, 513), (1, 20000, 200), (1, 40, 20001), (16, 30, 16384), (7, 50, 40000), (300, 250, 4000), (65, 4100, 4100),
+          (128, 4096, 4096), (129, 4097, 4099), (256, 4096, 4096), (257, 4100, 4100), (100, 4095, 4200)]
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
