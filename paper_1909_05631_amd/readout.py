@@ -31,22 +31,20 @@ def _on_gpu(name: str, t, like=None):
 
 
 def _rows(name: str, t, rows, cols, dtype, like=None) -> tuple[int, int]:
-    """Address and row stride of a matrix of rows x cols (None: any) and `dtype`. A call asks it of each of its matrices: what is
-    right is found so in the first lines."""
-    if isinstance(t, torch.Tensor) and t.dim() == 2 and t.dtype == dtype:
-        (m, n), (ld, step), device = t.shape, t.stride(), t.get_device()
-        if (device >= 0 and (like is None or device == like.get_device()) and (rows is None or m == rows) and (cols is None or n == cols)
-                and (step == 1 or n <= 1) and (ld >= n or m <= 1)):
-            return t.data_ptr(), ld if m > 1 else n
+    """Address and row stride of a matrix of rows x cols (None: any) and `dtype`."""
     _on_gpu(name, t, like)
     shape = t.shape
     if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         raise ValueError(f"{name} has shape {tuple(shape)}, not ({rows}, {cols})")
     if t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype}, not {dtype}")
-    if shape[1] > 1 and t.stride(1) != 1:
+    m, n = shape
+    ld, step = t.stride()
+    if n > 1 and step != 1:
         raise ValueError(f"the values within a row of {name} are not contiguous")
-    raise ValueError(f"the rows of {name} overlap")
+    if m > 1 and ld < n:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.data_ptr(), ld if m > 1 else n
 
 
 def _vector(name: str, t, n: int, dtype, like) -> int:
