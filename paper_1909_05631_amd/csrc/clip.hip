@@ -1,20 +1,23 @@
 // The common norm of a list of tensors, n = sqrt(sum of v^2 over all of them), and the list scaled by min(1, most / n).
 //
 // The list is cut into pieces of one size, about 2048 for all of it (8 workgroups a CU, all resident at once, so that none
-// waits for another). One launch for every 64 tensors, whose descriptions travel as its arguments, leaves each piece's sum of
-// squares and its description in the workspace; one more goes over all pieces: every workgroup sums the pieces' sums for
+// waits for another). One launch for every 136 tensors (64 where one has rows apart from each other), whose descriptions
+// travel as its arguments, leaves each piece's sum of squares and its description in the workspace; one more goes over all pieces: every workgroup sums the pieces' sums for
 // itself, in the same order, and scales its piece. Neither waits for the host, and no sum depends on the order of
 // arrival: the same list gives the same bits.
 //
 // Squares and sums are taken in 64 bits: a list's norm is exact to its rounding to fp32 whatever the values' sizes (squares of
 // 1e-45 and of 3e38 are normal numbers there), and memory still bounds the pass.
+// Bound by memory for large lists, which are read twice and written once: 16 tensors of 2.6 GB together 1.57 ms, 0.48 for the
+// squares (5.3 TB/s) and 1.09 for the rest (4.7); a copy runs at 4.9. By launches and by the list's description for small ones: 3 of
+// 4 MB together 17 us, of which the kernels take 8; 240 of 77 MB 138 us, 113 of them in the binding (64 us on the card).
 #include "dense.h"
 
 using namespace dense;
 
 namespace {
 
-constexpr int kMaxTensors = 4096, kBatch = 64, kPieces = 2048;
+constexpr int kMaxTensors = 4096, kPieces = 2048;
 constexpr int64_t kLeastPiece = 8192, kUnit = 4096;  // bytes
 constexpr int64_t kSegment = 4096;                   // bytes of a strided row that a workgroup takes by itself
 
@@ -26,18 +29,42 @@ struct Piece {
   int dtype, contiguous;
 };
 
-// Tensors of one launch, and the first of each one's pieces there.
-struct Tensor {
-  const void *in;
-  void *out;
-  int64_t rows, cols, ld, ldo;
-  int first, dtype;
+// Tensors of one launch, and the first of each one's pieces there: contiguous ones, or any. (A launch's arguments stay
+// below 4 KB.)
+template <int COUNT>
+struct List {
+  static constexpr int kMost = COUNT;
+  const void *in[COUNT];
+  void *out[COUNT];
+  int first[COUNT];
+  int count, first_piece;  // tensors, and the launch's first piece
+  int64_t bytes;           // of a piece
 };
-struct Batch {
-  Tensor of[kBatch];
-  int count, first;  // of the launch's pieces
-  int64_t bytes;     // of a piece
+struct Contiguous : List<136> {
+  int64_t size[136];  // values, twice, and one more for bf16
+  __host__ void set(int i, int64_t, int64_t cols, int64_t, int64_t, int dtype) { size[i] = cols * 2 + (dtype == SDNN_BF16); }
+  __device__ int dtype(int i) const { return size[i] & 1 ? SDNN_BF16 : SDNN_FP32; }
+  __device__ Piece piece(int i, int64_t start, int64_t per) const {
+    const int64_t all = size[i] >> 1;
+    return {in[i], out[i], start, min(per, all - start), all, 0, 0, dtype(i), true};
+  }
 };
+struct Strided : List<64> {
+  int64_t rows[64], cols[64], ld[64], ldo[64];
+  int8_t kind[64];
+  __host__ void set(int i, int64_t r, int64_t c, int64_t l, int64_t lo, int dtype) {
+    rows[i] = r;
+    cols[i] = c;
+    ld[i] = l;
+    ldo[i] = lo;
+    kind[i] = (int8_t)dtype;
+  }
+  __device__ int dtype(int i) const { return kind[i]; }
+  __device__ Piece piece(int i, int64_t start, int64_t per) const {
+    return {in[i], out[i], start, min(per, rows[i] * cols[i] - start), cols[i], ld[i], ldo[i], kind[i], rows[i] == 1};
+  }
+};
+static_assert(sizeof(Contiguous) <= 4000 && sizeof(Strided) <= 4000, "a launch's arguments");
 
 template <class T>
 using Chunk = T __attribute__((ext_vector_type(16 / sizeof(T))));
@@ -94,17 +121,21 @@ __device__ __forceinline__ double sum_of_workgroup(double v) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__global__ __launch_bounds__(256) void k_squares(const Batch batch, Piece *pieces, double *sums) {
+template <class L>
+__global__ __launch_bounds__(256) void k_squares(const L list, Piece *pieces, double *sums) {
   const int lane = threadIdx.x & 63, b = blockIdx.x;
   // the last tensor whose pieces begin at or before this one
-  const uint64_t before = __ballot(lane < batch.count && batch.of[lane < batch.count ? lane : 0].first <= b);
-  const Tensor &t = batch.of[__popcll(before) - 1];
-  const int64_t per = batch.bytes / (t.dtype == SDNN_BF16 ? 2 : 4), start = (b - t.first) * per, all = t.rows * t.cols;
-  const Piece p{t.in, t.out, start, min(per, all - start), t.cols, t.ld, t.ldo, t.dtype, t.rows == 1 || (t.ld == t.cols && t.ldo == t.cols)};
-  const double sum = sum_of_workgroup(t.dtype == SDNN_BF16 ? squares_of<__bf16>(p) : squares_of<float>(p));
+  int at = -1;
+#pragma unroll
+  for (int i = 0; i < L::kMost; i += 64) at += __popcll(__ballot(i + lane < list.count && list.first[min(i + lane, L::kMost - 1)] <= b));
+  at = tile::uniform(at);
+  const int dtype = list.dtype(at);
+  const int64_t per = list.bytes / (dtype == SDNN_BF16 ? 2 : 4);
+  const Piece p = list.piece(at, (b - list.first[at]) * per, per);
+  const double sum = sum_of_workgroup(dtype == SDNN_BF16 ? squares_of<__bf16>(p) : squares_of<float>(p));
   if (threadIdx.x == 0) {
-    pieces[batch.first + b] = p;
-    sums[batch.first + b] = sum;
+    pieces[list.first_piece + b] = p;
+    sums[list.first_piece + b] = sum;
   }
 }
 
@@ -225,32 +256,47 @@ sdnn_status check_list(const sdnn_tensor *tensors, int64_t n, bool clip) {
 }
 
 // The pieces' sums and descriptions; `total` of them.
-sdnn_status squares(const sdnn_tensor *tensors, int64_t n, const Space &sp, int *total, hipStream_t stream) {
-  int64_t bytes = 0;
-  for (int64_t i = 0; i < n; ++i) bytes += tensors[i].rows * tensors[i].cols * dtype_bytes(tensors[i].dtype);
-  Batch batch;
-  batch.bytes = std::max(kLeastPiece, ceil_div(ceil_div(bytes, kPieces), kUnit) * kUnit);
-  batch.count = 0;
-  batch.first = 0;
+bool contiguous(const sdnn_tensor &t) { return t.rows <= 1 || (t.ld == t.cols && (!t.out || t.ldo == t.cols)); }
+
+template <class L>
+sdnn_status squares_of_list(const sdnn_tensor *tensors, int64_t n, int64_t piece, const Space &sp, int *total, hipStream_t stream) {
+  L list;
+  list.bytes = piece;
+  list.count = list.first_piece = 0;
   int here = 0;  // pieces of this launch
   for (int64_t i = 0; i < n; ++i) {
     const sdnn_tensor &t = tensors[i];
     const int64_t size = t.rows * t.cols * dtype_bytes(t.dtype);
     if (size > 0) {
-      const bool flat = t.rows == 1 || (t.ld == t.cols && (!t.out || t.ldo == t.cols));
-      batch.of[batch.count++] = {t.data, t.out ? t.out : t.data, flat ? 1 : t.rows, flat ? t.rows * t.cols : t.cols, t.ld, t.out ? t.ldo : t.ld, here, t.dtype};
-      here += (int)ceil_div(size, batch.bytes);
+      const int k = list.count++;
+      const bool flat = contiguous(t);
+      list.in[k] = t.data;
+      list.out[k] = t.out ? t.out : t.data;
+      list.first[k] = here;
+      list.set(k, flat ? 1 : t.rows, flat ? t.rows * t.cols : t.cols, t.ld, t.out ? t.ldo : t.ld, t.dtype);
+      here += (int)ceil_div(size, piece);
     }
-    if (batch.count == kBatch || (i == n - 1 && batch.count > 0)) {
-      hipLaunchKernelGGL(k_squares, dim3((unsigned)here), dim3(256), 0, stream, batch, sp.pieces, sp.sums);
+    if (list.count == L::kMost || (i == n - 1 && list.count > 0)) {
+      hipLaunchKernelGGL((k_squares<L>), dim3((unsigned)here), dim3(256), 0, stream, list, sp.pieces, sp.sums);
       const sdnn_status st = launched("squares");
       if (st != SDNN_OK) return st;
-      batch.first += here;
-      batch.count = here = 0;
+      list.first_piece += here;
+      list.count = here = 0;
     }
   }
-  *total = batch.first;
+  *total = list.first_piece;
   return SDNN_OK;
+}
+
+sdnn_status squares(const sdnn_tensor *tensors, int64_t n, const Space &sp, int *total, hipStream_t stream) {
+  int64_t bytes = 0;
+  bool flat = true;
+  for (int64_t i = 0; i < n; ++i) {
+    bytes += tensors[i].rows * tensors[i].cols * dtype_bytes(tensors[i].dtype);
+    flat = flat && contiguous(tensors[i]);
+  }
+  const int64_t piece = std::max(kLeastPiece, ceil_div(ceil_div(bytes, kPieces), kUnit) * kUnit);
+  return flat ? squares_of_list<Contiguous>(tensors, n, piece, sp, total, stream) : squares_of_list<Strided>(tensors, n, piece, sp, total, stream);
 }
 
 }  // namespace

@@ -96,6 +96,28 @@ def test_strided_rows_and_odd_addresses(kind):
     assert [t._base.isnan().sum() for t in tensors] == gaps
 
 
+def test_more_strided_matrices_than_one_launch_takes():
+    """150 narrow matrices of rows apart from each other, contiguous and empty ones among them."""
+    from paper_1909_05631_amd import readout
+    torch = torch_cuda()
+    log("clip many strided")
+    tensors = []
+    for i in range(150):
+        wide = torch.full((5 + i % 7, 40 + i), float("nan"), dtype=(torch.float32, torch.bfloat16)[i % 2], device="cuda")
+        t = wide[:, 3:3 + (i * 5) % 37] if i % 5 else wide[1:3]
+        t.copy_(torch.randn(t.shape, device="cuda"))
+        tensors.append(t)
+    before = [t.clone() for t in tensors]
+    gaps = [t._base.isnan().sum() for t in tensors]
+    ws, norm = workspace(readout, torch, len(tensors)), torch.empty(1, device="cuda")
+    outs = [torch.empty_like(t, memory_format=torch.contiguous_format) for t in tensors]
+    readout.clip(tensors, 3.0, norm, ws, out=outs)
+    check(torch, before, outs, norm, 3.0)
+    readout.clip(tensors, 3.0, norm, ws)
+    check(torch, before, tensors, norm, 3.0)
+    assert [t._base.isnan().sum() for t in tensors] == gaps
+
+
 def test_halves_of_one_matrix():
     """Two column halves share their rows' memory and overlap nowhere."""
     from paper_1909_05631_amd import readout
