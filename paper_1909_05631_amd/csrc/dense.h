@@ -269,11 +269,21 @@ struct Matrix {
   }
 };
 
-template <class B, int KIND, int BM, int BN, bool ACROSS_A, bool ACROSS_B, bool TWO_B, class Epilogue>
-__global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blocks blocks, Epilogue epilogue) {
+// What the last workgroups of a product's launch do besides: nothing, or work that was ready before it.
+struct NoTail {
+  static constexpr bool kAny = false;
+  int blocks() const { return 0; }
+};
+
+template <class B, int KIND, int BM, int BN, bool ACROSS_A, bool ACROSS_B, bool TWO_B, class Epilogue, class Tail>
+__global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blocks blocks, Epilogue epilogue, Tail tail) {
   __shared__ __attribute__((aligned(1024))) char lds[B::kLds];
-  int r, c, split;
-  blocks.locate(blockIdx.x, gridDim.x, r, c, split);
+  int r, c, split, total = gridDim.x;
+  if constexpr (Tail::kAny) {
+    total -= tail.blocks();
+    if ((int)blockIdx.x >= total) return tail(blockIdx.x - total, B::kThreads, lds);
+  }
+  blocks.locate(blockIdx.x, total, r, c, split);
   r = tile::uniform(r);
   c = tile::uniform(c);
   int s0, s1;
@@ -285,21 +295,21 @@ __global__ __launch_bounds__(B::kThreads) void k_product(Matrix a, Matrix b, Blo
 }
 
 // Launches the blocks of one shape. What the sizes need of it is the caller's rule.
-template <int KIND, int BM, int BN, int WM, int WN, int STAGES, int GROUPS, bool ACROSS_A, bool ACROSS_B, bool TWO_B = false, class Epilogue>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES, int GROUPS, bool ACROSS_A, bool ACROSS_B, bool TWO_B = false, class Epilogue, class Tail>
 sdnn_status launch(const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, int splits, const Epilogue &e, hipStream_t stream, const char *what, bool symmetric,
-                   int batch) {
+                   int batch, const Tail &tail) {
   using B = tile::Block<KIND, BM, BN, WM, WN, ACROSS_A, ACROSS_B, STAGES, GROUPS, TWO_B>;
   Blocks blocks;
   blocks.slabs = (int)ceil_div(k, tile::Geometry<KIND>::kPerSlab) * tile::Geometry<KIND>::kSlabs;
   blocks.per = (int)ceil_div(blocks.slabs, splits);
   blocks.splits = splits;
   const int64_t r = ceil_div(rows, BM), c = ceil_div(cols, BN);
-  const int64_t n = symmetric ? c * (c + 1) / 2 : r * c * splits;
+  const int64_t n = (symmetric ? c * (c + 1) / 2 : r * c * splits) + tail.blocks();
   blocks.symmetric = symmetric;
   if (n * B::kThreads > 0xffffffffll || a.pitch > kMaxPitch || b.pitch > kMaxPitch || b.pitch_second > kMaxPitch) return fail(SDNN_EINVAL, "%s: %lld x %lld outputs are too many for one launch", what, (long long)rows, (long long)cols);
   blocks.rows = (int)r;
   blocks.cols = (int)c;
-  hipLaunchKernelGGL((k_product<B, KIND, BM, BN, ACROSS_A, ACROSS_B, TWO_B, Epilogue>), dim3((unsigned)n, (unsigned)batch), dim3(B::kThreads), 0, stream, a, b, blocks, e);
+  hipLaunchKernelGGL((k_product<B, KIND, BM, BN, ACROSS_A, ACROSS_B, TWO_B, Epilogue, Tail>), dim3((unsigned)n, (unsigned)batch), dim3(B::kThreads), 0, stream, a, b, blocks, e, tail);
   return launched(what);
 }
 
@@ -345,29 +355,30 @@ inline Plan plan(int kind, int64_t rows, int64_t cols, int64_t k, int most_split
 }
 
 // TWO: b is of two matrices (blocks of 192 columns do not split into wave parts of whole pairs).
-template <int KIND, bool AA, bool AB, bool TWO = false, class E>
-sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1) {
+template <int KIND, bool AA, bool AB, bool TWO = false, class E, class Tail = NoTail>
+sdnn_status run_shape(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, bool symmetric = false, int batch = 1,
+                      const Tail &tail = {}) {
   constexpr int kPair = KIND == tile::KIND_MX ? 1 : 2;  // (its scales need LDS too: two blocks a CU instead)
   if constexpr (KIND == tile::KIND_F32) {
     switch (p.shape) {
-      case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-      case kFlat: return launch<KIND, 32, 128, 1, 4, 3, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-      case kTall: return launch<KIND, 128, 32, 4, 1, 3, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-      default: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      case kSmall: return launch<KIND, 64, 64, 2, 2, 4, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+      case kFlat: return launch<KIND, 32, 128, 1, 4, 3, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+      case kTall: return launch<KIND, 128, 32, 4, 1, 3, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+      default: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
     }
   } else {
   switch (p.shape) {
-    case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+    case kWide: return launch<KIND, 256, 256, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
     case kBroad:
-      if constexpr (!AA && !AB && !TWO) return launch<KIND, 256, 192, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      if constexpr (!AA && !AB && !TWO) return launch<KIND, 256, 192, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
     case kMiddle:
-      if constexpr (!AA && !AB && !TWO) return launch<KIND, 192, 192, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kPaired: return launch<KIND, 128, 128, 2, 2, 2, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kStream: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
-    default: return launch<KIND, 128, 32, 4, 1, 3, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch);
+      if constexpr (!AA && !AB && !TWO) return launch<KIND, 192, 192, 2, 4, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+    case kSquare: return launch<KIND, 128, 128, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+    case kPaired: return launch<KIND, 128, 128, 2, 2, 2, 2, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+    case kStream: return launch<KIND, 64, 64, 2, 2, 2, 1, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+    case kSmall: return launch<KIND, 64, 64, 2, 2, 4, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+    case kFlat: return launch<KIND, 32, 128, 1, 4, 3, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
+    default: return launch<KIND, 128, 32, 4, 1, 3, kPair, AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, symmetric, batch, tail);
   }
   }
 }

@@ -581,25 +581,32 @@ sdnn_status grad_of(const Sizes &s, const Inputs<T> &in, int activation, const K
   if (st != SDNN_OK) return st;
   const int64_t per_value = kProduct == KIND_THREE ? 2 : (int64_t)sizeof(T), ld = s.ld_slab();
   const Matrix d{sp.slopes, s.slopes_pitch(), s.rows, 2 * s.half() * per_value, 0};
+  // dx's split sums are joined by the weights' launch where there is one
+  const Store<T> ex{to.dx, to.lddx, s.rows, s.features, vector_rows(to.dx, to.lddx)};
+  SumTail<Store<T>> tail{nullptr, 0, 0, 1, ld, ex};
   if (to.dx) {
-    const Store<T> e{to.dx, to.lddx, s.rows, s.features, vector_rows(to.dx, to.lddx)};
+    const char *what = "gated gradient of the rows";
     if (sp.dx.splits == 1) {
-      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), e, stream, "gated gradient of the rows");
+      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), ex, stream, what);
     } else {
-      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), Accumulate{sp.dx_slabs, ld, s.rows, s.features, false}, stream, "gated gradient of the rows");
-      if (st == SDNN_OK) st = sum_slabs(sp.dx_slabs, sp.dx.splits, ld, e, stream, "gated gradient of the rows");
+      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), Accumulate{sp.dx_slabs, ld, s.rows, s.features, false}, stream, what);
+      if (weights)
+        tail = sum_tail(sp.dx_slabs, sp.dx.splits, ld, ex);
+      else if (st == SDNN_OK)
+        st = sum_slabs(sp.dx_slabs, sp.dx.splits, ld, ex, stream, what);
     }
     if (st != SDNN_OK) return st;
   }
   if (weights) {
+    const char *what = "gated gradient of the weights";
     const int64_t rows = s.half() + s.hidden;
     const TwoStores<T> e{to.dwg, to.dwu, to.lddg, to.lddu, s.hidden, s.half(), rows, s.features,
                          (!to.dwg || vector_rows(to.dwg, to.lddg)) && (!to.dwu || vector_rows(to.dwu, to.lddu))};
     if (sp.dw.splits == 1) {
-      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, e, stream, "gated gradient of the weights");
+      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, e, stream, what, false, 1, tail);
     } else {
-      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, Accumulate{sp.dw_slabs, ld, rows, s.features, false}, stream, "gated gradient of the weights");
-      if (st == SDNN_OK) st = sum_slabs(sp.dw_slabs, sp.dw.splits, ld, e, stream, "gated gradient of the weights");
+      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, Accumulate{sp.dw_slabs, ld, rows, s.features, false}, stream, what, false, 1, tail);
+      if (st == SDNN_OK) st = sum_slabs(sp.dw_slabs, sp.dw.splits, ld, e, stream, what);
     }
   }
   return st;

@@ -38,16 +38,15 @@ struct Store {
   }
 };
 
-// The slabs' sum, rounded to the output's type: 256 / GROUPS items a workgroup, each group taking every GROUPS-th slab. S: a
-// Store, or another that says where a row goes (nullptr: nowhere).
+// The slabs' sum, rounded to the output's type: THREADS / GROUPS items a workgroup, each group taking every GROUPS-th slab. S:
+// a Store, or another that says where a row goes (nullptr: nowhere). `shared`: an f32x4 a thread.
 template <class S, int GROUPS>
-__global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int splits, int64_t ld_slab, S to) {
-  constexpr int kItems = 256 / GROUPS;
-  __shared__ f32x4 shared[GROUPS][kItems];
+__device__ __forceinline__ void sum_of_slabs(const float *slabs, int splits, int64_t ld_slab, const S &to, int block, int blocks, int threads, f32x4 *shared) {
+  const int items = threads / GROUPS;
   const int64_t per = ld_slab / 4, total = to.rows * per;
   const float by = to.factor ? *to.factor : 1.0f;
-  const int group = threadIdx.x / kItems, item = threadIdx.x % kItems;
-  for (int64_t i0 = (int64_t)blockIdx.x * kItems; i0 < total; i0 += (int64_t)gridDim.x * kItems) {
+  const int group = threadIdx.x / items, item = threadIdx.x % items;
+  for (int64_t i0 = (int64_t)block * items; i0 < total; i0 += (int64_t)blocks * items) {
     const int64_t i = i0 + item, r = i / per, c = (i - r * per) * 4;
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (i < total)
@@ -55,10 +54,10 @@ __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int split
       for (int s = group; s < splits; s += GROUPS) v += *(const f32x4 *)(slabs + (s * to.rows + r) * ld_slab + c);
     if constexpr (GROUPS > 1) {
       __syncthreads();
-      shared[group][item] = v;
+      shared[threadIdx.x] = v;
       __syncthreads();
       if (group == 0)
-        for (int g = 1; g < GROUPS; ++g) v += shared[g][item];
+        for (int g = 1; g < GROUPS; ++g) v += shared[g * items + item];
     }
     if (group == 0 && i < total && c < to.cols) {
       typename S::Value *out = to.row(r);
@@ -66,17 +65,50 @@ __global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int split
     }
   }
 }
+template <class S, int GROUPS>
+__global__ __launch_bounds__(256) void k_sum_slabs(const float *slabs, int splits, int64_t ld_slab, S to) {
+  __shared__ f32x4 shared[256];
+  sum_of_slabs<S, GROUPS>(slabs, splits, ld_slab, to, blockIdx.x, gridDim.x, 256, shared);
+}
+inline int sum_groups(int splits) { return splits >= 32 ? 16 : splits >= 8 ? 4 : 1; }
 
 template <class S>
 sdnn_status sum_slabs(const float *slabs, int splits, int64_t ld_slab, const S &to, hipStream_t stream, const char *what) {
   const int64_t items = to.rows * (ld_slab / 4);
-  if (splits >= 32)
-    hipLaunchKernelGGL((k_sum_slabs<S, 16>), dim3((unsigned)std::min<int64_t>(ceil_div(items, 16), 8192)), dim3(256), 0, stream, slabs, splits, ld_slab, to);
-  else if (splits >= 8)
-    hipLaunchKernelGGL((k_sum_slabs<S, 4>), dim3((unsigned)std::min<int64_t>(ceil_div(items, 64), 8192)), dim3(256), 0, stream, slabs, splits, ld_slab, to);
+  const int groups = sum_groups(splits);
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(items, 256 / groups), 8192));
+  if (groups == 16)
+    hipLaunchKernelGGL((k_sum_slabs<S, 16>), grid, dim3(256), 0, stream, slabs, splits, ld_slab, to);
+  else if (groups == 4)
+    hipLaunchKernelGGL((k_sum_slabs<S, 4>), grid, dim3(256), 0, stream, slabs, splits, ld_slab, to);
   else
-    hipLaunchKernelGGL((k_sum_slabs<S, 1>), dim3((unsigned)std::min<int64_t>(ceil_div(items, 256), 8192)), dim3(256), 0, stream, slabs, splits, ld_slab, to);
+    hipLaunchKernelGGL((k_sum_slabs<S, 1>), grid, dim3(256), 0, stream, slabs, splits, ld_slab, to);
   return launched(what);
+}
+
+// The same by the last workgroups of the next product's launch, for one launch less (none: count is 0).
+template <class S>
+struct SumTail {
+  static constexpr bool kAny = true;
+  const float *slabs;
+  int splits, count, groups;
+  int64_t ld_slab;
+  S to;
+  __host__ __device__ int blocks() const { return count; }
+  __device__ __forceinline__ void operator()(int block, int threads, char *lds) const {
+    if (groups == 16)
+      sum_of_slabs<S, 16>(slabs, splits, ld_slab, to, block, count, threads, (f32x4 *)lds);
+    else if (groups == 4)
+      sum_of_slabs<S, 4>(slabs, splits, ld_slab, to, block, count, threads, (f32x4 *)lds);
+    else
+      sum_of_slabs<S, 1>(slabs, splits, ld_slab, to, block, count, threads, (f32x4 *)lds);
+  }
+};
+template <class S>
+SumTail<S> sum_tail(const float *slabs, int splits, int64_t ld_slab, const S &to) {
+  const int groups = sum_groups(splits);
+  const int64_t items = to.rows * (ld_slab / 4);
+  return {slabs, splits, (int)std::min<int64_t>(ceil_div(items, 256 / groups), 1024), groups, ld_slab, to};
 }
 
 // Rows that the tiles read as they are: whole dwords.
