@@ -12,8 +12,8 @@
 // sum, and [dwg; dwu] = [dg du]^T x. Nothing is transposed or concatenated in memory.
 //
 // fp32: the layer's sums run along rows of x and w, which take a power of two each and go in two fp16 parts; the gradient's run
-// across rows of any size, so dg, du, w and x go there in three bf16 parts, which need no scale. Where rows or outputs are at most
-// 192 all go to the fp32 matrix instructions as they are. Up to 16 rows have a kernel of their own (k_few_rows).
+// across rows of any size, so dg, du, w and x go there in three bf16 parts, which need no scale. Where rows or outputs are few
+// all go to the fp32 matrix instructions as they are. Up to 16 rows have a kernel of their own (k_few_rows).
 //
 // What bounds it, measured on this card (a copy runs at 4.9 TB/s, the library's bf16 product at 1633 TFLOP/s):
 //   8192 x 4096 to 16384, bf16: 5.45 ms, matrix instructions: the layer 1.75 ms (1260 TFLOP/s; 0.1 ms of it for keeping g and
@@ -28,6 +28,8 @@
 #include "copies.h"
 #include "sums.h"
 
+#include <utility>
+
 using namespace dense;
 using namespace copies;
 using namespace sums;
@@ -40,8 +42,12 @@ using tile::KIND_THREE;
 namespace {
 
 constexpr int64_t kMaxHidden = 1 << 19;    // a row of dg and du in three parts is then the longest that the tiles take
-constexpr int64_t kSplitValues = 1 << 24;  // values of g and u whose features may be split
-constexpr int64_t kPlain = 192;            // fp32 rows or outputs for the plain fp32 products
+constexpr int64_t kSplitValues = 1 << 24;  // values of g and u whose features may be split: past that there is a 256 x 256 block for every CU
+// fp32 rows or outputs (the fewer of the two) for the plain fp32 products, which read the operands as they are: the layer's, and its
+// gradient's. us, plain and in parts, 1000 to 2048: the layer 64 rows 18 / 25, 192 rows 26 / 26, 300 rows 43 / 32, the gradient 64
+// rows 29 / 40, 192 47 / 61, 300 70 / 86, 512 92 / 95; 4096 to 8192: the layer 128 rows 147 / 211, 192 210 / 238, 300 402 / 271, the
+// gradient 192 444 / 502, 300 723 / 736, 400 1025 / 772.
+constexpr int64_t kPlain = 192, kPlainGradient = 300;
 
 // act(g) and, for the gradient, act'(g).
 struct Activated {
@@ -413,7 +419,7 @@ struct Sizes {
   int64_t rows, hidden, features;
   int32_t dtype;
   int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, hidden) <= kPlain ? KIND_F32 : KIND_SPLIT; }
-  int product_kind() const { return kind() == KIND_SPLIT ? KIND_THREE : kind(); }
+  int product_kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, hidden) <= kPlainGradient ? KIND_F32 : KIND_THREE; }  // the gradient's
   int bytes() const { return dtype_bytes(dtype); }
   // Bytes of a row of features written anew, as the layer and as the gradient take it.
   int64_t pitch(int kind) const {
@@ -521,7 +527,8 @@ struct Kept {
   int64_t ldg, ldu;
 };
 
-// Few rows whose weights are read where they are.
+// Few rows whose weights are read where they are. us, here and in tiles: bf16 1 x 1024 to 4096 8.3 / 10.1, 1 x 4096 to 16384 50 / 64,
+// 16 x 4096 to 16384 55 / 68, 8 x 16384 to 4096 62 / 63; fp32 1 x 4096 to 8192 58 / 70, 16 x 1000 to 100 9.8 / 10.1.
 template <class T>
 bool few_rows(const Sizes &s, const Inputs<T> &in) {
   return s.rows <= 16 && s.rows * (int64_t)stage_pitch(steps_of<T>((int)s.features)) <= kRoom<16> && usable_in_place(in.wg, in.ldg, s.features, sizeof(T)) &&
@@ -574,9 +581,8 @@ struct Gradients {
   int64_t lddx, lddg, lddu;
 };
 
-template <int KIND, class T>
+template <int kProduct, class T>
 sdnn_status grad_of(const Sizes &s, const Inputs<T> &in, int activation, const Kept<T> &kept, const T *dh, int64_t lddh, const Gradients<T> &to, Carver &carver, hipStream_t stream) {
-  constexpr int kProduct = KIND == KIND_SPLIT ? KIND_THREE : KIND;
   const GradSpace sp(carver, s);
   const bool weights = to.dwg || to.dwu;
   const Slopes<T> p{kept.gate, kept.up, dh, kept.ldg, kept.ldu, lddh, vector_rows(kept.gate, kept.ldg) && vector_rows(kept.up, kept.ldu) && vector_rows(dh, lddh), activation,
@@ -659,26 +665,26 @@ size_t workspace_of(const Sizes &s, int gradient) {
   return std::max(layer.used, grad.used);
 }
 
-template <int KIND, class T>
-sdnn_status layer_call(const Sizes &s, const void *x, int64_t ldx, const void *wg, int64_t ldg, const void *wu, int64_t ldu, int32_t activation, void *h, int64_t ldh, void *gate, int64_t ldgate, void *up,
-                       int64_t ldup, void *workspace, hipStream_t stream) {
-  Carver c{(char *)workspace};
-  return layer_of<KIND, T>(s, {(const T *)x, (const T *)wg, (const T *)wu, ldx, ldg, ldu}, activation, (T *)h, ldh, {(T *)gate, (T *)up, ldgate, ldup}, c, stream);
+template <class T>
+sdnn_status layer_call(const Sizes &s, const Inputs<T> &in, int activation, T *h, int64_t ldh, const Kept<T> &kept, Carver &c, hipStream_t stream) {
+  if constexpr (sizeof(T) == 2)
+    return layer_of<KIND_BF16>(s, in, activation, h, ldh, kept, c, stream);
+  else
+    return s.kind() == KIND_F32 ? layer_of<KIND_F32>(s, in, activation, h, ldh, kept, c, stream) : layer_of<KIND_SPLIT>(s, in, activation, h, ldh, kept, c, stream);
 }
 
-template <int KIND, class T>
-sdnn_status grad_call(const Sizes &s, const void *x, int64_t ldx, const void *wg, int64_t ldg, const void *wu, int64_t ldu, int32_t activation, const void *gate, int64_t ldgate, const void *up, int64_t ldup,
-                      const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dwg, int64_t lddg, void *dwu, int64_t lddu, void *workspace, hipStream_t stream) {
-  const Inputs<T> in{(const T *)x, (const T *)wg, (const T *)wu, ldx, ldg, ldu};
-  Carver c{(char *)workspace};
-  Kept<T> kept{(T *)gate, (T *)up, ldgate, ldup};
-  if (!gate) {
+template <class T>
+sdnn_status grad_call(const Sizes &s, const Inputs<T> &in, int activation, Kept<T> kept, const T *dh, int64_t lddh, const Gradients<T> &to, Carver c, hipStream_t stream) {
+  if (!kept.gate) {
     kept = again_space<T>(c, s);
     Carver over = c;
-    const sdnn_status st = layer_of<KIND, T>(s, in, activation, nullptr, 0, kept, over, stream);
+    const sdnn_status st = layer_call<T>(s, in, activation, nullptr, 0, kept, over, stream);
     if (st != SDNN_OK) return st;
   }
-  return grad_of<KIND, T>(s, in, activation, kept, (const T *)dh, lddh, {(T *)dx, (T *)dwg, (T *)dwu, lddx, lddg, lddu}, c, stream);
+  if constexpr (sizeof(T) == 2)
+    return grad_of<KIND_BF16>(s, in, activation, kept, dh, lddh, to, c, stream);
+  else
+    return s.product_kind() == KIND_F32 ? grad_of<KIND_F32>(s, in, activation, kept, dh, lddh, to, c, stream) : grad_of<KIND_THREE>(s, in, activation, kept, dh, lddh, to, c, stream);
 }
 
 template <class T>
@@ -709,8 +715,12 @@ sdnn_status sdnn_gated(const void *x, int64_t ldx, const void *w_gate, int64_t l
   const Sizes s{n_rows, n_hidden, n_features, dtype};
   if ((st = check_workspace(workspace, workspace_bytes, workspace_of(s, kLayerOnly))) != SDNN_OK) return st;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const auto call = s.kind() == KIND_BF16 ? layer_call<KIND_BF16, __bf16> : s.kind() == KIND_F32 ? layer_call<KIND_F32, float> : layer_call<KIND_SPLIT, float>;
-  return call(s, x, ldx, w_gate, ldw_gate, w_up, ldw_up, activation, h, ldh, gate, ldgate, up, ldup, workspace, stream);
+  const auto call = [&](auto value) {
+    using T = decltype(value);
+    Carver c{(char *)workspace};
+    return layer_call<T>(s, {(const T *)x, (const T *)w_gate, (const T *)w_up, ldx, ldw_gate, ldw_up}, activation, (T *)h, ldh, {(T *)gate, (T *)up, ldgate, ldup}, c, stream);
+  };
+  return dtype == SDNN_BF16 ? call((__bf16)0.0f) : call(0.0f);
 }
 
 sdnn_status sdnn_gated_grad(const void *x, int64_t ldx, const void *w_gate, int64_t ldw_gate, const void *w_up, int64_t ldw_up, int32_t dtype, int32_t activation, const void *gate, int64_t ldgate,
@@ -739,8 +749,12 @@ sdnn_status sdnn_gated_grad(const void *x, int64_t ldx, const void *w_gate, int6
     return launched("gated gradient");
   }
   if ((st = check_workspace(workspace, workspace_bytes, workspace_of(s, gate ? kFromKept : kAgain))) != SDNN_OK) return st;
-  const auto call = s.kind() == KIND_BF16 ? grad_call<KIND_BF16, __bf16> : s.kind() == KIND_F32 ? grad_call<KIND_F32, float> : grad_call<KIND_SPLIT, float>;
-  return call(s, x, ldx, w_gate, ldw_gate, w_up, ldw_up, activation, gate, ldgate, up, ldup, dh, lddh, dx, lddx, dw_gate, lddw_gate, dw_up, lddw_up, workspace, stream);
+  const auto call = [&](auto value) {
+    using T = decltype(value);
+    return grad_call<T>(s, {(const T *)x, (const T *)w_gate, (const T *)w_up, ldx, ldw_gate, ldw_up}, activation, {(T *)gate, (T *)up, ldgate, ldup}, (const T *)dh, lddh,
+                        {(T *)dx, (T *)dw_gate, (T *)dw_up, lddx, lddw_gate, lddw_up}, Carver{(char *)workspace}, stream);
+  };
+  return dtype == SDNN_BF16 ? call((__bf16)0.0f) : call(0.0f);
 }
 
 }  // extern "C"

@@ -35,8 +35,10 @@ constexpr int64_t kManyWeights = 1 << 24, kManyOutputs = 4096;  // see Sizes::fe
 // Weights that are written as values at a time. Fewer (2^26 bf16 values would stay in the Infinity Cache) leave the products too
 // few blocks: 64 rows to 16384 x 16384 360 us so, 336 at once, 2000 rows 1300 us and 1140.
 constexpr int64_t kPieceValues = 1 << 28;
-constexpr int64_t kSplitResults = 1 << 24;     // results of a product whose k may be split
-constexpr int64_t kPlain = 192;                // fp32 rows or outputs for the plain fp32 products
+constexpr int64_t kSplitResults = 1 << 24;  // results of a product whose k may be split: past that there is a 256 x 256 block for every CU
+// fp32 rows or outputs (the fewer of the two) for the plain fp32 products. us, plain and in two fp16 parts: 192 x 1000 to 2048 27 / 32,
+// 1000 x 1000 to 192 19 / 26, 300 x 1000 to 2048 33 / 33, 300 x 4096 to 8192 229 / 210, 600 x 600 to 600 22 / 22.
+constexpr int64_t kPlain = 192;
 
 __host__ __device__ inline int64_t groups_of(int64_t n, int group) { return ceil_div(n, group); }
 __host__ __device__ inline int64_t pitch_of(int64_t n, int group) { return groups_of(n, group) * (group / 2); }  // bytes of a row of codes

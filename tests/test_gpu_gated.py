@@ -104,7 +104,8 @@ class Case:
 
 
 SHAPES = [(1, 1, 1), (1, 16, 64), (1, 300, 1000), (2, 17, 3), (3, 1000, 130), (4, 33, 31), (5, 100, 257), (16, 129, 65), (17, 64, 128), (33, 31, 40), (64, 256, 128), (100, 10, 1024), (200, 193, 72),
-          (257, 1000, 72), (300, 2047, 40), (1021, 130, 500), (700, 700, 260), (2500, 300, 33), (3, 9000, 64), (1, 40, 9000), (300, 20, 5000)]
+          (257, 1000, 72), (300, 2047, 40), (1021, 130, 500), (700, 700, 260), (2500, 300, 33), (3, 9000, 64), (1, 40, 9000), (300, 20, 5000), (192, 500, 65), (193, 500, 65), (300, 500, 65), (301, 500, 65),
+          (500, 192, 65), (500, 301, 65), (700, 300, 65)]
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
@@ -227,7 +228,7 @@ def test_large_and_small_gates():
 def test_rows_of_very_different_size():
     """fp32: a row or an output far larger than the others leaves these their precision."""
     log("gated wide range")
-    for rows, hidden in ((40, 50), (300, 300)):
+    for rows, hidden in ((40, 50), (300, 300), (310, 305)):
         c = Case(rows, hidden, 96, "float32", seed=9)
         c.x[7] *= 2.0 ** 40
         c.wu[11] *= 2.0 ** 30
