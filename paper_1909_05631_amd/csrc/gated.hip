@@ -488,7 +488,7 @@ sdnn_status operands(const Sizes &s, const Inputs<T> &in, const Copies &to, bool
   const char *base[3];
   int64_t pitch[3], extent = KIND == KIND_SPLIT ? s.pitch(KIND) : KIND == KIND_THREE ? ceil_div(s.features, 8) * 16 : s.features * (int64_t)sizeof(T);
   constexpr bool kParts = KIND == KIND_SPLIT || KIND == KIND_THREE;
-  // both weights are read in place, or neither: they share one extent
+  // each is read in place or written anew; a row written anew is at least as long as what is read of it
   bool in_place[3];
   for (int i = 0; i < 3; ++i) in_place[i] = !kParts && usable_in_place(data[i], ld[i], s.features, sizeof(T));
   if (s.features * sizeof(T) % 4) extent = s.pitch(KIND);  // no row is usable in place then

@@ -33,7 +33,7 @@ namespace {
 constexpr int64_t kFewRows = 64;               // rows that k_few takes at once
 constexpr int64_t kManyWeights = 1 << 24, kManyOutputs = 4096;  // see Sizes::few
 // Weights that are written as values at a time. Fewer (2^26 bf16 values would stay in the Infinity Cache) leave the products too
-// few blocks: 64 rows to 16384 x 16384 360 us so, 336 at once, 2000 rows 1300 us and 1140.
+// few blocks: 512 x 16384 to 16384 478 us so, 388 at once; 2000 rows 1037 and 960.
 constexpr int64_t kPieceValues = 1 << 28;
 constexpr int64_t kSplitResults = 1 << 24;  // results of a product whose k may be split: past that there is a 256 x 256 block for every CU
 // fp32 rows or outputs (the fewer of the two) for the plain fp32 products. us, plain and in two fp16 parts: 192 x 1000 to 2048 27 / 32,
