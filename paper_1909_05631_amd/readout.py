@@ -299,7 +299,8 @@ def _list(tensors, out, norm):
     if None in codes:
         _dtype(dtypes[codes.index(None)])
     table = np.zeros((n, 7), np.int64)
-    table[:, 0], table[:, 1], table[:, 6] = addresses, to_addresses, codes
+    table[:, 0], table[:, 6] = addresses, codes
+    table[:, 1] = table[:, 0] if to is tensors else to_addresses
     flat = all(map(torch.Tensor.is_contiguous, tensors)) and (to is tensors or all(map(torch.Tensor.is_contiguous, to)))
     shape = torch.Tensor.numel if flat else torch.Tensor.size
     shapes = list(map(shape, tensors))
