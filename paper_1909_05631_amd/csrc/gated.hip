@@ -26,6 +26,7 @@
 #include "dense.h"
 #include "few.h"
 #include "copies.h"
+#include "parts.h"
 #include "sums.h"
 
 #include <utility>
@@ -429,8 +430,14 @@ struct Sizes {
   int64_t half() const { return ceil_div(hidden, 64) * 64; }    // values of dg in a row, whole slabs of any kind
   int64_t slopes_pitch() const { return product_kind() == KIND_THREE ? half() / 64 * 2 * tile::kGroup3 : half() * 2 * bytes(); }
   Plan layer() const { return plan(kind(), rows, paired(), features, rows * paired() <= kSplitValues && rows <= 65535 ? kMaxSplits : 1); }
-  Plan dx() const { return plan(product_kind(), rows, features, 2 * half(), kMaxSplits); }
-  Plan dw() const { return plan(product_kind(), half() + hidden, features, rows, kMaxSplits); }
+  Plan dx() const { return product(rows, features, 2 * half()); }
+  Plan dw() const { return product(half() + hidden, features, rows); }
+  Plan product(int64_t m, int64_t n, int64_t k) const {
+    const Plan p = plan(product_kind(), m, n, k, kMaxSplits);
+    if (product_kind() != KIND_THREE) return p;
+    const parts::Splits at_once = parts::plan(m, n, k, kMaxSplits);
+    return at_once.us < p.us ? Plan{kShapes, at_once.splits, at_once.us} : p;
+  }
   int64_t ld_slab() const { return ceil_div(features, 4) * 4; }
 };
 
@@ -581,6 +588,14 @@ struct Gradients {
   int64_t lddx, lddg, lddu;
 };
 
+// A product of the gradient by its plan: kShapes stands for blocks whose parts lie in LDS at once.
+template <int KIND, bool AA, bool AB, bool TWO, class E, class Tail = NoTail>
+sdnn_status product(const Plan &p, const Matrix &a, const Matrix &b, int64_t rows, int64_t cols, int64_t k, const E &e, hipStream_t stream, const char *what, const Tail &tail = {}) {
+  if constexpr (KIND == KIND_THREE)
+    if (p.shape == kShapes) return parts::launch<AA, AB, TWO>(a, b, rows, cols, k, p.splits, e, stream, what, tail);
+  return run_shape<KIND, AA, AB, TWO>(p, a, b, rows, cols, k, e, stream, what, false, 1, tail);
+}
+
 template <int kProduct, class T>
 sdnn_status grad_of(const Sizes &s, const Inputs<T> &in, int activation, const Kept<T> &kept, const T *dh, int64_t lddh, const Gradients<T> &to, Carver &carver, hipStream_t stream) {
   const GradSpace sp(carver, s);
@@ -601,9 +616,9 @@ sdnn_status grad_of(const Sizes &s, const Inputs<T> &in, int activation, const K
   if (to.dx) {
     const char *what = "gated gradient of the rows";
     if (sp.dx.splits == 1) {
-      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), ex, stream, what);
+      st = product<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), ex, stream, what);
     } else {
-      st = run_shape<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), Accumulate{sp.dx_slabs, ld, s.rows, s.features, false}, stream, what);
+      st = product<kProduct, false, true, true>(sp.dx, d, o.w, s.rows, s.features, 2 * s.half(), Accumulate{sp.dx_slabs, ld, s.rows, s.features, false}, stream, what);
       if (weights)
         tail = sum_tail(sp.dx_slabs, sp.dx.splits, ld, ex);
       else if (st == SDNN_OK)
@@ -617,9 +632,9 @@ sdnn_status grad_of(const Sizes &s, const Inputs<T> &in, int activation, const K
     const TwoStores<T> e{to.dwg, to.dwu, to.lddg, to.lddu, s.hidden, s.half(), rows, s.features,
                          (!to.dwg || vector_rows(to.dwg, to.lddg)) && (!to.dwu || vector_rows(to.dwu, to.lddu))};
     if (sp.dw.splits == 1) {
-      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, e, stream, what, false, 1, tail);
+      st = product<kProduct, true, true, false>(sp.dw, d, o.x, rows, s.features, s.rows, e, stream, what, tail);
     } else {
-      st = run_shape<kProduct, true, true>(sp.dw, d, o.x, rows, s.features, s.rows, Accumulate{sp.dw_slabs, ld, rows, s.features, false}, stream, what, false, 1, tail);
+      st = product<kProduct, true, true, false>(sp.dw, d, o.x, rows, s.features, s.rows, Accumulate{sp.dw_slabs, ld, rows, s.features, false}, stream, what, tail);
       if (st == SDNN_OK) st = sum_slabs(sp.dw_slabs, sp.dw.splits, ld, e, stream, what);
     }
   }

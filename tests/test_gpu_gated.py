@@ -123,6 +123,27 @@ def test_layer_and_gradient(rows, hidden, features, dtype):
         assert c.torch.equal(v, kept[k]), f"{k} differs where g and u are computed again"
 
 
+@pytest.mark.parametrize("rows,hidden,features,pad,offset", [(310, 2048, 1000, 0, 0), (1021, 2047, 1000, 0, 0), (2049, 640, 262, 3, 5), (1100, 402, 1501, 1, 0), (1055, 417, 1503, 0, 1),
+                                                              (8192, 400, 400, 24, 8), (400, 4000, 1030, 0, 0)])
+def test_gradient_of_middle_sizes(rows, hidden, features, pad, offset):
+    """fp32: about a block of 128 x 128 outputs for every CU; rows, outputs and features that end inside one, and inside a step
+    of 32; split sums, and one of the results alone."""
+    log(f"gated {rows} x {hidden} x {features} {pad} {offset}")
+    c = Case(rows, hidden, features, "float32", act="gelu", seed=hidden, pad=pad, offset=offset)
+    around = [t.as_strided((t.untyped_storage().nbytes() // t.element_size(),), (1,), 0) for t in (c.dx, c.dwg, c.dwu)]
+    before = [a.isnan().sum() for a in around]
+    c.run()
+    c.check()
+    assert [a.isnan().sum() for a in around] == before
+    kept = {k: v.clone() for k, v in c.outputs().items()}
+    for only in ("dx", "dwg", "dwu"):
+        v = c.outputs()[only]
+        v.fill_(3)
+        to = [v if name == only else None for name in ("dx", "dwg", "dwu")]
+        c.r.gated_gradient(c.x, c.wg, c.wu, c.dh, *to, c.ws, activation=c.act, gate=c.gate, up=c.up)
+        assert c.torch.equal(v, kept[only]), only
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
 def test_activations_of_exact_sums(act, dtype):
