@@ -3,6 +3,8 @@
 // tile.h's blocks take one part of each operand a slab: six slabs bring 12 parts of 64 values of k, of which 6 are different. Here a
 // step of 32 values brings those 6 alone, and its six products are taken from registers: half the bytes from L2 and LDS. 48 KB
 // a step, three steps on their way; 8 waves of 64 x 32 outputs read a step's fragments while they multiply the last one's.
+// Bound by the matrix instructions and by what LDS gives beside them, about half of each's rate. The gradient's products of
+// 1021 x 1000 to 2047 take 46 and 45 us so, 68 and 73 in tile.h's blocks of the same size.
 #ifndef SDNN_PARTS_H
 #define SDNN_PARTS_H
 
@@ -15,7 +17,12 @@ using tile::i32x4;
 
 constexpr int kSide = 128, kStep = 32, kThreads = 512;
 constexpr int kPart = kSide * kStep * 2;  // bytes of a part of an operand's step: 16 a lane
-constexpr double kStepUs = 1.3;            // of a step where every CU has a block
+// Microseconds of a step in the model that chooses between these blocks and tile.h's, whose own figures are a third too short
+// for three parts (a step takes 1.1 to 1.2 where every CU has a block). The gradient with 0.8, with 1.0 and with 1.3, and with
+// tile.h's blocks alone, us: 310 x 300 to 2000 42 / 47 / 47 / 47, 400 x 4096 to 8192 734 / 743 / 748 / 776, 2000 x 2048 to 4096
+// 642 / 638 / 661 / 678, 4096 x 4096 to 8192 4955 / 4956 / 5070 / 5060; with blocks of this kind for everything 600 x 600 to 600
+// takes 82 instead of 49.
+constexpr double kStepUs = 0.8;
 
 // Moves a step of one operand to LDS, a part at a time. along: rows of 64 bytes, their four chunks permuted by the row; across: 32 rows
 // of k of 256 bytes, as tile::Loader lays them. Reads past the operand and past step `end` are zeros.
@@ -131,9 +138,10 @@ struct Block {
       // step s + 1 has arrived, and every wave holds the fragments of step s: its buffer takes step s + 3
       tile::wait_loads<6 * (kStages - 2)>();
       tile::meet();
-      load(s + kStages, at);
+      const int freed = at;
       at = at + 1 == kStages ? 0 : at + 1;
       read(next, lds + at * kStage);
+      load(s + kStages, freed);
       constexpr int kA[6] = {2, 0, 1, 1, 0, 0}, kB[6] = {0, 2, 1, 0, 1, 0};  // the smallest products first
 #pragma unroll
       for (int p = 0; p < 6; ++p)
@@ -141,6 +149,14 @@ struct Block {
         for (int i = 0; i < kTM; ++i)
 #pragma unroll
           for (int j = 0; j < kTN; ++j) acc[i][j] = tile::mfma<tile::KIND_BF16>(now.b[kB[p]][j], now.a[kA[p]][i], acc[i][j]);
+      // a read after every one or two products (1500 x 1000 to 3000: the two products 13 us faster than in the compiler's order)
+      constexpr int kReads = kTM * 3 * (ACROSS_A ? 2 : 1) + kTN * 3 * (ACROSS_B ? 2 : 1), kProducts = 6 * kTM * kTN, kEach = kProducts / kReads;
+#pragma unroll
+      for (int i = 0; i < kReads; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, kProducts - kReads * kEach, 0);
     };
 #pragma unroll 1
     for (int s = s0; s < s1; s += 2) {  // (a step past s1 is zeros)
