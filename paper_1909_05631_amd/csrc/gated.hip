@@ -20,8 +20,8 @@
 //     u), dg and du 0.27 ms (1.34 GB at 5.0 TB/s), dx and the weights' gradients 1.6 ms each (1370).
 //   2000 x 4096 to 16384, bf16, the layer alone: 433 us, 1240 TFLOP/s.
 //   64 x 1024 to 4096, bf16: 35 us, four launches of 4 to 10 us, and the host's time for them.
-//   1021 x 1000 to 2047, fp32: 161 us: the layer 48 us and 13 for x and w in parts, the gradient's two products 46 and 45 us in
-//     three parts (185 TFLOP/s of 275: one block a CU, see parts.h), 22 us for writing parts.
+//   1021 x 1000 to 2047, fp32: 174 us: the layer 48 us and 13 for x and w in parts, the gradient's two products 46 and 45 us in
+//     three parts (185 TFLOP/s of 275: one block a CU, see parts.h), 22 us for its slopes and parts.
 //   1 x 4096 to 16384, bf16: 50 us, the weights at 5.3 TB/s; 16 rows 55 us.
 #include "dense.h"
 #include "few.h"
@@ -44,12 +44,13 @@ namespace {
 
 constexpr int64_t kMaxHidden = 1 << 19;    // a row of dg and du in three parts is then the longest that the tiles take
 constexpr int64_t kSplitValues = 1 << 24;  // values of g and u whose features may be split: past that there is a 256 x 256 block for every CU
-// fp32 rows or outputs (the fewer of the two) for the plain fp32 products, which read the operands as they are: the layer's and its
-// gradient's, and the gradient's where all three sizes' product is at most kSmall. us, plain and in parts, 1000 to 2048: the layer 64
-// rows 18 / 25, 192 rows 26 / 26, 300 rows 43 / 32, the gradient 64 rows 29 / 39, 192 48 / 47, 250 54 / 53, 300 66 / 59; 4096 to 8192:
-// the layer 128 rows 147 / 211, 192 210 / 238, 300 402 / 271, the gradient 128 337 / 414, 192 446 / 476, 256 618 / 544; 2000 x 1000
-// to 250, the gradient, 61 / 55, but 300 x 300 to 400 24 / 29.
-constexpr int64_t kPlain = 192, kPlainSmall = 300, kSmall = 1 << 27;
+// fp32 rows or outputs for the plain fp32 products, which read the operands as they are, and, for the gradient, the fewer of both
+// where all three sizes' product is at most kSmall. us, plain and in parts: the layer 1000 to 2048, 64 rows 18 / 25, 192 rows 26 / 26,
+// 300 rows 43 / 32, 4096 to 8192, 128 rows 147 / 211, 192 210 / 238, 300 402 / 271, 8192 x 4096 to 64 outputs 86 / 104, 96 118 / 122,
+// 128 146 / 129; the gradient 1000 to 2048, 64 rows 29 / 39, 192 48 / 47, 250 54 / 53, 300 66 / 59, 4096 to 8192, 128 337 / 414, 192
+// 446 / 476, 256 618 / 544, 8192 x 4096 to 64 outputs 194 / 224, 96 329 / 270; but 300 x 300 to 400 24 / 29, 2000 x 1000 to 128
+// 42 / 46, to 250 61 / 55.
+constexpr int64_t kPlainRows = 192, kPlainHidden = 96, kPlainSmall = 300, kSmall = 1 << 28;
 
 // act(g) and, for the gradient, act'(g).
 struct Activated {
@@ -420,8 +421,10 @@ __global__ __launch_bounds__(256) void k_zero(T *out, int64_t ld, int64_t rows, 
 struct Sizes {
   int64_t rows, hidden, features;
   int32_t dtype;
-  int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, hidden) <= kPlain ? KIND_F32 : KIND_SPLIT; }
-  int product_kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : std::min(rows, hidden) <= (rows * hidden <= kSmall / features ? kPlainSmall : kPlain) ? KIND_F32 : KIND_THREE; }  // the gradient's
+  bool plain() const { return rows <= kPlainRows || hidden <= kPlainHidden; }
+  int kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : plain() ? KIND_F32 : KIND_SPLIT; }
+  bool small() const { return std::min(rows, hidden) <= kPlainSmall && rows * hidden <= kSmall / features; }
+  int product_kind() const { return dtype == SDNN_BF16 ? KIND_BF16 : plain() || small() ? KIND_F32 : KIND_THREE; }  // the gradient's
   int bytes() const { return dtype_bytes(dtype); }
   // Bytes of a row of features written anew, as the layer and as the gradient take it.
   int64_t pitch(int kind) const {

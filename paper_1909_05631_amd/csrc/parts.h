@@ -17,8 +17,8 @@ using tile::i32x4;
 
 constexpr int kSide = 128, kStep = 32, kThreads = 512;
 constexpr int kPart = kSide * kStep * 2;  // bytes of a part of an operand's step: 16 a lane
-// Microseconds of a step in the model that chooses between these blocks and tile.h's, whose own figures are a third too short
-// for three parts (a step takes 1.1 to 1.2 where every CU has a block). The gradient with 0.8, with 1.0 and with 1.3, and with
+// Microseconds of a step in the model that chooses between these blocks and tile.h's. A step takes 1.1 to 1.2 where every CU has a
+// block, but that model's figures for tile.h's are too short for three parts as well. The gradient with 0.8, with 1.0 and with 1.3, and with
 // tile.h's blocks alone, us: 310 x 300 to 2000 42 / 47 / 47 / 47, 400 x 4096 to 8192 734 / 743 / 748 / 776, 2000 x 2048 to 4096
 // 642 / 638 / 661 / 678, 4096 x 4096 to 8192 4955 / 4956 / 5070 / 5060; with blocks of this kind for everything 600 x 600 to 600
 // takes 82 instead of 49.
@@ -87,6 +87,7 @@ struct Reader {
 
 template <bool ACROSS_A, bool ACROSS_B, bool TWO_B>
 struct Block {
+  static_assert(ACROSS_B || !TWO_B, "two matrices follow each other along k, which is across");
   static constexpr int kThreads = parts::kThreads, kTM = 4, kTN = 2, kStages = 3, kStage = 6 * kPart, kLds = kStages * kStage;
   f32x4 acc[kTM][kTN];
   static __device__ __forceinline__ int wave() { return tile::uniform(threadIdx.x >> 6); }

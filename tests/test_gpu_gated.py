@@ -124,7 +124,7 @@ def test_layer_and_gradient(rows, hidden, features, dtype):
 
 
 @pytest.mark.parametrize("rows,hidden,features,pad,offset", [(310, 2048, 1000, 0, 0), (1021, 2047, 1000, 0, 0), (2049, 640, 262, 3, 5), (1100, 402, 1501, 1, 0), (1055, 417, 1503, 0, 1),
-                                                              (8192, 400, 400, 24, 8), (400, 4000, 1030, 0, 0), (193, 2048, 1000, 0, 0), (1000, 200, 1200, 0, 2)])
+                                                              (8192, 400, 400, 24, 8), (400, 4000, 1030, 0, 0), (193, 2048, 1000, 0, 0), (1000, 200, 1400, 0, 2), (2500, 97, 1200, 0, 0)])
 def test_gradient_of_middle_sizes(rows, hidden, features, pad, offset):
     """fp32: about a block of 128 x 128 outputs for every CU; rows, outputs and features that end inside one, and inside a step
     of 32; split sums, and one of the results alone."""
