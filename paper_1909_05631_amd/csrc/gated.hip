@@ -20,7 +20,7 @@
 //     u), dg and du 0.27 ms (1.34 GB at 5.0 TB/s), dx and the weights' gradients 1.6 ms each (1370).
 //   2000 x 4096 to 16384, bf16, the layer alone: 433 us, 1240 TFLOP/s.
 //   64 x 1024 to 4096, bf16: 35 us, four launches of 4 to 10 us, and the host's time for them.
-//   1021 x 1000 to 2047, fp32: 174 us: the layer 48 us and 13 for x and w in parts, the gradient's two products 46 and 45 us in
+//   1021 x 1000 to 2047, fp32: 167 us: the layer 48 us and 13 for x and w in parts, the gradient's two products 46 and 45 us in
 //     three parts (185 TFLOP/s of 275: one block a CU, see parts.h), 22 us for its slopes and parts.
 //   1 x 4096 to 16384, bf16: 50 us, the weights at 5.3 TB/s; 16 rows 55 us.
 #include "dense.h"
