@@ -50,6 +50,12 @@ inline bool good_group(int64_t g) { return g == 32 || g == 64 || g == 128; }
 template <class T>
 __device__ __forceinline__ float rounded(float v) { return (float)(T)v; }
 
+// (v - offset) / scale. A difference past the largest number is taken of halves, which are exact there: the scale is then 2^124 or more.
+__device__ __forceinline__ float steps_over(float v, float offset, float scale) {
+  const float d = v - offset;
+  return __builtin_isfinite(d) ? d / scale : (0.5f * v - 0.5f * offset) / (0.5f * scale);
+}
+
 // Eight values a lane, GROUP / 8 lanes a group. The scale and offset are rounded to the weights' type before codes are taken
 // with them, so that these are the nearest to what they will stand for.
 template <class T, int GROUP, bool OFFSETS>
@@ -87,7 +93,7 @@ __global__ __launch_bounds__(256) void k_quantize(const T *w, int64_t ld, int64_
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float q = OFFSETS ? 0.0f : 8.0f;
-        if (c * 8 + i < n && scale > 0.0f) q = OFFSETS ? fminf(fmaxf(rintf((v[i] - offset) / scale), 0.0f), 15.0f) : fminf(fmaxf(rintf(v[i] / scale), -8.0f), 7.0f) + 8.0f;
+        if (c * 8 + i < n && scale > 0.0f) q = OFFSETS ? fminf(fmaxf(rintf(steps_over(v[i], offset, scale)), 0.0f), 15.0f) : fminf(fmaxf(rintf(v[i] / scale), -8.0f), 7.0f) + 8.0f;
         word |= (uint32_t)q << 4 * i;
       }
       if (c < per) {
