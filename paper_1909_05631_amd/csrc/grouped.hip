@@ -56,6 +56,13 @@ __device__ __forceinline__ float steps_over(float v, float offset, float scale) 
   return __builtin_isfinite(d) ? d / scale : (0.5f * v - 0.5f * offset) / (0.5f * scale);
 }
 
+// (high - low) / 15. Within a factor of two of each other their difference is exact, and quotients of each could cancel to
+// nothing of it (low 1, high the next number). Others lose at most two bits as quotients, whose difference passes no largest number.
+__device__ __forceinline__ float step_of(float low, float high) {
+  const bool near = low > 0.0f ? high <= 2.0f * low : low >= 2.0f * high;
+  return near ? (high - low) / 15.0f : high / 15.0f - low / 15.0f;
+}
+
 // Eight values a lane, GROUP / 8 lanes a group. The scale and offset are rounded to the weights' type before codes are taken
 // with them, so that these are the nearest to what they will stand for.
 template <class T, int GROUP, bool OFFSETS>
@@ -87,8 +94,7 @@ __global__ __launch_bounds__(256) void k_quantize(const T *w, int64_t ld, int64_
         bad |= __shfl_xor((int)bad, d) != 0;
       }
       const float offset = OFFSETS ? rounded<T>(low) : 0.0f;
-      // (a range past the largest number is no infinity this way)
-      const float scale = bad ? __builtin_nanf("") : rounded<T>(OFFSETS ? high / 15.0f - low / 15.0f : fmaxf(-low, high) / 7.0f);
+      const float scale = bad ? __builtin_nanf("") : rounded<T>(OFFSETS ? step_of(low, high) : fmaxf(-low, high) / 7.0f);
       uint32_t word = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -1,4 +1,5 @@
-"""Weights of 4 bits on the GPU where a group's values or their differences reach the ends of fp32's range.
+"""Weights of 4 bits on the GPU where a group's values or their differences reach the ends of fp32's range, or where its range is
+far smaller than its values.
 
 Bounds. A code is the nearest where its value is as near as any other's, but for the roundings of a difference and of a
 quotient of at most 16 steps, 2^-24 of them each: 2^-19 steps either way, 2^-18 between two codes' distances."""
@@ -45,4 +46,31 @@ def test_ranges_past_the_largest_number(group, dtype):
     w[2, 5:] = 0.0
     (q, s, o), out, _ = quantised(w, group, True)
     assert bool(out.isfinite().all())
+    assert_nearest(torch, w, q, s, o)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_ranges_far_smaller_than_their_values(group, dtype):
+    """With offsets: the scale is (max - min) / 15, off by at most 2^-24 of it where the two are within a factor of two, their
+    difference exact; else by the roundings of two quotients, together at most three times the difference's size, and of their
+    difference: 4 * 2^-24. bf16 rounds once more, by 2^-8."""
+    torch = torch_cuda()
+    log(f"grouped narrow range {group} {dtype}")
+    dt, gen = getattr(torch, dtype), torch.Generator("cuda").manual_seed(group)
+    lows = [1.0, -1.0, 1000.0, -1000.0, 1e6, -1e6, 1e30, -1e30, 1e-30, -1e-30, 2.0 ** 127, -(2.0 ** 127)]
+    widths = [2.0 ** -k for k in ((23, 22, 21, 20, 16, 10, 7, 5, 2, 1) if dtype == "float32" else (7, 6, 5, 4, 3, 2, 1))] + [0.0, 0.9]
+    low = torch.tensor(lows, device="cuda").repeat_interleave(len(widths))[:, None]
+    width = torch.tensor(widths, device="cuda").repeat(len(lows))[:, None]
+    near = torch.rand(low.shape[0], 200, generator=gen, device="cuda")
+    near[:, ::32] = 0.0
+    near[:, 1::32] = 1.0
+    w = (low + low * width * near).to(dt)
+    (q, s, o), out, scales = quantised(w, group, True)
+    wide = torch.nn.functional.pad(w.double(), (0, scales.shape[1] * group - 200), value=float("nan")).reshape(w.shape[0], -1, group)
+    there = ~wide.isnan()
+    top, bottom = torch.where(there, wide, -torch.inf).amax(2), torch.where(there, wide, torch.inf).amin(2)
+    want = (top - bottom) / 15
+    unit = 2.0 ** -22 + (2.0 ** -8 if dtype == "bfloat16" else 0.0)
+    assert bool((want > 0).any()) and bool(((scales.double() - want).abs() <= unit * want).all())
     assert_nearest(torch, w, q, s, o)
