@@ -367,8 +367,9 @@ sdnn_status sdnn_clip(const sdnn_tensor *tensors, int64_t n_tensors, float max_n
 int64_t sdnn_grouped_groups(int64_t n_values, int32_t group);
 
 /* Quantise w (n_rows x n_values, row stride ldw). Without offsets a group's scale is its largest magnitude over 7; with
- * them (max - min) / 15, and the offset is the minimum. Both are rounded to `dtype`, then codes to the nearest value that
- * they can stand for, ties to the even code. A group with an infinity or a NaN stands for NaN. */
+ * them (max - min) / 15, and the offset is the minimum. Both are rounded to `dtype` (the scale to the number below where the
+ * largest code would stand for an infinity), then codes to the nearest value that they can stand for, ties to the even
+ * code. A group with an infinity or a NaN stands for NaN. */
 sdnn_status sdnn_grouped_quantize(const void *w, int64_t ldw, int32_t dtype, int64_t n_rows, int64_t n_values,
                                   int32_t group, uint8_t *codes, void *scales, void *offsets, void *hip_stream);
 

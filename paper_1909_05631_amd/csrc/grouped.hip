@@ -63,6 +63,12 @@ __device__ __forceinline__ float step_of(float low, float high) {
   return near ? (high - low) / 15.0f : high / 15.0f - low / 15.0f;
 }
 
+// The scale, or the next number below it where the largest code's value would be rounded to infinity.
+template <class T>
+__device__ __forceinline__ float finite_scale(float scale, float codes, float offset) {
+  return rounded<T>(fmaf(codes, scale, offset)) == __builtin_inff() ? __uint_as_float(__float_as_uint(scale) - (sizeof(T) == 2 ? 0x10000u : 1u)) : scale;
+}
+
 // Eight values a lane, GROUP / 8 lanes a group. The scale and offset are rounded to the weights' type before codes are taken
 // with them, so that these are the nearest to what they will stand for.
 template <class T, int GROUP, bool OFFSETS>
@@ -94,7 +100,7 @@ __global__ __launch_bounds__(256) void k_quantize(const T *w, int64_t ld, int64_
         bad |= __shfl_xor((int)bad, d) != 0;
       }
       const float offset = OFFSETS ? rounded<T>(low) : 0.0f;
-      const float scale = bad ? __builtin_nanf("") : rounded<T>(OFFSETS ? step_of(low, high) : fmaxf(-low, high) / 7.0f);
+      const float scale = bad ? __builtin_nanf("") : finite_scale<T>(rounded<T>(OFFSETS ? step_of(low, high) : fmaxf(-low, high) / 7.0f), OFFSETS ? 15.0f : 7.0f, offset);
       uint32_t word = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -9,6 +9,7 @@ from tests.gpu_util import log, torch_cuda
 from tests.test_gpu_grouped import parts_of
 
 pytestmark = pytest.mark.gpu
+MOST = {"float32": (2.0 - 2.0 ** -23) * 2.0 ** 127, "bfloat16": (2.0 - 2.0 ** -7) * 2.0 ** 127}
 
 
 def quantised(w, group, offsets):
@@ -74,3 +75,29 @@ def test_ranges_far_smaller_than_their_values(group, dtype):
     unit = 2.0 ** -22 + (2.0 ** -8 if dtype == "bfloat16" else 0.0)
     assert bool((want > 0).any()) and bool(((scales.double() - want).abs() <= unit * want).all())
     assert_nearest(torch, w, q, s, o)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("offsets", [False, True])
+def test_the_largest_numbers_are_read_back_finite(offsets, dtype):
+    """Groups whose largest magnitudes are the largest numbers of the type and those below them: within half a step and the
+    roundings of the scale (15 times 2^-8 of a step, twice where the next scale below is taken) and of the result."""
+    torch = torch_cuda()
+    log(f"grouped largest {offsets} {dtype}")
+    dt, most = getattr(torch, dtype), MOST[dtype]
+    last = 2.0 ** (127 - (7 if dtype == "bfloat16" else 23))  # the largest numbers' last place
+    tops = torch.tensor([most - k * last for k in range(120)], dtype=torch.float64, device="cuda")
+    w = torch.zeros(360, 64, dtype=torch.float64, device="cuda")
+    w[:120, 0], w[120:240, 0], w[240:, 0] = tops, -tops, most
+    w[:240:3, 1] = -w[:240:3, 0]
+    w[240:, 1] = -most * (torch.arange(120, dtype=torch.float64, device="cuda") / 120)  # offsets far from the largest number
+    w[:, 2] = w[:, 0] / 3
+    w[:, 40] = w[:, 0] * 0.9
+    w[1::2, 41] = -w[1::2, 40]
+    w = w.to(dt)
+    assert bool(w.isfinite().all()) and float(w.abs().max()) == most
+    for group in (32, 64):
+        (q, s, o), out, _ = quantised(w, group, offsets)
+        assert bool(out.isfinite().all())
+        unit = 2.0 ** -8 if dtype == "bfloat16" else 2.0 ** -22
+        assert bool(((out.double() - w.double()).abs() <= (0.5 + 30 * unit) * s + unit * w.double().abs()).all())
