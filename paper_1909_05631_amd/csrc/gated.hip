@@ -52,25 +52,38 @@ constexpr int64_t kSplitValues = 1 << 24;  // values of g and u whose features m
 // 42 / 46, to 250 61 / 55.
 constexpr int64_t kPlainRows = 192, kPlainHidden = 96, kPlainSmall = 300, kSmall = 1 << 28;
 
-// act(g) and, for the gradient, act'(g).
+// exp(x + rest), rest far smaller than x, to two units of its last place: what the exponent's rounding loses, up to 2^-17 of the
+// result, is put back as a factor.
+__device__ __forceinline__ float exp_of_sum(float x, float rest) {
+  constexpr float kLog = 1.44269504088896340736f, kLogRest = 1.44269504088896340736 - (double)kLog;
+  const float y = x * kLog, lost = fmaf(x, kLog, -y) + fmaf(x, kLogRest, rest * kLog);
+  return __builtin_amdgcn_exp2f(y) * fmaf(lost, 0.69314718055994530942f, 1.0f);
+}
+
+// act(g) and, for the gradient, act'(g), for values of type T: where act goes to zero, fp32 keeps its relative precision. bf16 has
+// no such bits, and takes exp as it is: off by (g^2 + 8) 2^-24 of itself there for gelu, (|g| + 8) 2^-24 for silu.
 struct Activated {
   float value, slope;
 };
-template <bool SLOPE>
+template <class T, bool SLOPE>
 __device__ __forceinline__ Activated activated(int activation, float g) {
+  constexpr bool kFull = sizeof(T) == 4;
   Activated a;
   a.slope = 0.0f;
   if (activation == SDNN_SILU) {
     // g p with p = 1 / (1 + exp(-g)); the exponential may be infinite: p is then 0
-    const float p = __builtin_amdgcn_rcpf(1.0f + few::exp_of(-g));  // (to one unit of its last place)
+    const float e = kFull ? exp_of_sum(__builtin_amdgcn_fmed3f(-g, -200.0f, 200.0f), 0.0f) : few::exp_of(-g);
+    const float p = __builtin_amdgcn_rcpf(1.0f + e);  // (to one unit of its last place)
     a.value = g * p;
     if (SLOPE) a.slope = fmaf(a.value, 1.0f - p, p);
   } else if (activation == SDNN_GELU) {
     // g P with P the normal distribution, whose tail below -|g| is exp(-g^2 / 2) t p(t), t = 1 / (1 + |g| / sqrt 8): p is
     // fitted to erfc's scaled form there (9th degree, by least squares reweighted towards the largest relative error, 2e-8), so that
-    // the tail keeps its relative precision, 3.3e-7 with fp32's roundings (the layer 2000 x 4096 to 16384: 456 us, with erfcf 487)
+    // the tail is within 3.7e-7 of itself with fp32's roundings (the layer 2000 x 4096 to 16384: 456 us, with erfcf 487)
     constexpr float kTail[10] = {0.141032249f, 0.14142856f, 0.119322069f, 0.112772763f, -0.0491647162f, 0.210649297f, -0.335027367f, 0.214477479f, -0.0616335161f, 0.006143176f};
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.35355339059327f, 1.0f)), e = few::exp_of(-0.5f * g * g);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.35355339059327f, 1.0f));
+    const float q = fminf(fabsf(g), 16.0f), square = q * q;  // (exp(-128) is zero)
+    const float e = kFull ? exp_of_sum(-0.5f * square, -0.5f * fmaf(q, q, -square)) : few::exp_of(-0.5f * g * g);
     float p = kTail[9];
 #pragma unroll
     for (int i = 8; i >= 0; --i) p = fmaf(p, t, kTail[i]);
@@ -114,7 +127,7 @@ struct Layer {
   }
   __device__ __forceinline__ f32x4 product(f32x4 g, f32x4 u) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g[i] = activated<false>(activation, g[i]).value * u[i];
+    for (int i = 0; i < 4; ++i) g[i] = activated<T, false>(activation, g[i]).value * u[i];
     return g;
   }
   template <class B>
@@ -364,7 +377,7 @@ __global__ __launch_bounds__(256) void k_slopes(Slopes<T> p) {
       load_some(p.dh + t * p.ldd, c, p.hidden, p.vec, d);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const Activated a = activated<true>(p.activation, g[i]);
+        const Activated a = activated<T, true>(p.activation, g[i]);
         g[i] = c + i < p.hidden ? d[i] * u[i] * a.slope : 0.0f;
         u[i] = c + i < p.hidden ? d[i] * a.value : 0.0f;
       }
