@@ -50,20 +50,17 @@ inline bool good_group(int64_t g) { return g == 32 || g == 64 || g == 128; }
 template <class T>
 __device__ __forceinline__ float rounded(float v) { return (float)(T)v; }
 
-// (v - offset) / scale. A difference past the largest number is taken of halves, which are exact there: the scale is then 2^124 or more.
-__device__ __forceinline__ float steps_over(float v, float offset, float scale) {
-  const float d = v - offset;
-  return __builtin_isfinite(d) ? d / scale : (0.5f * v - 0.5f * offset) / (0.5f * scale);
-}
-
-// (high - low) / 15. Within a factor of two of each other their difference is exact, and quotients of each could cancel to
-// nothing of it (low 1, high the next number). Others lose at most two bits as quotients, whose difference passes no largest number.
+// (high - low) / 15. Within a factor of two of each other (of one sign) their difference is exact, and quotients of each could
+// cancel to nothing of it (low 1, high the next number). Others lose at most two bits as quotients, whose difference passes no largest
+// number.
 __device__ __forceinline__ float step_of(float low, float high) {
-  const bool near = low > 0.0f ? high <= 2.0f * low : low >= 2.0f * high;
-  return near ? (high - low) / 15.0f : high / 15.0f - low / 15.0f;
+  const float range = high - low;
+  const bool near = range <= 0.5f * fmaxf(-low, high);
+  const float step = high / 15.0f - low / 15.0f;
+  return __builtin_expect(near, false) ? range / 15.0f : step;
 }
 
-// The scale, or the next number below it where the largest code's value would be rounded to infinity.
+// The next number below a scale whose largest code's value would be rounded to infinity.
 template <class T>
 __device__ __forceinline__ float finite_scale(float scale, float codes, float offset) {
   return rounded<T>(fmaf(codes, scale, offset)) == __builtin_inff() ? __uint_as_float(__float_as_uint(scale) - (sizeof(T) == 2 ? 0x10000u : 1u)) : scale;
@@ -100,12 +97,21 @@ __global__ __launch_bounds__(256) void k_quantize(const T *w, int64_t ld, int64_
         bad |= __shfl_xor((int)bad, d) != 0;
       }
       const float offset = OFFSETS ? rounded<T>(low) : 0.0f;
-      const float scale = bad ? __builtin_nanf("") : finite_scale<T>(rounded<T>(OFFSETS ? step_of(low, high) : fmaxf(-low, high) / 7.0f), OFFSETS ? 15.0f : 7.0f, offset);
+      float scale = bad ? __builtin_nanf("") : rounded<T>(OFFSETS ? step_of(low, high) : fmaxf(-low, high) / 7.0f), from = offset, by = scale;
+      if (__builtin_expect(fmaxf(-low, high) > 0x1p127f, false)) {
+        by = scale = finite_scale<T>(scale, OFFSETS ? 15.0f : 7.0f, offset);
+        if (OFFSETS && !__builtin_isfinite(high - low)) {  // halves' differences are finite, and exact halves: the scale is 2^124 or more
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] *= 0.5f;
+          from *= 0.5f;
+          by *= 0.5f;
+        }
+      }
       uint32_t word = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float q = OFFSETS ? 0.0f : 8.0f;
-        if (c * 8 + i < n && scale > 0.0f) q = OFFSETS ? fminf(fmaxf(rintf(steps_over(v[i], offset, scale)), 0.0f), 15.0f) : fminf(fmaxf(rintf(v[i] / scale), -8.0f), 7.0f) + 8.0f;
+        if (c * 8 + i < n && scale > 0.0f) q = OFFSETS ? fminf(fmaxf(rintf((v[i] - from) / by), 0.0f), 15.0f) : fminf(fmaxf(rintf(v[i] / by), -8.0f), 7.0f) + 8.0f;
         word |= (uint32_t)q << 4 * i;
       }
       if (c < per) {
