@@ -285,6 +285,15 @@ def _asked(name: str, tensors, norm) -> tuple[list, list]:
     return list(map(attrgetter("dtype"), tensors)), list(map(torch.Tensor.data_ptr, tensors))
 
 
+def _refuse_pair(tensors, to) -> None:
+    """Refuses an output of another type than its tensor's, or of other values: of another number where both are contiguous, of
+    another shape otherwise."""
+    for i, (a, b) in enumerate(zip(tensors, to)):
+        flat = a.is_contiguous() and b.is_contiguous()
+        if a.dtype != b.dtype or (a.numel() != b.numel() if flat else a.shape != b.shape):
+            raise ValueError(f"out[{i}] is {tuple(b.shape)} of {b.dtype}, not {tuple(a.shape)} of {a.dtype}")
+
+
 def _list(tensors, out, norm):
     """The C ABI's description of a list of tensors (sdnn_tensor, seven words each) and its length."""
     _on_gpu("norm", norm)
@@ -302,15 +311,14 @@ def _list(tensors, out, norm):
     table[:, 0], table[:, 6] = addresses, codes
     table[:, 1] = table[:, 0] if to is tensors else to_addresses
     flat = all(map(torch.Tensor.is_contiguous, tensors)) and (to is tensors or all(map(torch.Tensor.is_contiguous, to)))
-    shape = torch.Tensor.numel if flat else torch.Tensor.size
-    shapes = list(map(shape, tensors))
-    if to is not tensors and (dtypes != to_dtypes or shapes != list(map(shape, to))):
-        for i, (a, b) in enumerate(zip(tensors, to)):
-            if a.dtype != b.dtype or shape(a) != shape(b):
-                raise ValueError(f"out[{i}] is {tuple(b.shape)} of {b.dtype}, not {tuple(a.shape)} of {a.dtype}")
     if flat:
+        shapes = list(map(torch.Tensor.numel, tensors))
+        if to is not tensors and (dtypes != to_dtypes or shapes != list(map(torch.Tensor.numel, to))):
+            _refuse_pair(tensors, to)
         table[:, 2], table[:, 3] = 1, shapes
     else:
+        if to is not tensors:
+            _refuse_pair(tensors, to)
         for i, (a, b) in enumerate(zip(tensors, to)):
             (rows, cols, ld), (rows_out, cols_out, ldo) = _extent(f"tensors[{i}]", a), _extent(f"out[{i}]", b)
             if rows != rows_out or cols != cols_out:  # one of them is contiguous, the other a matrix of rows
@@ -330,7 +338,7 @@ def global_norm(tensors, norm, workspace, stream=None) -> None:
 
 def clip(tensors, max_norm: float, norm, workspace, out=None, stream=None) -> None:
     """The norm, as `global_norm` has it, and every value times min(1, max_norm / norm), into the tensors of `out` (of the same
-    types and shapes, contiguous ones of as many values; None: the tensors themselves)."""
+    types and shapes; next to a contiguous tensor, a contiguous one of as many values; None: the tensors themselves)."""
     table, n = _list(tensors, out, norm)
     _call(norm, "sdnn_clip", table.ctypes.data, n, max_norm, _vector("norm", norm, 1, torch.float32, norm), *_workspace(workspace, norm),
           _stream_handle(stream))
