@@ -284,6 +284,13 @@ struct Four {
   T v[4];
 };
 
+// Orders a wave's LDS stores and the reads of what other lanes of it stored. (They are carried out in the order in which the
+// wave issues them; this keeps the compiler to it, and costs nothing.)
+__device__ __forceinline__ void wave_meets() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Shapes of a workgroup: 16 rows of x in half a CU's LDS or all of it, 32 or 64 rows, whose fragments serve two tiles of
 // outputs each. A wave multiplies STEPS steps at a time, with those of the next AHEAD times on their way.
 template <int TILES, int OUTS, int STEPS, int AHEAD, int WAVES, int PER_SIMD, int ROOM>
@@ -379,12 +386,14 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kPerSimd) void k_few(Few<T> p) {
     const auto multiply = [&](const i32x4 (&codes)[OUTS], int s) {
       const int g0 = (first_step + s) * 4 >> SHIFT;
       if (g0 >= next) {  // 16 more groups
+        wave_meets();  // what other lanes read of the last ones
 #pragma unroll
         for (int o = 0; o < OUTS; ++o) {
           T *to = held + (o * 32 + i16) * kHeldPitch + 4 * j4;
           *(Four<T> *)to = next_scales[o];
           if constexpr (OFFSETS) *(Four<T> *)(to + 16 * kHeldPitch) = next_offsets[o];
         }
+        wave_meets();
         next += kHeld;
         ask();
       }
@@ -463,6 +472,7 @@ __global__ __launch_bounds__(64 * S::kWaves, S::kPerSimd) void k_few(Few<T> p) {
     }
     if (TILES == 1 && p.parts > 1) {
       f32x4 *room = (f32x4 *)wave_room[wave];
+      wave_meets();  // its scales have been read
       room[lane] = acc[0][0];
       __syncthreads();
       if (part == 0)
