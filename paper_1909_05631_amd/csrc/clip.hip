@@ -1,10 +1,11 @@
 // The common norm of a list of tensors, n = sqrt(sum of v^2 over all of them), and the list scaled by min(1, most / n).
 //
-// The list is cut into pieces of one size, about 2048 for all of it (8 workgroups a CU, all resident at once, so that none
-// waits for another). One launch for every 136 tensors (64 where one has rows apart from each other), whose descriptions
-// travel as its arguments, leaves each piece's sum of squares and its description in the workspace; one more goes over all pieces: every workgroup sums the pieces' sums for
-// itself, in the same order, and scales its piece. Neither waits for the host, and no sum depends on the order of
-// arrival: the same list gives the same bits.
+// The list is cut into pieces of one size, the list's 2048th part (a CU holds 8 workgroups, so 2048 run at once). Every
+// tensor's last piece may be a shorter one: up to a tensor's number more pieces than 2048, which begin as others end (2077 for 240
+// tensors of 77 MB). One launch for every 136 tensors (64 where one has rows apart from each other), whose descriptions travel
+// as its arguments, leaves each piece's sum of squares and its description in the workspace; one more goes over all pieces: every
+// workgroup sums the pieces' sums for itself, in the same order, and scales its piece. Neither waits for the host, and no
+// sum depends on the order of arrival: the same list gives the same bits.
 //
 // Squares and sums are taken in 64 bits: a list's norm is exact to its rounding to fp32 whatever the values' sizes (squares of
 // 1e-45 and of 3e38 are normal numbers there), and memory still bounds the pass.

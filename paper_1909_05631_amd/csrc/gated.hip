@@ -49,7 +49,7 @@ constexpr int64_t kSplitValues = 1 << 24;  // values of g and u whose features m
 // 300 rows 43 / 32, 4096 to 8192, 128 rows 147 / 211, 192 210 / 238, 300 402 / 271, 8192 x 4096 to 64 outputs 86 / 104, 96 118 / 122,
 // 128 146 / 129; the gradient 1000 to 2048, 64 rows 29 / 39, 192 48 / 47, 250 54 / 53, 300 66 / 59, 4096 to 8192, 128 337 / 414, 192
 // 446 / 476, 256 618 / 544, 8192 x 4096 to 64 outputs 194 / 224, 96 329 / 270; but 300 x 300 to 400 24 / 29, 2000 x 1000 to 128
-// 42 / 46, to 250 61 / 55.
+// 42 / 46, to 250 61 / 55. (One border of outputs for both: the gradient's own would be 64, since it pads halves to 64 outputs.)
 constexpr int64_t kPlainRows = 192, kPlainHidden = 96, kPlainSmall = 300, kSmall = 1 << 28;
 
 // exp(x + rest), rest far smaller than x, to two units of its last place: what the exponent's rounding loses, up to 2^-17 of the
