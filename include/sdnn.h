@@ -313,8 +313,8 @@ size_t sdnn_gated_workspace_bytes(int64_t n_rows, int64_t n_hidden, int64_t n_fe
  *   sdnn_gated_grad. None of the three may overlap an input or another.
  * g and u are fp32 sums, of exact products for bf16 inputs; fp32 inputs are multiplied as they are or as two fp16 parts
  * each (22 bits or more of each value down to 2^-17 of its row's largest). h is taken from these sums, whether they are kept or
- * not, and rounded once; for fp32 act keeps its relative precision where it goes to zero. An infinity or a NaN reaches the results of its own row of x or of its own outputs alone; NaN
- * may stand where the formula has an infinity. */
+ * not, and rounded once; for fp32 act keeps its relative precision where it goes to zero. An infinity or a NaN reaches the
+ * results of its own row of x or of its own outputs alone; NaN may stand where the formula has an infinity. */
 sdnn_status sdnn_gated(const void *x, int64_t ldx, const void *w_gate, int64_t ldw_gate, const void *w_up, int64_t ldw_up,
                        int32_t dtype, int32_t activation, int64_t n_rows, int64_t n_hidden, int64_t n_features, void *h,
                        int64_t ldh, void *gate, int64_t ldgate, void *up, int64_t ldup, void *workspace,
